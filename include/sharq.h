@@ -397,6 +397,149 @@ SHARQ_API sharq_status sharq_linear_grouped(const sharq_act *a, const int32_t *r
                                   const sharq_weight *w, void *Y, sharq_dtype ydt, int64_t ldy,
                                   void *stream);
 
+/*
+ * A paged key/value cache: what lies between the qkv projection's output and
+ * the o projection's input of a decoder layer whose linears are the ones above.
+ * A page holds page_size consecutive tokens of one sequence, for every
+ * key/value head; a sequence's page table names its pages in order.
+ *
+ *   pages, page_size   pages of the pool; tokens of a page, a power of two in
+ *                      [16, 1024].
+ *   kv_heads, head_dim key/value heads; their width, 64 or 128.
+ *                      pages * kv_heads * page_size is below 2^31.
+ *   fmt                SHARQ_KV_BF16: k, v bf16 [pages][kv_heads][page_size][head_dim].
+ *                      SHARQ_KV_MXFP4: k, v E2M1 codes (two a byte, the lower
+ *                      index in the low nibble) [pages][kv_heads][page_size][head_dim/2]
+ *                      and k_scale, v_scale E8M0 [pages][kv_heads][page_size][head_dim/32],
+ *                      one per 32 consecutive values of a token's head.
+ *   scale_rule         MXFP4: the sharq_scale_rule that sharq_kv_append applies.
+ *   k, v 16-byte aligned, the scales 4-byte aligned.
+ */
+typedef enum { SHARQ_KV_BF16 = 0, SHARQ_KV_MXFP4 = 1 } sharq_kv_format;
+
+typedef struct {
+  int64_t pages;
+  int32_t page_size, kv_heads, head_dim;
+  sharq_kv_format fmt;
+  void *k, *v;
+  uint8_t *k_scale, *v_scale;
+  sharq_scale_rule scale_rule;
+} sharq_kv_cache;
+
+/*
+ * The sequences of a call.  Sequence s owns the rows [row_offsets[s],
+ * row_offsets[s + 1]) of the call's row tensors and has lens[s] tokens in the
+ * cache, its rows of this call among them, which are its last ones: row i of
+ * its n is the token at position lens[s] - n + i.  A single new token is n = 1,
+ * a whole prompt n = lens[s].
+ *
+ *   seqs, rows    sequences; rows of the row tensors, at least row_offsets[seqs].
+ *                 Rows behind the last sequence are padding: neither looked at
+ *                 nor written.
+ *   max_rows      no sequence has more rows in this call.
+ *   max_len       no sequence has more tokens; max_len <= ld_table * page_size
+ *                 and at most 2^30.
+ *   row_offsets   device int32 [seqs + 1], non-decreasing, first 0.
+ *   lens          device int32 [seqs].
+ *   page_table    device int32 [seqs][ld_table].  Entries of pages that hold no
+ *                 token that the call reads or writes may hold anything.
+ * The device arrays are read on the device; the host never waits for them.  An
+ * entry of the page table outside [0, pages) is an absent page: its tokens are
+ * not stored by sharq_kv_append, read as zeros by sharq_kv_read and invisible to
+ * sharq_attention.  So are tokens at negative positions (more rows than
+ * lens[s]).  Pages that a call writes belong to one sequence alone.
+ */
+typedef struct {
+  int64_t seqs, rows, max_rows, max_len, ld_table;
+  const int32_t *row_offsets, *lens, *page_table;
+} sharq_kv_batch;
+
+/* Bytes of each buffer of a cache (0 k, 1 v, 2 k_scale, 3 v_scale), from its
+ * sizes and format alone.  0 for an unused buffer or invalid sizes. */
+SHARQ_API size_t sharq_kv_buffer_bytes(const sharq_kv_cache *c, int32_t which);
+
+/*
+ * Rotates the rows' queries and keys by their positions and puts the keys and
+ * values into the cache, in one pass over the qkv projection's output.
+ *   Q [rows][q_heads * head_dim], K, V [rows][kv_heads * head_dim]: bf16, row
+ *   strides ldq, ldk, ldv elements (slices of one qkv output, usually).
+ *   q_heads may be 0 (Q, Q_out unused).
+ *   cos, sin: fp32 [angles][head_dim / 2], the angle tables, row = position;
+ *   16-byte aligned.  NULL, both of them: nothing is rotated.
+ *   positions: device int32 [rows], the rows of the angle tables to use, or
+ *   NULL: the tokens' positions in their sequences.
+ * With h = head_dim / 2, y_j = x_j cos_j - x_{j+h} sin_j and
+ * y_{j+h} = x_{j+h} cos_j + x_j sin_j for j < h, every product and sum rounded
+ * to fp32 and the result once to bf16 (Q_out, row stride ldqo; it may be Q
+ * itself with ldqo == ldq) or to the cache's format.  Values are not rotated.
+ * A row at a negative position, or whose angle is not in the tables, is left
+ * out: neither its query nor its key and value are written.
+ */
+SHARQ_API sharq_status sharq_kv_append(const void *Q, const void *K, const void *V, sharq_dtype xdt, int64_t q_heads,
+                                       int64_t ldq, int64_t ldk, int64_t ldv, const float *cos, const float *sin,
+                                       int64_t angles, const int32_t *positions, const sharq_kv_cache *cache,
+                                       const sharq_kv_batch *batch, void *Q_out, int64_t ldqo, void *stream);
+
+/*
+ * Reads the rows' keys and values back from the cache (keys as they were
+ * stored, rotated): K, V [rows][kv_heads * head_dim] bf16, row strides ldk, ldv,
+ * 16-byte aligned with 16-byte row strides.  An MXFP4 value E2M1 * 2^e is a
+ * bf16, so nothing is rounded.  row_offsets that cover lens read whole sequences.
+ */
+SHARQ_API sharq_status sharq_kv_read(const sharq_kv_cache *cache, const sharq_kv_batch *batch, void *K, int64_t ldk,
+                                     void *V, int64_t ldv, sharq_dtype ydt, void *stream);
+
+/*
+ * What a row sees of its sequence: the row at position p sees the tokens
+ * t <= p with p - t < window (window 0: all of them) or t < sinks.
+ *   scale         factor of the scores q.k, positive and finite.
+ *   prefix_table, prefix_len
+ *                 tokens that all sequences of the call share: those at the
+ *                 positions below prefix_len (a multiple of page_size, at most
+ *                 max_len) lie on the pages of prefix_table (device int32
+ *                 [prefix_len / page_size]) for every sequence, whose own page
+ *                 table entries for them are not looked at.  Their keys and
+ *                 values are then read for all sequences together.  NULL and 0:
+ *                 none.  The result is that of the same call without a shared
+ *                 prefix whose page tables name these pages, but for the order
+ *                 of fp32 sums.
+ */
+typedef struct {
+  float scale;
+  int64_t window, sinks;
+  const int32_t *prefix_table;
+  int64_t prefix_len;
+} sharq_attn;
+
+/* Bytes of workspace that sharq_attention needs for these sizes (the device
+ * arrays are not looked at); 0: none needed, or invalid arguments. */
+SHARQ_API size_t sharq_attention_workspace_bytes(const sharq_kv_cache *cache, const sharq_kv_batch *batch,
+                                                 const sharq_attn *attn, int64_t q_heads);
+
+/*
+ * Causal attention of the rows over their cached sequences:
+ *   O = softmax(scale Q K^T over the visible tokens) V,
+ * K and V including the rows' own (appended before).  Query head h reads
+ * key/value head h / (q_heads / kv_heads); q_heads is a multiple of kv_heads,
+ * at most 128 times.  One call takes prompts, chunks of prompts and single
+ * tokens, mixed.
+ *   Q, O: bf16 [rows][q_heads * head_dim], row strides ldq, ldo, 16-byte aligned
+ *   with 16-byte row strides; O overlaps neither Q nor the cache.
+ *   lse: fp32 [rows][q_heads] or NULL: the natural logarithm of the sum of
+ *   e^score of every row and head.
+ *   workspace: device memory of at least sharq_attention_workspace_bytes,
+ *   16-byte aligned; its contents before and after mean nothing.  Calls that may
+ *   run at the same time need workspaces of their own.
+ * A row that sees no token gets O = 0 and lse = -inf.  Cache slots that no row
+ * of the call sees may hold anything; the keys, values and queries that are
+ * seen must be finite, their scores too.  Products are summed in fp32; the
+ * weights are rounded to bf16 for the product with V, their sum is not.
+ */
+SHARQ_API sharq_status sharq_attention(const void *Q, sharq_dtype xdt, int64_t q_heads, int64_t ldq,
+                                       const sharq_kv_cache *cache, const sharq_kv_batch *batch,
+                                       const sharq_attn *attn, void *O, int64_t ldo, float *lse, void *workspace,
+                                       size_t workspace_bytes, void *stream);
+
 SHARQ_API const char *sharq_status_str(sharq_status s);
 
 /* Library version string. */

@@ -53,6 +53,23 @@ class WeightStruct(ctypes.Structure):
                 ("tensor_scale", ctypes.c_void_p), ("scale_rule", ctypes.c_int)]
 
 
+class KVCacheStruct(ctypes.Structure):
+    _fields_ = [("pages", ctypes.c_int64), ("page_size", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("fmt", ctypes.c_int), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p), ("scale_rule", ctypes.c_int)]
+
+
+class KVBatchStruct(ctypes.Structure):
+    _fields_ = [("seqs", ctypes.c_int64), ("rows", ctypes.c_int64), ("max_rows", ctypes.c_int64),
+                ("max_len", ctypes.c_int64), ("ld_table", ctypes.c_int64), ("row_offsets", ctypes.c_void_p),
+                ("lens", ctypes.c_void_p), ("page_table", ctypes.c_void_p)]
+
+
+class AttnStruct(ctypes.Structure):
+    _fields_ = [("scale", ctypes.c_float), ("window", ctypes.c_int64), ("sinks", ctypes.c_int64),
+                ("prefix_table", ctypes.c_void_p), ("prefix_len", ctypes.c_int64)]
+
+
 def _load():
     if not os.path.exists(_LIB_PATH):
         raise ImportError(f"{_LIB_PATH} is not built; run `python -m paper_2606_26587_amd.build`")
@@ -89,6 +106,19 @@ def _load():
     L.sharq_linear_grouped.restype = ctypes.c_int
     L.sharq_linear_grouped.argtypes = [ctypes.POINTER(ActStruct), c_vp, c_vp, c_i64, ctypes.POINTER(WeightStruct),
                                        c_vp, ctypes.c_int, c_i64, c_vp]
+    cache_p, batch_p, attn_p = (ctypes.POINTER(t) for t in (KVCacheStruct, KVBatchStruct, AttnStruct))
+    L.sharq_kv_buffer_bytes.restype = ctypes.c_size_t
+    L.sharq_kv_buffer_bytes.argtypes = [cache_p, ctypes.c_int32]
+    L.sharq_kv_append.restype = ctypes.c_int
+    L.sharq_kv_append.argtypes = [c_vp, c_vp, c_vp, ctypes.c_int, c_i64, c_i64, c_i64, c_i64, c_vp, c_vp, c_i64, c_vp,
+                                  cache_p, batch_p, c_vp, c_i64, c_vp]
+    L.sharq_kv_read.restype = ctypes.c_int
+    L.sharq_kv_read.argtypes = [cache_p, batch_p, c_vp, c_i64, c_vp, c_i64, ctypes.c_int, c_vp]
+    L.sharq_attention_workspace_bytes.restype = ctypes.c_size_t
+    L.sharq_attention_workspace_bytes.argtypes = [cache_p, batch_p, attn_p, c_i64]
+    L.sharq_attention.restype = ctypes.c_int
+    L.sharq_attention.argtypes = [c_vp, ctypes.c_int, c_i64, c_i64, cache_p, batch_p, attn_p, c_vp, c_i64, c_vp, c_vp,
+                                  ctypes.c_size_t, c_vp]
     return L
 
 
@@ -177,6 +207,84 @@ class QuantWeight:
         return WeightStruct(self.N, self.K, self.experts, self.fmt, self.codes.data_ptr(), self.scale.data_ptr(),
                             self.scale_dn.data_ptr(),
                             None if self.tensor_scale is None else self.tensor_scale.data_ptr(), self.scale_rule)
+
+
+KV_FORMATS = {"bf16": 0, "mx": 1, "mxfp4": 1}
+
+
+@dataclass
+class KVCache:
+    """A paged key/value cache (device buffers; sharq_kv_cache in include/sharq.h).
+    fmt "bf16": k, v [pages, kv_heads, page_size, head_dim]; "mx": k, v uint8
+    codes [..., head_dim / 2] and their E8M0 scales uint8 [..., head_dim / 32]."""
+    fmt: str
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: Optional[torch.Tensor] = None
+    v_scale: Optional[torch.Tensor] = None
+    scale_rule: str = "floor"                 # "mx": E8M0 rule of sharq_kv_append (SCALE_RULES)
+
+    def __post_init__(self):
+        mx = KV_FORMATS[self.fmt] == 1
+        shape = tuple(self.k.shape)
+        ok = len(shape) == 4 and tuple(self.v.shape) == shape
+        for t in (self.k, self.v):
+            ok = ok and t.dtype == (torch.uint8 if mx else torch.bfloat16)
+        if mx and ok:
+            ok = self.k_scale is not None and self.v_scale is not None
+            for t in (self.k_scale, self.v_scale):
+                ok = ok and t.dtype == torch.uint8 and tuple(t.shape) == shape[:3] + (shape[3] // 16,)
+        given = [t for t in (self.k, self.v, self.k_scale, self.v_scale) if t is not None]
+        if not ok or any(not t.is_contiguous() or t.device != self.k.device for t in given):
+            raise SharqError(EINVAL, "KVCache")
+        self.pages, self.kv_heads, self.page_size = shape[:3]
+        self.head_dim = shape[3] * 2 if mx else shape[3]
+
+    def struct(self) -> KVCacheStruct:
+        return KVCacheStruct(self.pages, self.page_size, self.kv_heads, self.head_dim, KV_FORMATS[self.fmt],
+                             self.k.data_ptr(), self.v.data_ptr(), _ptr(self.k_scale), _ptr(self.v_scale),
+                             SCALE_RULES[self.scale_rule])
+
+
+@dataclass
+class KVBatch:
+    """The sequences of a call (sharq_kv_batch): row_offsets int32 [seqs + 1], lens
+    int32 [seqs] (the call's rows among them), page_table int32 [seqs, n], on the
+    GPU; the rows of the row tensors, and the host's bounds of a sequence's rows and
+    length."""
+    row_offsets: torch.Tensor
+    lens: torch.Tensor
+    page_table: torch.Tensor
+    rows: int
+    max_rows: int
+    max_len: int
+
+    def __post_init__(self):
+        seqs = self.lens.numel()
+        for t, shape in ((self.row_offsets, (seqs + 1,)), (self.lens, (seqs,)), (self.page_table[:, :0], (seqs, 0))):
+            if t.dtype != torch.int32 or tuple(t.shape) != shape or t.device != self.lens.device:
+                raise SharqError(EINVAL, "KVBatch")
+        if not (self.row_offsets.is_contiguous() and self.lens.is_contiguous() and
+                (self.page_table.shape[1] <= 1 or self.page_table.stride(1) == 1) and
+                (seqs <= 1 or self.page_table.stride(0) >= self.page_table.shape[1])):
+            raise SharqError(EINVAL, "KVBatch")
+
+    def struct(self) -> KVBatchStruct:
+        # one sequence's stride may be anything: its single row is as long as the table is wide
+        ld = self.page_table.stride(0) if self.lens.numel() > 1 else self.page_table.shape[1]
+        return KVBatchStruct(self.lens.numel(), self.rows, self.max_rows, self.max_len, ld,
+                             self.row_offsets.data_ptr(), self.lens.data_ptr(), self.page_table.data_ptr())
+
+
+def alloc_kv_cache(pages: int, page_size: int, kv_heads: int, head_dim: int, fmt: str = "bf16", device="cuda",
+                   scale_rule: str = "floor") -> KVCache:
+    """An empty paged cache; its pages are read only where something was appended."""
+    shape = (pages, kv_heads, page_size)
+    if KV_FORMATS[fmt] == 0:
+        return KVCache(fmt, *(torch.empty(shape + (head_dim,), dtype=torch.bfloat16, device=device) for _ in "kv"),
+                       scale_rule=scale_rule)
+    return KVCache(fmt, *(torch.empty(shape + (head_dim // n,), dtype=torch.uint8, device=device)
+                          for n in (2, 2, 32, 32)), scale_rule=scale_rule)
 
 
 def alloc_act(rows: int, K: int, n: int = 2, m: int = 4, fmt="mx", device="cuda", pairs: bool = False,
@@ -333,6 +441,126 @@ def sharq_linear_grouped(a: PreparedAct, row_index: Optional[torch.Tensor], expe
                                     ctypes.byref(wst), _ptr(out), _DT.get(out.dtype, -1),
                                     out.stride(0) if out.dim() == 2 else w.N, _stream(stream)),
            "sharq_linear_grouped")
+    return out
+
+
+def _rows(t: Optional[torch.Tensor], batch: KVBatch, cache: KVCache, where: str, width: int = 0):
+    """A row tensor [batch.rows, heads * head_dim] (bf16, any row stride, on the cache's device, which must be the
+    current one) -> its heads."""
+    if (t.dim() != 2 or t.shape[0] != batch.rows or t.dtype != torch.bfloat16 or (t.shape[1] > 1 and t.stride(1) != 1)
+            or t.shape[1] % cache.head_dim or (width and t.shape[1] != width) or t.device != cache.k.device):
+        raise SharqError(EINVAL, where)
+    return t.shape[1] // cache.head_dim
+
+
+def _ld(t: torch.Tensor) -> int:
+    """Row stride in elements; that of a single row means nothing."""
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _here(cache: KVCache, batch: KVBatch, where: str):
+    """The kernels are launched on the current device: the buffers must be its own."""
+    if not cache.k.is_cuda or cache.k.device != batch.lens.device or cache.k.get_device() != torch.cuda.current_device():
+        raise SharqError(EINVAL, where)
+
+
+def sharq_kv_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, cache: KVCache, batch: KVBatch,
+                    cos: Optional[torch.Tensor] = None, sin: Optional[torch.Tensor] = None,
+                    positions: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+                    stream=None) -> Optional[torch.Tensor]:
+    """Rotate the rows' queries and keys (cos, sin: fp32 [positions, head_dim / 2]; None: no rotation) and put keys and
+    values into the cache.  q, k, v: bf16 [rows, heads * head_dim], e.g. slices of the qkv projection's output.
+    Returns the rotated queries (q_out; `q` itself for an in-place update), None without q."""
+    where = "sharq_kv_append"
+    _here(cache, batch, where)
+    wk = cache.kv_heads * cache.head_dim
+    _rows(k, batch, cache, where, wk)
+    _rows(v, batch, cache, where, wk)
+    heads = 0
+    if q is not None:
+        heads = _rows(q, batch, cache, where)
+        if q_out is None:
+            q_out = torch.empty((batch.rows, q.shape[1]), dtype=q.dtype, device=q.device)
+        _rows(q_out, batch, cache, where, q.shape[1])
+    angles = 0
+    if (cos is None) != (sin is None):
+        raise SharqError(EINVAL, where)
+    if cos is not None:
+        angles = cos.shape[0]
+        for t in (cos, sin):
+            if (t.dtype != torch.float32 or tuple(t.shape) != (angles, cache.head_dim // 2) or not t.is_contiguous()
+                    or t.device != cache.k.device):
+                raise SharqError(EINVAL, where)
+    if positions is not None and (positions.dtype != torch.int32 or tuple(positions.shape) != (batch.rows,)
+                                  or not positions.is_contiguous() or positions.device != cache.k.device):
+        raise SharqError(EINVAL, where)
+    cs, bs = cache.struct(), batch.struct()
+    _check(lib.sharq_kv_append(_ptr(q), k.data_ptr(), v.data_ptr(), BF16, heads, 0 if q is None else _ld(q), _ld(k),
+                               _ld(v), _ptr(cos), _ptr(sin), angles, _ptr(positions), ctypes.byref(cs),
+                               ctypes.byref(bs), None if q is None else q_out.data_ptr(),
+                               0 if q is None else _ld(q_out), _stream(stream)), where)
+    return None if q is None else q_out
+
+
+def sharq_kv_read(cache: KVCache, batch: KVBatch, k_out: Optional[torch.Tensor] = None,
+                  v_out: Optional[torch.Tensor] = None, stream=None):
+    """The rows' cached keys and values as bf16 [rows, kv_heads * head_dim] (padding rows are left as they are)."""
+    where = "sharq_kv_read"
+    _here(cache, batch, where)
+    wk = cache.kv_heads * cache.head_dim
+    if k_out is None:
+        k_out = torch.empty((batch.rows, wk), dtype=torch.bfloat16, device=cache.k.device)
+    if v_out is None:
+        v_out = torch.empty((batch.rows, wk), dtype=torch.bfloat16, device=cache.k.device)
+    _rows(k_out, batch, cache, where, wk)
+    _rows(v_out, batch, cache, where, wk)
+    cs, bs = cache.struct(), batch.struct()
+    _check(lib.sharq_kv_read(ctypes.byref(cs), ctypes.byref(bs), k_out.data_ptr(), _ld(k_out), v_out.data_ptr(),
+                             _ld(v_out), BF16, _stream(stream)), where)
+    return k_out, v_out
+
+
+def attention_workspace_bytes(cache: KVCache, batch: KVBatch, q_heads: int, window: int = 0, sinks: int = 0,
+                              prefix_len: int = 0) -> int:
+    """Bytes of workspace of sharq_attention for these sizes."""
+    cs, bs, ts = cache.struct(), batch.struct(), AttnStruct(1.0, window, sinks, None, prefix_len)
+    return lib.sharq_attention_workspace_bytes(ctypes.byref(cs), ctypes.byref(bs), ctypes.byref(ts), q_heads)
+
+
+def sharq_attention(q: torch.Tensor, cache: KVCache, batch: KVBatch, scale: Optional[float] = None, window: int = 0,
+                    sinks: int = 0, prefix_table: Optional[torch.Tensor] = None, prefix_len: int = 0,
+                    out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                    workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Causal attention of the rows over their cached sequences (their own keys and values appended before).
+    scale: 1 / sqrt(head_dim) by default; window: 0, all tokens; sinks: first tokens that stay visible;
+    prefix_table, prefix_len: pages that all sequences begin with, read once for all.  lse: fp32 [rows, q_heads], filled
+    when given.  workspace: a buffer of attention_workspace_bytes, allocated here when needed and None."""
+    where = "sharq_attention"
+    _here(cache, batch, where)
+    heads = _rows(q, batch, cache, where)
+    if out is None:
+        out = torch.empty((batch.rows, q.shape[1]), dtype=q.dtype, device=q.device)
+    _rows(out, batch, cache, where, q.shape[1])
+    if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (batch.rows, heads)
+                            or not lse.is_contiguous() or lse.device != q.device):
+        raise SharqError(EINVAL, where)
+    if prefix_table is not None and (prefix_table.dtype != torch.int32 or not prefix_table.is_contiguous()
+                                     or prefix_table.numel() * cache.page_size < prefix_len
+                                     or prefix_table.device != q.device):
+        raise SharqError(EINVAL, where)
+    cs, bs = cache.struct(), batch.struct()
+    ts = AttnStruct(cache.head_dim ** -0.5 if scale is None else scale, window, sinks, _ptr(prefix_table), prefix_len)
+    if workspace is None:
+        size = lib.sharq_attention_workspace_bytes(ctypes.byref(cs), ctypes.byref(bs), ctypes.byref(ts), heads)
+        if size:   # on the stream that uses it: freed on return, and taken again only behind the call
+            with torch.cuda.stream(stream):
+                workspace = torch.empty(size, dtype=torch.uint8, device=q.device)
+    elif workspace.device != q.device or not workspace.is_contiguous():
+        raise SharqError(EINVAL, where)
+    _check(lib.sharq_attention(q.data_ptr(), BF16, heads, _ld(q), ctypes.byref(cs), ctypes.byref(bs), ctypes.byref(ts),
+                               out.data_ptr(), _ld(out), _ptr(lse), _ptr(workspace),
+                               0 if workspace is None else workspace.numel() * workspace.element_size(),
+                               _stream(stream)), where)
     return out
 
 
