@@ -21,39 +21,12 @@
 // P is rounded to bf16 for the second product (V is bf16, and so is the output);
 // m, l, o and the sum of P stay in fp32.
 
-#include "sharq_kv_device.hpp"
+#include "sharq_attn.hpp"
 
 namespace sharq {
 
-typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
-typedef short v4s __attribute__((ext_vector_type(4)));
-
-struct AttnArgs {
-  const uint16_t* q;
-  int64_t ldq;
-  uint16_t* o;
-  int64_t ldo;
-  float* lse;
-  KvBatchArgs b;
-  KvCacheArgs c;
-  const int32_t* prefix_table;
-  int prefix_len;
-  int group, q_heads, window, sinks, tiles;
-  float scale;   // of the scores, times log2 e
-};
-
-constexpr int kT = 64;        // tokens of a key/value tile
-constexpr int kRowsA = 128;   // rows of a workgroup: 32 a wavefront
-
-// Position of 16-byte chunk c of token t's row in an LDS tile.  The keys are
-// read 16 tokens at a time at one chunk, the values 4 tokens at a time at 64
-// consecutive bytes: under this exchange of chunks both fall on all 64 banks.
-template <int D>
-__device__ __forceinline__ int kv_chunk(int t, int c) {
-  constexpr int kC = D / 8;
-  const int f = D == 128 ? ((t & 3) << 2 | ((t >> 2) & 3)) : (((t >> 1) & 1) << 2 | ((t >> 2) & 3));
-  return t * kC + (c ^ f);
-}
+constexpr int kT = kAttnTile;        // tokens of a key/value tile
+constexpr int kRowsA = kAttnRows;    // rows of a workgroup: 32 a wavefront
 
 // Sequence and tile of work unit `unit` of tiles of kRowsA rows; false: none.
 __device__ __forceinline__ bool find_tile(const KvBatchArgs& b, int group, int unit, int& seq, int& tile) {
@@ -81,49 +54,83 @@ __device__ __forceinline__ bool find_tile(const KvBatchArgs& b, int group, int u
   return false;
 }
 
-template <int D, bool MX>
-__global__ __launch_bounds__(256, 2) void k_attn(AttnArgs a) {
+// The rows of one tile: the sequences' own parts (ALL false: a tile's rows are
+// of one sequence) or the shared prefix (ALL: rows of all sequences).
+template <int D, bool MX, bool ALL>
+__global__ __launch_bounds__(256, 2) void k_attn(AttnArgs a, int tiles, int chunk_tiles, int first_slot) {
   constexpr int kC = D / 8, kDT = D / 32;   // 16-byte chunks of a row, 32-wide tiles of D
   __shared__ uint4 sk[kT * kC], sv[kT * kC];
+  __shared__ int lds_p[8];
   const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
   // heads fastest: workgroups are dealt to the XCDs in turn, so each L2 sees few heads' keys and values.
   // Late tiles of a sequence, which see most tokens, first.
   const int head = (int)(blockIdx.x % (unsigned)a.c.heads);
-  const int unit = a.tiles - 1 - (int)(blockIdx.x / (unsigned)a.c.heads);
-  int seq, tile;
-  if (!find_tile(a.b, a.group, unit, seq, tile)) return;
-  const SeqRows sr = seq_rows(a.b, seq);
-  const int base = sr.len - sr.n;                       // position of the sequence's first row
-  const int rows = (int)((int64_t)sr.n * a.group - (int64_t)tile * kRowsA < kRowsA
-                             ? (int64_t)sr.n * a.group - (int64_t)tile * kRowsA : kRowsA);
-  // this lane's row (the last one again where the tile is not full)
+  const int uc = (int)(blockIdx.x / (unsigned)a.c.heads), chunk = uc / tiles, unit = tiles - 1 - uc % tiles;
   const int rr = wave * 32 + (lane & 31);
-  const int64_t r = (int64_t)tile * kRowsA + (rr < rows ? rr : rows - 1);
-  const int token = (int)(r / a.group), qh = head * a.group + (int)(r % a.group);
-  const int p = base + token;
-  const int p_lo = base + (int)((int64_t)tile * kRowsA / a.group);
-  const int p_hi = base + (int)(((int64_t)tile * kRowsA + rows - 1) / a.group);
+  int seq = 0, rows, row_g, qh, p, p_lo, p_hi, t0, t1;   // of this lane: row of the call, query head, position
+  if (ALL) {
+    const int64_t total = (int64_t)kv_clamp(a.b.offs[a.b.seqs], 0, a.b.rows) * a.group, r0 = (int64_t)unit * kRowsA;
+    if (r0 >= total) return;
+    rows = total - r0 < kRowsA ? (int)(total - r0) : kRowsA;
+    const int64_t r = r0 + (rr < rows ? rr : rows - 1);
+    row_g = (int)(r / a.group), qh = head * a.group + (int)(r % a.group);
+    const int last = (int)((r0 + rows - 1) / a.group);
+    // this lane's sequence: past those that end at or before its row, 64 offsets at a time
+    const int s0 = find_seq(a.b, (int)(r0 / a.group));
+    int s = s0;
+    for (int at = s0; at < a.b.seqs; at += 64) {
+      const int end = at + lane < a.b.seqs ? a.b.offs[at + lane + 1] : 0x7FFFFFFF;
+      for (int i = 0; i < 64; ++i) s += __builtin_amdgcn_readlane(end, i) <= row_g;
+      if (__builtin_amdgcn_readlane(end, 63) > last) break;
+    }
+    const SeqRows sr = seq_rows(a.b, s < a.b.seqs ? s : a.b.seqs - 1);
+    p = sr.len - sr.n + (row_g - sr.first);
+    int lo = p, hi = p;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int u = __shfl_xor(lo, d), w = __shfl_xor(hi, d);
+      lo = u < lo ? u : lo, hi = w > hi ? w : hi;
+    }
+    if (lane == 0) lds_p[wave] = lo, lds_p[4 + wave] = hi;
+    __syncthreads();
+    p_lo = lds_p[0], p_hi = lds_p[4];
+#pragma unroll
+    for (int i = 1; i < 4; ++i) {
+      p_lo = lds_p[i] < p_lo ? lds_p[i] : p_lo;
+      p_hi = lds_p[4 + i] > p_hi ? lds_p[4 + i] : p_hi;
+    }
+    t0 = 0, t1 = a.prefix_len;
+  } else {
+    int tile;
+    if (!find_tile(a.b, a.group, unit, seq, tile)) return;
+    const SeqRows sr = seq_rows(a.b, seq);
+    const int64_t r0 = (int64_t)tile * kRowsA, total = (int64_t)sr.n * a.group;
+    const int base = sr.len - sr.n;   // position of the sequence's first row
+    rows = total - r0 < kRowsA ? (int)(total - r0) : kRowsA;
+    const int64_t r = r0 + (rr < rows ? rr : rows - 1);
+    const int token = (int)(r / a.group);
+    row_g = sr.first + token, qh = head * a.group + (int)(r % a.group), p = base + token;
+    p_lo = base + (int)(r0 / a.group), p_hi = base + (int)((r0 + rows - 1) / a.group);
+    t0 = a.t0, t1 = sr.len;
+  }
 
   v8bf qf[D / 16];
   {
-    const uint16_t* qp = a.q + (int64_t)(sr.first + token) * a.ldq + (int64_t)qh * D + 8 * half;
+    const uint16_t* qp = a.q + (int64_t)row_g * a.ldq + (int64_t)qh * D + 8 * half;
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) qf[i] = *reinterpret_cast<const v8bf*>(qp + 16 * i);
   }
   v16f o[kDT] = {};
-  float m = -__FLT_MAX__, l = 0.0f;
+  float m = kNoMax, l = 0.0f;
 
-  for (int part = 0; part < 2; ++part) {
-    const int t0 = part ? a.prefix_len : 0, t1 = part ? sr.len : (a.prefix_len < sr.len ? a.prefix_len : sr.len);
-    const int32_t* table = part ? a.b.table + seq * a.b.ldt : a.prefix_table;
-    const KvSpan span = kv_span(t0, t1, p_lo, p_hi, a.window, a.sinks, kT);
-    for (int ti = 0; ti < span.n; ++ti) {
+  const KvSpan span = kv_span(t0, t1, p_lo, p_hi, a.window, a.sinks, kT);
+  const int first = chunk * chunk_tiles, end = span.n < first + chunk_tiles ? span.n : first + chunk_tiles;
+  for (int ti = first; ti < end; ++ti) {
       const int ts = kv_tile_start(span, t0, ti, kT);
       // lane i: cache row of token ts + i, -1 where no row of the tile sees it (it may hold anything)
       const int t = ts + lane;
       int at = -1;
-      if (t < span.hi && (t >= span.low || t < a.sinks))
-        at = kv_row(table[t >> a.c.page_shift], t, a.c.pages, a.c.heads, head, a.c.page_shift);
+      if (t < span.hi && (t >= span.low || t < a.sinks)) at = token_row(a, seq, t, head);
       const unsigned long long live = __ballot(at >= 0);
       __syncthreads();
 #pragma unroll
@@ -165,7 +172,7 @@ __global__ __launch_bounds__(256, 2) void k_attn(AttnArgs a) {
           top = fmaxf(top, s[mt][i]);
         }
       top = fmaxf(top, __shfl_xor(top, 32));
-      const float shift = top * a.scale, alpha = __builtin_amdgcn_exp2f(m * a.scale - shift);
+      const float shift = attn_shift(top, a.scale), alpha = __builtin_amdgcn_exp2f((m - top) * a.scale);
       m = top;
       float sum = 0.0f;
       v8bf pf[4];
@@ -184,51 +191,77 @@ __global__ __launch_bounds__(256, 2) void k_attn(AttnArgs a) {
       for (int st = 0; st < 4; ++st)
 #pragma unroll
         for (int d = 0; d < kDT; ++d) {
-          v4s x[2];
-#pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            // a group of 16 lanes reads 4 tokens x 16 values; lane i gets value i of the 4 tokens
-            const int tok = 16 * st + 8 * u + 4 * half + ((lane & 15) >> 2);
-            const int ch = 4 * d + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-            const char* at_lds = reinterpret_cast<const char*>(&sv[kv_chunk<D>(tok, ch)]) + 8 * (lane & 1);
-            x[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(at_lds));
-          }
-          const v8bf vf = __builtin_bit_cast(v8bf, __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7));
+          const int tok = 16 * st + 4 * half + ((lane & 15) >> 2);
+          const int ch = 4 * d + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+          const char* at_lds = reinterpret_cast<const char*>(sv) + 8 * (lane & 1);
+          const v8bf vf = join_bf(lds_read_tr(at_lds + 16 * kv_chunk<D>(tok, ch)),
+                                  lds_read_tr(at_lds + 16 * kv_chunk<D>(tok + 8, ch)));
           o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[st], o[d], 0, 0, 0);
         }
-    }
   }
   l += __shfl_xor(l, 32);
   if (rr >= rows) return;
+  if (a.slots) {
+    const int64_t at = ((int64_t)(first_slot + chunk) * a.b.rows + row_g) * a.q_heads + qh;
+    if (half == 0) a.ml[at] = make_float2(m, l);
+    if (!(l > 0.0f)) return;
+#pragma unroll
+    for (int d = 0; d < kDT; ++d)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<float4*>(a.po + at * D + 32 * d + 8 * i + 4 * half) =
+            make_float4(o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]);
+    return;
+  }
   const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-  uint16_t* op = a.o + (int64_t)(sr.first + token) * a.ldo + (int64_t)qh * D;
+  uint16_t* op = a.o + (int64_t)row_g * a.ldo + (int64_t)qh * D;
 #pragma unroll
   for (int d = 0; d < kDT; ++d)
 #pragma unroll
     for (int i = 0; i < 4; ++i)
       *reinterpret_cast<uint2*>(op + 32 * d + 8 * i + 4 * half) =
           make_uint2(bf16x2(o[d][4 * i] * inv, o[d][4 * i + 1] * inv), bf16x2(o[d][4 * i + 2] * inv, o[d][4 * i + 3] * inv));
-  if (a.lse && half == 0)
-    a.lse[(int64_t)(sr.first + token) * a.q_heads + qh] =
-        l > 0.0f ? (m * a.scale + __log2f(l)) * 0.69314718055994531f : -__builtin_inff();
+  if (a.lse && half == 0) a.lse[(int64_t)row_g * a.q_heads + qh] = attn_lse(m, l, a.scale);
 }
 
-hipError_t launch_attention(const uint16_t* q, int64_t ldq, uint16_t* o, int64_t ldo, float* lse,
-                            const KvBatchArgs& b, const KvCacheArgs& c, int max_rows, const int32_t* prefix_table,
-                            int prefix_len, int q_heads, int D, bool mx, int window, int sinks, float scale,
-                            hipStream_t st) {
-  const int group = q_heads / c.heads;
-  // no sequence has more than max_rows rows, and all together have no more than b.rows
-  const int64_t most = (int64_t)b.seqs * (((int64_t)max_rows * group + kRowsA - 1) / kRowsA);
-  const int64_t packed = (int64_t)b.rows * group / kRowsA + b.seqs;
-  const AttnArgs a{q, ldq, o, ldo, lse, b, c, prefix_table, prefix_len, group, q_heads, window, sinks,
-                   (int)(most < packed ? most : packed), (float)((double)scale * 1.4426950408889634)};
-  const dim3 g((unsigned)a.tiles * (unsigned)c.heads), t(256);
+template <int D, bool MX>
+static void rows(bool all, dim3 g, const AttnArgs& a, int tiles, int chunk_tiles, int first_slot, hipStream_t st) {
+  if (all) k_attn<D, MX, true><<<g, 256, 0, st>>>(a, tiles, chunk_tiles, first_slot);
+  else k_attn<D, MX, false><<<g, 256, 0, st>>>(a, tiles, chunk_tiles, first_slot);
+}
+
+static hipError_t launch_attn_rows(const AttnArgs& a, int D, bool mx, bool all, const AttnSplit& s, int first_slot,
+                                   hipStream_t st) {
+  const dim3 g((unsigned)s.tiles * (unsigned)a.c.heads * (unsigned)s.chunks);
   if (D == 128)
-    mx ? k_attn<128, true><<<g, t, 0, st>>>(a) : k_attn<128, false><<<g, t, 0, st>>>(a);
+    mx ? rows<128, true>(all, g, a, s.tiles, s.chunk_tiles, first_slot, st)
+       : rows<128, false>(all, g, a, s.tiles, s.chunk_tiles, first_slot, st);
   else
-    mx ? k_attn<64, true><<<g, t, 0, st>>>(a) : k_attn<64, false><<<g, t, 0, st>>>(a);
+    mx ? rows<64, true>(all, g, a, s.tiles, s.chunk_tiles, first_slot, st)
+       : rows<64, false>(all, g, a, s.tiles, s.chunk_tiles, first_slot, st);
   return hipGetLastError();
+}
+
+hipError_t launch_attn_few(const AttnArgs& a, int D, bool mx, int nq, int chunks, int chunk_tiles, int first_slot,
+                           hipStream_t st);
+hipError_t launch_attn_merge(const AttnArgs& a, int D, hipStream_t st);
+
+hipError_t launch_attention(const uint16_t* q, int64_t ldq, uint16_t* o, int64_t ldo, float* lse,
+                            const KvBatchArgs& b, const KvCacheArgs& c, const AttnPlan& plan,
+                            const int32_t* prefix_table, int prefix_len, int q_heads, int D, bool mx, int window,
+                            int sinks, float scale, void* ws, hipStream_t st) {
+  const int64_t items = (int64_t)b.rows * q_heads;
+  AttnArgs a{q, ldq, o, ldo, lse, b, c, prefix_table, prefix_len, plan.shared ? prefix_len : 0, q_heads / c.heads,
+             q_heads, window, sinks, (float)((double)scale * 1.4426950408889634),
+             static_cast<float2*>(ws), nullptr, plan.slots};
+  if (plan.slots) a.po = reinterpret_cast<float*>(static_cast<char*>(ws) + attn_ml_bytes(items, plan.slots));
+  hipError_t e = hipSuccess;
+  if (plan.shared) e = launch_attn_rows(a, D, mx, true, plan.prefix, plan.own.chunks, st);
+  if (e != hipSuccess) return e;
+  e = plan.few ? launch_attn_few(a, D, mx, plan.few, plan.own.chunks, plan.own.chunk_tiles, 0, st)
+               : launch_attn_rows(a, D, mx, false, plan.own, 0, st);
+  if (e != hipSuccess || plan.slots == 0) return e;
+  return launch_attn_merge(a, D, st);
 }
 
 }  // namespace sharq

@@ -1,0 +1,74 @@
+// What the attention kernels share: their arguments, the layout of a tile of
+// keys or values in LDS, and where a workgroup's results go.
+#pragma once
+
+#include "sharq_kv_device.hpp"
+
+namespace sharq {
+
+typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
+typedef short v4s __attribute__((ext_vector_type(4)));
+
+struct AttnArgs {
+  const uint16_t* q;
+  int64_t ldq;
+  uint16_t* o;
+  int64_t ldo;
+  float* lse;
+  KvBatchArgs b;
+  KvCacheArgs c;
+  const int32_t* prefix_table;
+  int prefix_len;
+  int t0;            // a sequence's own part begins at this token: prefix_len, or 0 (the whole sequence)
+  int group, q_heads, window, sinks;
+  float scale;       // of the scores, times log2 e
+  // partial results, where the tokens of a row are split over workgroups: slot
+  // s of row r and head h holds the running maximum (of the unscaled scores)
+  // and the sum of the softmax, ml[(s * rows + r) * q_heads + h], and the unnormalised
+  // output po[same][D], all fp32.  slots 0: results go to o.
+  float2* ml;
+  float* po;
+  int slots;
+};
+
+// Position of 16-byte chunk c of token t's row in an LDS tile of D bf16 a row.
+// The keys are read 16 tokens at a time at one chunk, the values 4 tokens at 64
+// consecutive bytes or 8 at 32: under this exchange of chunks all of them fall
+// on all 64 banks.
+template <int D>
+__device__ __forceinline__ int kv_chunk(int t, int c) {
+  constexpr int kC = D / 8;
+  const int f = D == 128 ? ((t & 3) << 2 | ((t >> 2) & 1) << 1 | ((t >> 3) & 1))
+                         : (((t >> 1) & 1) << 2 | ((t >> 2) & 1) << 1 | ((t >> 3) & 1));
+  return t * kC + (c ^ f);
+}
+
+// Transposing LDS read: a group of 16 lanes reads 4 rows of 16 values, lane i
+// giving the address of values 4 (i % 4) .. + 3 of row i / 4, and gets value i
+// of the 4 rows.
+__device__ __forceinline__ v4s lds_read_tr(const void* p) {
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)p);
+}
+
+__device__ __forceinline__ v8bf join_bf(v4s a, v4s b) {
+  return __builtin_bit_cast(v8bf, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// A row that saw nothing has sum 0 and the running maximum's start, a finite
+// number, so that no difference of maxima is a NaN.
+constexpr float kNoMax = -__FLT_MAX__;
+
+// What scores, times scale, are taken less of before the exponential.
+__device__ __forceinline__ float attn_shift(float top, float scale) { return top == kNoMax ? 0.0f : top * scale; }
+
+// Cache row of token t of a sequence, -1 when its page is absent.
+__device__ __forceinline__ int token_row(const AttnArgs& a, int seq, int t, int head) {
+  const int32_t* table = t < a.prefix_len ? a.prefix_table : a.b.table + seq * a.b.ldt;
+  return kv_row(table[t >> a.c.page_shift], t, a.c.pages, a.c.heads, head, a.c.page_shift);
+}
+
+__device__ __forceinline__ float attn_lse(float m, float l, float scale) {
+  return l > 0.0f ? (m * scale + __log2f(l)) * 0.69314718055994531f : -__builtin_inff();
+}
+
+}  // namespace sharq

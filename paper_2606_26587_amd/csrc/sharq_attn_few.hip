@@ -1,0 +1,329 @@
+// Attention over the paged cache where a sequence has few rows: single tokens
+// and a few drafted ones.  What is read is nearly all keys and values, once, so
+// the kernel is built to stream them from HBM.
+//
+// A workgroup takes the rows of one sequence that share a key/value head (its
+// new tokens times the G query heads of that head, up to 16 NQ) and a range of
+// its cached tokens; its four wavefronts take 32 NT tokens in turn and keep
+// softmax states of their own, which are joined through LDS at the end.  Long
+// sequences are split over several workgroups, whose partial results
+// k_attn_merge joins.
+//
+// S^T = K Q^T and O^T = V^T P^T with 16x16x32 bf16 MFMAs: a lane holds four
+// tokens of one row, so the rescaling needs no broadcast, and the accumulators
+// of two 16-token products, rounded to bf16, are the P operand of one product
+// over 32 tokens, if lane group g's eight k slots are taken as the tokens
+// {4g..4g+3, 16+4g..16+4g+3}.  Keys go from HBM straight into their operand's
+// registers (every byte is used by one lane alone); values through a wavefront's
+// own LDS for the transposing read.  An MXFP4 key's operand takes the k slots in
+// the order that gives each lane D/4 consecutive values of its token: one load,
+// one block scale.
+
+#include "sharq_attn.hpp"
+
+namespace sharq {
+
+constexpr int kSub = 32;   // tokens of one pass through the two products
+
+// The wavefronts' LDS writes before, its reads after (other lanes' data, one wavefront).
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+template <int D, bool MX, int NQ, int NT>
+__global__ __launch_bounds__(256) void k_attn_few(AttnArgs a, int chunk_tiles, int first_slot) {
+  constexpr int kC = D / 8, kJ = D / 32, kDT = D / 16;
+  constexpr int kTok = kSub * NT;            // tokens of a wavefront's turn
+  constexpr int kKL = MX ? D / 64 : 0;       // dwordx2 loads of a lane's codes of a key
+  __shared__ uint4 lds[4][kSub * kC];
+  __shared__ float2 lds_ml[4][16];
+  const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, col = lane & 15;
+  const int head = (int)(blockIdx.x % (unsigned)a.c.heads);
+  const int sc = (int)(blockIdx.x / (unsigned)a.c.heads), seq = sc % a.b.seqs, chunk = sc / a.b.seqs;
+  const SeqRows sr = seq_rows(a.b, seq);
+  if (sr.n == 0) return;
+  const int base = sr.len - sr.n, rows = sr.n * a.group < 16 * NQ ? sr.n * a.group : 16 * NQ;
+  const int p_hi = sr.len - 1;
+  const KvSpan span = kv_span(a.t0, sr.len, base, p_hi, a.window, a.sinks, kTok);
+  const int first = chunk * chunk_tiles, last = span.n < first + chunk_tiles ? span.n : first + chunk_tiles;
+
+  // rows of this lane: row 16 n + col of the tile (the last one again past it)
+  int grow[NQ], qh[NQ], p[NQ];
+  v8bf qf[NQ][kJ];
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) {
+    const int r = 16 * n + col < rows ? 16 * n + col : rows - 1;
+    grow[n] = sr.first + r / a.group, qh[n] = head * a.group + r % a.group, p[n] = base + r / a.group;
+    const uint16_t* qp = a.q + (int64_t)grow[n] * a.ldq + (int64_t)qh[n] * D;
+#pragma unroll
+    for (int j = 0; j < kJ; ++j) qf[n][j] = *reinterpret_cast<const v8bf*>(qp + (MX ? g * (D / 4) + 8 * j : 32 * j + 8 * g));
+  }
+  v4f o[NQ][kDT] = {};
+  float m[NQ], l[NQ];
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) m[n] = kNoMax, l[n] = 0.0f;
+
+  // cache row of token (lane % kTok) of a turn, -1 where no row sees it (it may hold anything)
+  auto locate = [&](int ti) {
+    const int t = kv_tile_start(span, a.t0, ti, kTok) + lane % kTok;
+    return ti < last && t < span.hi && (t >= span.low || t < a.sinks) ? token_row(a, seq, t, head) : -1;
+  };
+  uint4* const v_lds = lds[wave];
+  int next = locate(first + wave);
+  for (int ti = first + wave; ti < last; ti += 4) {
+    const int at = next, ts = kv_tile_start(span, a.t0, ti, kTok);
+    const unsigned long long live = __ballot(at >= 0);
+    // whether every row sees every token of the turn
+    const bool whole = live == ~0ull && ts + kTok - 1 <= base &&
+                       (p_hi - ts < a.window || ts + kTok <= a.sinks);
+    uint4 kb[NT][2][MX ? 1 : kJ], vb[NT][MX ? D / 64 : kC / 2];
+    uint32_t ke[NT][2], ve[NT][D / 64];
+#pragma unroll
+    for (int u = 0; u < NT; ++u) {
+#pragma unroll
+      for (int mt = 0; mt < 2; ++mt) {
+        const int64_t row = __shfl(at, u * kSub + mt * 16 + col);
+        if (MX) {
+          kb[u][mt][0] = make_uint4(0, 0, 0, 0);
+          ke[u][mt] = 0;
+          if (row >= 0) {
+            const uint8_t* s = a.c.k + row * (D / 2) + g * (D / 8);
+            if (kKL == 2) kb[u][mt][0] = *reinterpret_cast<const uint4*>(s);
+            else reinterpret_cast<uint2&>(kb[u][mt][0]) = *reinterpret_cast<const uint2*>(s);
+            ke[u][mt] = a.c.ks[row * (D / 32) + g * (D / 32) / 4];
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < kJ; ++j) {
+            kb[u][mt][j] = make_uint4(0, 0, 0, 0);
+            if (row >= 0) kb[u][mt][j] = *reinterpret_cast<const uint4*>(a.c.k + row * (D * 2) + 64 * j + 16 * g);
+          }
+        }
+      }
+      if (MX) {
+        constexpr int kPer = D / 32;   // lanes of a row
+#pragma unroll
+        for (int i = 0; i < D / 64; ++i) {
+          const int64_t row = __shfl(at, u * kSub + i * (64 / kPer) + lane / kPer);
+          vb[u][i] = make_uint4(0, 0, 0, 0);
+          ve[u][i] = 0;
+          if (row >= 0) {
+            vb[u][i] = *reinterpret_cast<const uint4*>(a.c.v + row * (D / 2) + 16 * (lane % kPer));
+            ve[u][i] = a.c.vs[row * (D / 32) + lane % kPer];
+          }
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < kC / 2; ++i) {
+          const int64_t row = __shfl(at, u * kSub + i * (64 / kC) + lane / kC);
+          vb[u][i] = make_uint4(0, 0, 0, 0);
+          if (row >= 0) vb[u][i] = *reinterpret_cast<const uint4*>(a.c.v + row * (D * 2) + 16 * (lane % kC));
+        }
+      }
+    }
+    next = locate(ti + 4);
+#pragma unroll
+    for (int u = 0; u < NT; ++u) {
+      v4f s[NQ][2] = {};
+#pragma unroll
+      for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+        for (int j = 0; j < kJ; ++j) {
+          uint4 kx;
+          if (MX) {
+            const uint32_t w[4] = {kb[u][mt][0].x, kb[u][mt][0].y, kb[u][mt][0].z, kb[u][mt][0].w};
+            kx = mx_bf16x8(w[j], ke[u][mt]);
+          } else {
+            kx = kb[u][mt][j];
+          }
+#pragma unroll
+          for (int n = 0; n < NQ; ++n)
+            s[n][mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, kx), qf[n][j], s[n][mt], 0, 0, 0);
+        }
+      wave_sync();   // the reads of the turn before are done
+      if (MX) {
+        constexpr int kPer = D / 32;
+#pragma unroll
+        for (int i = 0; i < D / 64; ++i) {
+          const int t = i * (64 / kPer) + lane / kPer, c0 = 4 * (lane % kPer);
+          const uint32_t w[4] = {vb[u][i].x, vb[u][i].y, vb[u][i].z, vb[u][i].w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v_lds[kv_chunk<D>(t, c0 + e)] = mx_bf16x8(w[e], ve[u][i]);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < kC / 2; ++i) v_lds[kv_chunk<D>(i * (64 / kC) + lane / kC, lane % kC)] = vb[u][i];
+      }
+      wave_sync();
+      v8bf pf[NQ];
+      float alpha[NQ];
+      bool moved = false;
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) {
+        if (!whole) {
+#pragma unroll
+          for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int j = u * kSub + mt * 16 + 4 * g + i, t = ts + j;
+              const bool seen = ((live >> j) & 1) && t <= p[n] && (p[n] - t < a.window || t < a.sinks);
+              s[n][mt][i] = seen ? s[n][mt][i] : -__builtin_inff();
+            }
+        }
+        float top = fmaxf(fmaxf(fmaxf(s[n][0][0], s[n][0][1]), fmaxf(s[n][0][2], s[n][0][3])),
+                          fmaxf(fmaxf(s[n][1][0], s[n][1][1]), fmaxf(s[n][1][2], s[n][1][3])));
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(fmaxf(top, __shfl_xor(top, 32)), m[n]);
+        moved |= top > m[n];
+        alpha[n] = __builtin_amdgcn_exp2f((m[n] - top) * a.scale);
+        m[n] = top;
+        const float shift = attn_shift(top, a.scale);
+        float sum = 0.0f, e[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][i >> 2][i & 3], a.scale, -shift));
+          sum += e[i];
+        }
+        pf[n] = __builtin_bit_cast(v8bf, make_uint4(bf16x2(e[0], e[1]), bf16x2(e[2], e[3]), bf16x2(e[4], e[5]),
+                                                    bf16x2(e[6], e[7])));
+        l[n] = l[n] * alpha[n] + sum;
+      }
+      if (__any(moved)) {
+#pragma unroll
+        for (int n = 0; n < NQ; ++n)
+#pragma unroll
+          for (int d = 0; d < kDT; ++d) o[n][d] *= alpha[n];
+      }
+#pragma unroll
+      for (int d = 0; d < kDT; ++d) {
+        const int t = 4 * g + (col >> 2), ch = 2 * d + ((lane & 3) >> 1);
+        const char* base_lds = reinterpret_cast<const char*>(v_lds) + 8 * (lane & 1);
+        const v8bf vf = join_bf(lds_read_tr(base_lds + 16 * kv_chunk<D>(t, ch)),
+                                lds_read_tr(base_lds + 16 * kv_chunk<D>(t + 16, ch)));
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) o[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[n], o[n][d], 0, 0, 0);
+      }
+    }
+  }
+
+  // the four wavefronts' states joined, 16 rows at a time; D fp32 values of a row take D / 4 chunks of 16 bytes
+  float4* const o_lds = reinterpret_cast<float4*>(lds[0]);   // [4][16][D / 4], as large as the values' tiles
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) {
+    l[n] += __shfl_xor(l[n], 16);
+    l[n] += __shfl_xor(l[n], 32);
+    __syncthreads();
+    if (g == 0) lds_ml[wave][col] = make_float2(m[n], l[n]);
+#pragma unroll
+    for (int d = 0; d < kDT; ++d)   // exchanged by row, so that 16 rows at one chunk use all banks
+      o_lds[(wave * 16 + col) * (D / 4) + ((4 * d + g) ^ col)] = make_float4(o[n][d][0], o[n][d][1], o[n][d][2], o[n][d][3]);
+    __syncthreads();
+    for (int i = tid; i < 16 * (D / 4); i += 256) {
+      const int r = i / (D / 4), ch = i % (D / 4), row = 16 * n + r;
+      if (row >= rows) continue;
+      float2 s[4];
+      float top = kNoMax;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        s[w] = lds_ml[w][r];
+        top = fmaxf(top, s[w].x);
+      }
+      float sum = 0.0f, x0 = 0.0f, x1 = 0.0f, x2 = 0.0f, x3 = 0.0f;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const float f = __builtin_amdgcn_exp2f((s[w].x - top) * a.scale);
+        const float4 x = o_lds[(w * 16 + r) * (D / 4) + (ch ^ r)];
+        sum += f * s[w].y, x0 += f * x.x, x1 += f * x.y, x2 += f * x.z, x3 += f * x.w;
+      }
+      const int64_t row_g = sr.first + row / a.group;
+      const int h = head * a.group + row % a.group;
+      if (a.slots) {
+        const int64_t at = ((int64_t)(first_slot + chunk) * a.b.rows + row_g) * a.q_heads + h;
+        if (ch == 0) a.ml[at] = make_float2(top, sum);
+        if (sum > 0.0f) *reinterpret_cast<float4*>(a.po + at * D + 4 * ch) = make_float4(x0, x1, x2, x3);
+      } else {
+        const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+        *reinterpret_cast<uint2*>(a.o + row_g * a.ldo + (int64_t)h * D + 4 * ch) =
+            make_uint2(bf16x2(x0 * inv, x1 * inv), bf16x2(x2 * inv, x3 * inv));
+        if (a.lse && ch == 0) a.lse[row_g * a.q_heads + h] = attn_lse(top, sum, a.scale);
+      }
+    }
+  }
+}
+
+// Joins the partial results of a row and head: one workgroup, 256 / (D / 4)
+// groups of threads that take every slot in turn, so that a single long sequence
+// in 64 slots is read in a few trips.  Sums are formed in a fixed order: the same
+// call gives the same bits.
+template <int D>
+__global__ __launch_bounds__(256) void k_attn_merge(AttnArgs a) {
+  constexpr int kPer = D / 4, kG = 256 / kPer;
+  __shared__ float4 lds_o[kG][kPer];
+  __shared__ float2 lds_s[kG];
+  const int64_t all = (int64_t)a.b.rows * a.q_heads;
+  const int grp = (int)threadIdx.x / kPer, ch = (int)threadIdx.x % kPer;
+  const int64_t items = (int64_t)kv_clamp(a.b.offs[a.b.seqs], 0, a.b.rows) * a.q_heads;   // without padding rows
+  for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+    float top = kNoMax, sum = 0.0f;
+    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+    for (int s = grp; s < a.slots; s += kG) {
+      const float2 t = a.ml[s * all + item];
+      if (!(t.y > 0.0f)) continue;   // that slot saw nothing: its output was not written
+      const float4 x = *reinterpret_cast<const float4*>(a.po + (s * all + item) * D + 4 * ch);
+      const float now = fmaxf(top, t.x), f = __builtin_amdgcn_exp2f((top - now) * a.scale),
+                  e = __builtin_amdgcn_exp2f((t.x - now) * a.scale);
+      sum = f * sum + e * t.y;
+      o.x = f * o.x + e * x.x, o.y = f * o.y + e * x.y, o.z = f * o.z + e * x.z, o.w = f * o.w + e * x.w;
+      top = now;
+    }
+    __syncthreads();   // the item before is done with
+    lds_o[grp][ch] = o;
+    if (ch == 0) lds_s[grp] = make_float2(top, sum);
+    __syncthreads();
+    if (grp != 0) continue;
+    top = kNoMax, sum = 0.0f, o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+    for (int i = 0; i < kG; ++i) top = fmaxf(top, lds_s[i].x);
+#pragma unroll
+    for (int i = 0; i < kG; ++i) {
+      const float e = __builtin_amdgcn_exp2f((lds_s[i].x - top) * a.scale);
+      const float4 x = lds_o[i][ch];
+      sum += e * lds_s[i].y;
+      o.x += e * x.x, o.y += e * x.y, o.z += e * x.z, o.w += e * x.w;
+    }
+    const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+    const int64_t row = item / a.q_heads, h = item % a.q_heads;
+    *reinterpret_cast<uint2*>(a.o + row * a.ldo + h * D + 4 * ch) =
+        make_uint2(bf16x2(o.x * inv, o.y * inv), bf16x2(o.z * inv, o.w * inv));
+    if (a.lse && ch == 0) a.lse[item] = attn_lse(top, sum, a.scale);
+  }
+}
+
+template <int D, bool MX>
+static void few(int nq, dim3 g, const AttnArgs& a, int chunk_tiles, int first_slot, hipStream_t st) {
+  constexpr int NT = MX ? 2 : 1;
+  if (nq == 1) k_attn_few<D, MX, 1, NT><<<g, 256, 0, st>>>(a, chunk_tiles, first_slot);
+  else if (nq == 2) k_attn_few<D, MX, 2, NT><<<g, 256, 0, st>>>(a, chunk_tiles, first_slot);
+  else k_attn_few<D, MX, 4, NT><<<g, 256, 0, st>>>(a, chunk_tiles, first_slot);
+}
+
+hipError_t launch_attn_few(const AttnArgs& a, int D, bool mx, int nq, int chunks, int chunk_tiles, int first_slot,
+                           hipStream_t st) {
+  const dim3 g((unsigned)chunks * (unsigned)a.b.seqs * (unsigned)a.c.heads);
+  if (D == 128) mx ? few<128, true>(nq, g, a, chunk_tiles, first_slot, st) : few<128, false>(nq, g, a, chunk_tiles, first_slot, st);
+  else mx ? few<64, true>(nq, g, a, chunk_tiles, first_slot, st) : few<64, false>(nq, g, a, chunk_tiles, first_slot, st);
+  return hipGetLastError();
+}
+
+hipError_t launch_attn_merge(const AttnArgs& a, int D, hipStream_t st) {
+  const int64_t items = (int64_t)a.b.rows * a.q_heads, most = 1 << 20;
+  const dim3 g((unsigned)(items < most ? items : most));
+  if (D == 128) k_attn_merge<128><<<g, 256, 0, st>>>(a);
+  else k_attn_merge<64><<<g, 256, 0, st>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace sharq

@@ -60,4 +60,77 @@ constexpr int kv_tile_start(const KvSpan& s, int t0, int i, int T) {
   return t0 + T * (i < s.ns ? i : i - s.ns + s.jf);
 }
 
+// ---------------------------------------------------------------------------
+// Work split of the attention
+// ---------------------------------------------------------------------------
+
+constexpr int kAttnTile = 64;    // tokens of a key/value tile where rows are many
+constexpr int kAttnRows = 128;   // rows (token x query head of a key/value head) of a tile there
+
+constexpr int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// `chunks` workgroups share the tokens of each of `tiles` row tiles, `chunk_tiles`
+// key/value tiles each.
+struct AttnSplit {
+  int tiles, chunks, chunk_tiles;
+};
+
+struct AttnPlan {
+  int few;          // 16-row tiles of the few-row kernel (1, 2, 4); 0: the kernel for many rows
+  bool shared;      // the prefix is read for all sequences together
+  AttnSplit own, prefix;
+  int slots;        // partial results of a row; 0: none, results are final
+};
+
+// Splits kv_tiles of each of `units` workgroups so that about `want` workgroups
+// run, each over a multiple of `least` tiles.
+constexpr AttnSplit attn_split(int64_t tiles, int64_t units, int64_t kv_tiles, int64_t want, int least) {
+  int64_t chunks = units > 0 ? want / units : 1;
+  if (chunks > ceil_div(kv_tiles, least)) chunks = ceil_div(kv_tiles, least);
+  if (chunks < 1) chunks = 1;
+  int64_t each = ceil_div(ceil_div(kv_tiles, chunks), least) * least;
+  if (each < least) each = least;
+  chunks = kv_tiles > 0 ? ceil_div(kv_tiles, each) : 1;
+  return {(int)tiles, (int)chunks, (int)each};
+}
+
+constexpr AttnPlan attn_plan(int64_t seqs, int64_t rows, int64_t max_rows, int64_t max_len, int heads, int group,
+                             bool mx, int64_t window, int64_t sinks, int64_t prefix_len) {
+  AttnPlan p{};
+  if (max_rows > rows) max_rows = rows;
+  // a window leaves little of a prefix, and rows that see different parts of it
+  p.shared = prefix_len > 0 && window >= max_len;
+  const int64_t r = max_rows * group, own = max_len - (p.shared ? prefix_len : 0);
+  p.few = r <= 16 ? 1 : r <= 32 ? 2 : r <= 64 ? 4 : 0;
+  // tokens that a tile of rows sees at most: its window and its own positions, and the sinks
+  const int64_t span = p.few ? max_rows : kAttnRows / group + 2;
+  const int64_t w = window < max_len ? window + span : own, part = w < own ? w : own;
+  const int64_t s = window < max_len ? (sinks < own - part ? sinks : own - part) : 0;
+  if (p.few) {
+    const int tok = mx ? 64 : 32;
+    const int64_t kv = part > 0 ? ceil_div(part, tok) + (part < own ? 1 : 0) + ceil_div(s, tok) : 0;
+    p.own = attn_split(1, seqs * heads, kv, 1024, 4);
+  } else {
+    // no sequence has more than max_rows rows, and all together have no more than rows
+    const int64_t most = seqs * ceil_div(r, kAttnRows), packed = rows * group / kAttnRows + seqs;
+    const int64_t tiles = most < packed ? most : packed;
+    const int64_t kv = part > 0 ? ceil_div(part, kAttnTile) + (part < own ? 1 : 0) + ceil_div(s, kAttnTile) : 0;
+    p.own = attn_split(tiles, tiles * heads, kv, 512, 4);
+  }
+  p.slots = p.own.chunks > 1 ? p.own.chunks : 0;
+  if (p.shared) {
+    const int64_t tiles = ceil_div(rows * group, kAttnRows);
+    p.prefix = attn_split(tiles, tiles * heads, ceil_div(prefix_len, kAttnTile), 512, 4);
+    p.slots = p.own.chunks + p.prefix.chunks;
+  }
+  return p;
+}
+
+// Bytes of the softmax states of `items` rows and heads in `slots` slots (the
+// partial outputs lie behind them, 16-byte aligned).
+constexpr int64_t attn_ml_bytes(int64_t items, int slots) { return ceil_div(items * slots * 8, 16) * 16; }
+constexpr int64_t attn_workspace(int64_t items, int slots, int D) {
+  return slots ? attn_ml_bytes(items, slots) + items * slots * D * 4 : 0;
+}
+
 }  // namespace sharq

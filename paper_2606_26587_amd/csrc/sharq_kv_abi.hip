@@ -16,9 +16,9 @@ hipError_t launch_kv_append(const uint16_t* q, const uint16_t* k, const uint16_t
 hipError_t launch_kv_read(uint16_t* ko, int64_t ldk, uint16_t* vo, int64_t ldv, const KvBatchArgs& b,
                           const KvCacheArgs& c, int D, bool mx, hipStream_t st);
 hipError_t launch_attention(const uint16_t* q, int64_t ldq, uint16_t* o, int64_t ldo, float* lse,
-                            const KvBatchArgs& b, const KvCacheArgs& c, int max_rows, const int32_t* prefix_table,
-                            int prefix_len, int q_heads, int D, bool mx, int window, int sinks, float scale,
-                            hipStream_t st);
+                            const KvBatchArgs& b, const KvCacheArgs& c, const AttnPlan& plan,
+                            const int32_t* prefix_table, int prefix_len, int q_heads, int D, bool mx, int window,
+                            int sinks, float scale, void* ws, hipStream_t st);
 }  // namespace sharq
 
 namespace {
@@ -95,6 +95,14 @@ sharq_status check_attn(const sharq_attn* t, const sharq_kv_cache* c, const shar
   return SHARQ_OK;
 }
 
+int attn_window(const sharq_attn* t) { return t->window == 0 || t->window > INT_MAX ? INT_MAX : (int)t->window; }
+int attn_sinks(const sharq_attn* t) { return t->sinks > INT_MAX ? INT_MAX : (int)t->sinks; }
+
+sharq::AttnPlan plan_of(const sharq_kv_cache* c, const sharq_kv_batch* b, const sharq_attn* t, int64_t q_heads) {
+  return sharq::attn_plan(b->seqs, b->rows, b->max_rows, b->max_len, c->kv_heads, (int)(q_heads / c->kv_heads),
+                          c->fmt == SHARQ_KV_MXFP4, attn_window(t), attn_sinks(t), t->prefix_len);
+}
+
 }  // namespace
 
 extern "C" {
@@ -156,7 +164,9 @@ size_t sharq_attention_workspace_bytes(const sharq_kv_cache* cache, const sharq_
   if (check_sizes(cache) != SHARQ_OK || check_batch(batch, cache, false) != SHARQ_OK ||
       check_attn(attn, cache, batch, q_heads, false) != SHARQ_OK)
     return 0;
-  return 0;
+  if (batch->rows == 0 || batch->seqs == 0 || batch->max_rows == 0) return 0;
+  return (size_t)sharq::attn_workspace(batch->rows * q_heads, plan_of(cache, batch, attn, q_heads).slots,
+                                       cache->head_dim);
 }
 
 sharq_status sharq_attention(const void* Q, sharq_dtype xdt, int64_t q_heads, int64_t ldq,
@@ -174,15 +184,13 @@ sharq_status sharq_attention(const void* Q, sharq_dtype xdt, int64_t q_heads, in
   if (batch->rows == 0 || batch->seqs == 0 || batch->max_rows == 0) return SHARQ_OK;
   if (!Q || !O) return SHARQ_EINVAL;
   if (!row_aligned(Q, ldq) || !row_aligned(O, ldo) || !aligned(lse, 4) || !aligned(workspace, 16)) return SHARQ_EALIGN;
-  const size_t need = sharq_attention_workspace_bytes(cache, batch, attn, q_heads);
+  const sharq::AttnPlan plan = plan_of(cache, batch, attn, q_heads);
+  const size_t need = (size_t)sharq::attn_workspace(batch->rows * q_heads, plan.slots, (int)D);
   if (need > 0 && (!workspace || workspace_bytes < need)) return SHARQ_EINVAL;
-  const int window = attn->window == 0 || attn->window > INT_MAX ? INT_MAX : (int)attn->window;
-  const int sinks = attn->sinks > INT_MAX ? INT_MAX : (int)attn->sinks;
   return hip_status(sharq::launch_attention(
       static_cast<const uint16_t*>(Q), ldq, static_cast<uint16_t*>(O), ldo, lse, batch_args(batch), cache_args(cache),
-      (int)(batch->max_rows < batch->rows ? batch->max_rows : batch->rows), attn->prefix_table, (int)attn->prefix_len,
-      (int)q_heads, (int)D, cache->fmt == SHARQ_KV_MXFP4, window, sinks, attn->scale,
-      reinterpret_cast<hipStream_t>(stream)));
+      plan, attn->prefix_table, (int)attn->prefix_len, (int)q_heads, (int)D, cache->fmt == SHARQ_KV_MXFP4,
+      attn_window(attn), attn_sinks(attn), attn->scale, workspace, reinterpret_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -179,3 +179,20 @@ def test_absent_pages(fmt):
 def test_large_scores(per, lens, fmt):
     """Scores in the hundreds: one token takes all the weight."""
     run(per, lens, 16, 4, 1, 128, fmt, peak=6.0, scale=1.0)
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("per,lens,prefix", [([1], [9000], 0), ([1, 3, 2], [6000, 10, 3500], 0), ([9], [5000], 0),
+                                             ([30, 18], [3000, 700], 0), ([1] * 3, [5000, 4100, 4500], 4096),
+                                             ([25, 1], [2300, 2100], 2048)])
+def test_tokens_split_over_workgroups(per, lens, prefix, D, fmt):
+    run(per, lens, 64, 8, 2, D, fmt, prefix_len=prefix, pad=1, seed=len(per))
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("per", [1, 40])
+def test_large_scale_where_a_wavefront_sees_nothing(per, fmt):
+    """The running maximum's start times a scale above 1 is not a number that may enter a sum."""
+    run([per], [500], 16, 4, 1, 128, fmt, scale=3.0, bad_pages=[(0, j, -1) for j in range(24)], peak=0.3)
+    run([per, per], [per, 70], 16, 4, 1, 128, fmt, scale=3.0, window=20, prefix_len=32, peak=0.3)
