@@ -212,7 +212,11 @@ class QuantWeight:
 KV_FORMATS = {"bf16": 0, "mx": 1, "mxfp4": 1}
 
 
-@dataclass
+# The two descriptors below are used by every layer of a decode step: they are
+# checked and turned into their C structures once, and cannot be changed after
+# (the tensors' contents can).
+
+@dataclass(frozen=True)
 class KVCache:
     """A paged key/value cache (device buffers; sharq_kv_cache in include/sharq.h).
     fmt "bf16": k, v [pages, kv_heads, page_size, head_dim]; "mx": k, v uint8
@@ -237,16 +241,16 @@ class KVCache:
         given = [t for t in (self.k, self.v, self.k_scale, self.v_scale) if t is not None]
         if not ok or any(not t.is_contiguous() or t.device != self.k.device for t in given):
             raise SharqError(EINVAL, "KVCache")
-        self.pages, self.kv_heads, self.page_size = shape[:3]
-        self.head_dim = shape[3] * 2 if mx else shape[3]
+        pages, kv_heads, page_size = shape[:3]
+        head_dim = shape[3] * 2 if mx else shape[3]
+        struct = KVCacheStruct(pages, page_size, kv_heads, head_dim, KV_FORMATS[self.fmt], self.k.data_ptr(),
+                               self.v.data_ptr(), _ptr(self.k_scale), _ptr(self.v_scale),
+                               SCALE_RULES[self.scale_rule])
+        self.__dict__.update(pages=pages, kv_heads=kv_heads, page_size=page_size, head_dim=head_dim,
+                             width=kv_heads * head_dim, device_index=self.k.get_device(), ref=ctypes.byref(struct))
 
-    def struct(self) -> KVCacheStruct:
-        return KVCacheStruct(self.pages, self.page_size, self.kv_heads, self.head_dim, KV_FORMATS[self.fmt],
-                             self.k.data_ptr(), self.v.data_ptr(), _ptr(self.k_scale), _ptr(self.v_scale),
-                             SCALE_RULES[self.scale_rule])
 
-
-@dataclass
+@dataclass(frozen=True)
 class KVBatch:
     """The sequences of a call (sharq_kv_batch): row_offsets int32 [seqs + 1], lens
     int32 [seqs] (the call's rows among them), page_table int32 [seqs, n], on the
@@ -269,11 +273,11 @@ class KVBatch:
                 (seqs <= 1 or self.page_table.stride(0) >= self.page_table.shape[1])):
             raise SharqError(EINVAL, "KVBatch")
 
-    def struct(self) -> KVBatchStruct:
-        # one sequence's stride may be anything: its single row is as long as the table is wide
-        ld = self.page_table.stride(0) if self.lens.numel() > 1 else self.page_table.shape[1]
-        return KVBatchStruct(self.lens.numel(), self.rows, self.max_rows, self.max_len, ld,
-                             self.row_offsets.data_ptr(), self.lens.data_ptr(), self.page_table.data_ptr())
+        # the stride of a single sequence means nothing: its row is as long as the table is wide
+        ld = self.page_table.stride(0) if seqs > 1 else self.page_table.shape[1]
+        struct = KVBatchStruct(seqs, self.rows, self.max_rows, self.max_len, ld, self.row_offsets.data_ptr(),
+                               self.lens.data_ptr(), self.page_table.data_ptr())
+        self.__dict__.update(device_index=self.lens.get_device(), ref=ctypes.byref(struct))
 
 
 def alloc_kv_cache(pages: int, page_size: int, kv_heads: int, head_dim: int, fmt: str = "bf16", device="cuda",
@@ -444,23 +448,23 @@ def sharq_linear_grouped(a: PreparedAct, row_index: Optional[torch.Tensor], expe
     return out
 
 
-def _rows(t: Optional[torch.Tensor], batch: KVBatch, cache: KVCache, where: str, width: int = 0):
-    """A row tensor [batch.rows, heads * head_dim] (bf16, any row stride, on the cache's device, which must be the
-    current one) -> its heads."""
-    if (t.dim() != 2 or t.shape[0] != batch.rows or t.dtype != torch.bfloat16 or (t.shape[1] > 1 and t.stride(1) != 1)
-            or t.shape[1] % cache.head_dim or (width and t.shape[1] != width) or t.device != cache.k.device):
+_BF = torch.bfloat16
+
+
+def _rows(t: torch.Tensor, rows: int, width: int, dev: int, where: str) -> int:
+    """Row stride of a row tensor [rows, width], bf16 on device `dev`, its rows contiguous."""
+    if t.dtype is not _BF or t.shape != (rows, width) or t.get_device() != dev:
         raise SharqError(EINVAL, where)
-    return t.shape[1] // cache.head_dim
-
-
-def _ld(t: torch.Tensor) -> int:
-    """Row stride in elements; that of a single row means nothing."""
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    ld, inner = t.stride()
+    if inner != 1 and width > 1:
+        raise SharqError(EINVAL, where)
+    return ld if rows > 1 else width   # the stride of a single row means nothing
 
 
 def _here(cache: KVCache, batch: KVBatch, where: str):
     """The kernels are launched on the current device: the buffers must be its own."""
-    if not cache.k.is_cuda or cache.k.device != batch.lens.device or cache.k.get_device() != torch.cuda.current_device():
+    dev = cache.device_index
+    if dev < 0 or dev != batch.device_index or dev != torch.cuda.current_device():
         raise SharqError(EINVAL, where)
 
 
@@ -473,32 +477,32 @@ def sharq_kv_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor,
     Returns the rotated queries (q_out; `q` itself for an in-place update), None without q."""
     where = "sharq_kv_append"
     _here(cache, batch, where)
-    wk = cache.kv_heads * cache.head_dim
-    _rows(k, batch, cache, where, wk)
-    _rows(v, batch, cache, where, wk)
-    heads = 0
+    rows, dev = batch.rows, cache.device_index
+    ldk, ldv = _rows(k, rows, cache.width, dev, where), _rows(v, rows, cache.width, dev, where)
+    heads = ldq = ldo = angles = 0
     if q is not None:
-        heads = _rows(q, batch, cache, where)
+        width = q.shape[-1]
+        heads, rest = divmod(width, cache.head_dim)
+        ldq = _rows(q, rows, width, dev, where)
+        if rest:
+            raise SharqError(EINVAL, where)
         if q_out is None:
-            q_out = torch.empty((batch.rows, q.shape[1]), dtype=q.dtype, device=q.device)
-        _rows(q_out, batch, cache, where, q.shape[1])
-    angles = 0
+            q_out = torch.empty((rows, width), dtype=q.dtype, device=q.device)
+        ldo = _rows(q_out, rows, width, dev, where)
     if (cos is None) != (sin is None):
         raise SharqError(EINVAL, where)
     if cos is not None:
         angles = cos.shape[0]
         for t in (cos, sin):
-            if (t.dtype != torch.float32 or tuple(t.shape) != (angles, cache.head_dim // 2) or not t.is_contiguous()
-                    or t.device != cache.k.device):
+            if (t.dtype is not torch.float32 or t.shape != (angles, cache.head_dim // 2) or not t.is_contiguous()
+                    or t.get_device() != dev):
                 raise SharqError(EINVAL, where)
-    if positions is not None and (positions.dtype != torch.int32 or tuple(positions.shape) != (batch.rows,)
-                                  or not positions.is_contiguous() or positions.device != cache.k.device):
+    if positions is not None and (positions.dtype is not torch.int32 or positions.shape != (rows,)
+                                  or not positions.is_contiguous() or positions.get_device() != dev):
         raise SharqError(EINVAL, where)
-    cs, bs = cache.struct(), batch.struct()
-    _check(lib.sharq_kv_append(_ptr(q), k.data_ptr(), v.data_ptr(), BF16, heads, 0 if q is None else _ld(q), _ld(k),
-                               _ld(v), _ptr(cos), _ptr(sin), angles, _ptr(positions), ctypes.byref(cs),
-                               ctypes.byref(bs), None if q is None else q_out.data_ptr(),
-                               0 if q is None else _ld(q_out), _stream(stream)), where)
+    _check(lib.sharq_kv_append(_ptr(q), k.data_ptr(), v.data_ptr(), BF16, heads, ldq, ldk, ldv, _ptr(cos), _ptr(sin),
+                               angles, _ptr(positions), cache.ref, batch.ref, None if q is None else q_out.data_ptr(),
+                               ldo, _stream(stream)), where)
     return None if q is None else q_out
 
 
@@ -507,24 +511,22 @@ def sharq_kv_read(cache: KVCache, batch: KVBatch, k_out: Optional[torch.Tensor] 
     """The rows' cached keys and values as bf16 [rows, kv_heads * head_dim] (padding rows are left as they are)."""
     where = "sharq_kv_read"
     _here(cache, batch, where)
-    wk = cache.kv_heads * cache.head_dim
+    shape = (batch.rows, cache.width)
     if k_out is None:
-        k_out = torch.empty((batch.rows, wk), dtype=torch.bfloat16, device=cache.k.device)
+        k_out = torch.empty(shape, dtype=_BF, device=cache.k.device)
     if v_out is None:
-        v_out = torch.empty((batch.rows, wk), dtype=torch.bfloat16, device=cache.k.device)
-    _rows(k_out, batch, cache, where, wk)
-    _rows(v_out, batch, cache, where, wk)
-    cs, bs = cache.struct(), batch.struct()
-    _check(lib.sharq_kv_read(ctypes.byref(cs), ctypes.byref(bs), k_out.data_ptr(), _ld(k_out), v_out.data_ptr(),
-                             _ld(v_out), BF16, _stream(stream)), where)
+        v_out = torch.empty(shape, dtype=_BF, device=cache.k.device)
+    ldk, ldv = (_rows(t, *shape, cache.device_index, where) for t in (k_out, v_out))
+    _check(lib.sharq_kv_read(cache.ref, batch.ref, k_out.data_ptr(), ldk, v_out.data_ptr(), ldv, BF16,
+                             _stream(stream)), where)
     return k_out, v_out
 
 
 def attention_workspace_bytes(cache: KVCache, batch: KVBatch, q_heads: int, window: int = 0, sinks: int = 0,
                               prefix_len: int = 0) -> int:
     """Bytes of workspace of sharq_attention for these sizes."""
-    cs, bs, ts = cache.struct(), batch.struct(), AttnStruct(1.0, window, sinks, None, prefix_len)
-    return lib.sharq_attention_workspace_bytes(ctypes.byref(cs), ctypes.byref(bs), ctypes.byref(ts), q_heads)
+    ts = AttnStruct(1.0, window, sinks, None, prefix_len)
+    return lib.sharq_attention_workspace_bytes(cache.ref, batch.ref, ctypes.byref(ts), q_heads)
 
 
 def sharq_attention(q: torch.Tensor, cache: KVCache, batch: KVBatch, scale: Optional[float] = None, window: int = 0,
@@ -537,30 +539,34 @@ def sharq_attention(q: torch.Tensor, cache: KVCache, batch: KVBatch, scale: Opti
     when given.  workspace: a buffer of attention_workspace_bytes, allocated here when needed and None."""
     where = "sharq_attention"
     _here(cache, batch, where)
-    heads = _rows(q, batch, cache, where)
+    rows, dev, width = batch.rows, cache.device_index, q.shape[-1]
+    heads, rest = divmod(width, cache.head_dim)
+    ldq = _rows(q, rows, width, dev, where)
+    if rest:
+        raise SharqError(EINVAL, where)
     if out is None:
-        out = torch.empty((batch.rows, q.shape[1]), dtype=q.dtype, device=q.device)
-    _rows(out, batch, cache, where, q.shape[1])
-    if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (batch.rows, heads)
-                            or not lse.is_contiguous() or lse.device != q.device):
+        out = torch.empty((rows, width), dtype=q.dtype, device=q.device)
+    ldo = _rows(out, rows, width, dev, where)
+    if lse is not None and (lse.dtype is not torch.float32 or lse.shape != (rows, heads) or not lse.is_contiguous()
+                            or lse.get_device() != dev):
         raise SharqError(EINVAL, where)
-    if prefix_table is not None and (prefix_table.dtype != torch.int32 or not prefix_table.is_contiguous()
+    if prefix_table is not None and (prefix_table.dtype is not torch.int32 or not prefix_table.is_contiguous()
                                      or prefix_table.numel() * cache.page_size < prefix_len
-                                     or prefix_table.device != q.device):
+                                     or prefix_table.get_device() != dev):
         raise SharqError(EINVAL, where)
-    cs, bs = cache.struct(), batch.struct()
     ts = AttnStruct(cache.head_dim ** -0.5 if scale is None else scale, window, sinks, _ptr(prefix_table), prefix_len)
+    size = 0
     if workspace is None:
-        size = lib.sharq_attention_workspace_bytes(ctypes.byref(cs), ctypes.byref(bs), ctypes.byref(ts), heads)
+        size = lib.sharq_attention_workspace_bytes(cache.ref, batch.ref, ctypes.byref(ts), heads)
         if size:   # on the stream that uses it: freed on return, and taken again only behind the call
             with torch.cuda.stream(stream):
                 workspace = torch.empty(size, dtype=torch.uint8, device=q.device)
-    elif workspace.device != q.device or not workspace.is_contiguous():
+    elif workspace.get_device() != dev or not workspace.is_contiguous():
         raise SharqError(EINVAL, where)
-    _check(lib.sharq_attention(q.data_ptr(), BF16, heads, _ld(q), ctypes.byref(cs), ctypes.byref(bs), ctypes.byref(ts),
-                               out.data_ptr(), _ld(out), _ptr(lse), _ptr(workspace),
-                               0 if workspace is None else workspace.numel() * workspace.element_size(),
-                               _stream(stream)), where)
+    else:
+        size = workspace.nbytes
+    _check(lib.sharq_attention(q.data_ptr(), BF16, heads, ldq, cache.ref, batch.ref, ctypes.byref(ts), out.data_ptr(),
+                               ldo, _ptr(lse), _ptr(workspace), size, _stream(stream)), where)
     return out
 
 
