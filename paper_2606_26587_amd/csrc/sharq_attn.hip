@@ -59,15 +59,16 @@ __device__ __forceinline__ bool find_tile(const KvBatchArgs& b, int group, int u
 template <int D, bool MX, bool ALL>
 __global__ __launch_bounds__(256, 2) void k_attn(AttnArgs a, int tiles, int chunk_tiles, int first_slot) {
   constexpr int kC = D / 8, kDT = D / 32;   // 16-byte chunks of a row, 32-wide tiles of D
-  __shared__ uint4 sk[kT * kC], sv[kT * kC];
-  __shared__ int lds_p[8];
-  const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
+  __shared__ uint4 lds[2][2][kT * kC];      // two stages of keys and values
+  int* const lds_p = reinterpret_cast<int*>(lds);
+  const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
   // heads fastest: workgroups are dealt to the XCDs in turn, so each L2 sees few heads' keys and values.
   // Late tiles of a sequence, which see most tokens, first.
   const int head = (int)(blockIdx.x % (unsigned)a.c.heads);
   const int uc = (int)(blockIdx.x / (unsigned)a.c.heads), chunk = uc / tiles, unit = tiles - 1 - uc % tiles;
   const int rr = wave * 32 + (lane & 31);
-  int seq = 0, rows, row_g, qh, p, p_lo, p_hi, t0, t1;   // of this lane: row of the call, query head, position
+  int seq = 0, rows, row_g, qh, p;                  // of this lane: row of the call, query head, position
+  int p_lo, p_hi, w_lo, w_hi, t0, t1;               // positions of the workgroup's and the wavefront's rows; tokens
   if (ALL) {
     const int64_t total = (int64_t)kv_clamp(a.b.offs[a.b.seqs], 0, a.b.rows) * a.group, r0 = (int64_t)unit * kRowsA;
     if (r0 >= total) return;
@@ -91,6 +92,7 @@ __global__ __launch_bounds__(256, 2) void k_attn(AttnArgs a, int tiles, int chun
       const int u = __shfl_xor(lo, d), w = __shfl_xor(hi, d);
       lo = u < lo ? u : lo, hi = w > hi ? w : hi;
     }
+    w_lo = __builtin_amdgcn_readfirstlane(lo), w_hi = __builtin_amdgcn_readfirstlane(hi);
     if (lane == 0) lds_p[wave] = lo, lds_p[4 + wave] = hi;
     __syncthreads();
     p_lo = lds_p[0], p_hi = lds_p[4];
@@ -99,6 +101,7 @@ __global__ __launch_bounds__(256, 2) void k_attn(AttnArgs a, int tiles, int chun
       p_lo = lds_p[i] < p_lo ? lds_p[i] : p_lo;
       p_hi = lds_p[4 + i] > p_hi ? lds_p[4 + i] : p_hi;
     }
+    __syncthreads();
     t0 = 0, t1 = a.prefix_len;
   } else {
     int tile;
@@ -111,6 +114,8 @@ __global__ __launch_bounds__(256, 2) void k_attn(AttnArgs a, int tiles, int chun
     const int token = (int)(r / a.group);
     row_g = sr.first + token, qh = head * a.group + (int)(r % a.group), p = base + token;
     p_lo = base + (int)(r0 / a.group), p_hi = base + (int)((r0 + rows - 1) / a.group);
+    const int wr = wave * 32 < rows ? wave * 32 : rows - 1, we = wave * 32 + 31 < rows ? wave * 32 + 31 : rows - 1;
+    w_lo = base + (int)((r0 + wr) / a.group), w_hi = base + (int)((r0 + we) / a.group);
     t0 = a.t0, t1 = sr.len;
   }
 
@@ -125,34 +130,79 @@ __global__ __launch_bounds__(256, 2) void k_attn(AttnArgs a, int tiles, int chun
 
   const KvSpan span = kv_span(t0, t1, p_lo, p_hi, a.window, a.sinks, kT);
   const int first = chunk * chunk_tiles, end = span.n < first + chunk_tiles ? span.n : first + chunk_tiles;
-  for (int ti = first; ti < end; ++ti) {
-      const int ts = kv_tile_start(span, t0, ti, kT);
-      // lane i: cache row of token ts + i, -1 where no row of the tile sees it (it may hold anything)
-      const int t = ts + lane;
-      int at = -1;
-      if (t < span.hi && (t >= span.low || t < a.sinks)) at = token_row(a, seq, t, head);
-      const unsigned long long live = __ballot(at >= 0);
-      __syncthreads();
+  // lane i: cache row of token i of a tile, -1 where no row sees it (it may hold anything)
+  auto locate = [&](int ti) {
+    const int t = kv_tile_start(span, t0, ti, kT) + lane;
+    return ti < end && t < span.hi && (t >= span.low || t < a.sinks) ? token_row(a, seq, t, head) : -1;
+  };
+  // A wavefront stages 16 tokens of a tile, which lie in one page: tiles start at multiples of 16.
+  constexpr int kI = MX ? 1 : kC / 4;   // 16-byte loads of a lane, keys or values
+  constexpr int kRowLanes = MX ? D / 32 : kC, kRowsLoad = 64 / kRowLanes;   // lanes of a row; rows of a load
+  uint4 kb, vb;        // MXFP4: the next tile's codes and scales on their way
+  uint32_t ke, ve;
+  uint32_t off[kI];    // bf16: this lane's place in the 16 tokens; the exchange of chunks is made here
 #pragma unroll
-      for (int i = 0; i < kT * kC / 256; ++i) {
-        const int id = i * 256 + tid, row = id / kC, ch = id % kC;
-        const int64_t src = __shfl(at, row);
-        uint4 kx{}, vx{};
-        if (src >= 0) {
-          if (MX) {
-            kx = mx_bf16x8(*reinterpret_cast<const uint32_t*>(a.c.k + src * (D / 2) + ch * 4),
-                           a.c.ks[src * (D / 32) + ch / 4]);
-            vx = mx_bf16x8(*reinterpret_cast<const uint32_t*>(a.c.v + src * (D / 2) + ch * 4),
-                           a.c.vs[src * (D / 32) + ch / 4]);
-          } else {
-            kx = *reinterpret_cast<const uint4*>(a.c.k + src * (D * 2) + ch * 16);
-            vx = *reinterpret_cast<const uint4*>(a.c.v + src * (D * 2) + ch * 16);
-          }
-        }
-        sk[kv_chunk<D>(row, ch)] = kx;
-        sv[kv_chunk<D>(row, ch)] = vx;
+  for (int i = 0; i < kI; ++i) {
+    const int row = i * kRowsLoad + lane / kRowLanes;
+    off[i] = (uint32_t)(row * D * 2 + 16 * (MX ? 0 : kv_chunk<D>(row, lane % kRowLanes) - row * kC));
+  }
+  auto load = [&](int at, int stage) {
+    const unsigned mine = (unsigned)(__ballot(at >= 0) >> (16 * wave)) & 0xFFFFu;
+    if (MX) {
+      kb = vb = make_uint4(0, 0, 0, 0);
+      ke = ve = 0;
+    }
+    if (mine == 0) return;
+    const int l0 = 16 * wave + __builtin_ctz(mine);
+    const int64_t row0 = __builtin_amdgcn_readlane(at, l0) - (l0 & 15);
+    if (MX) {
+      const int row = lane / kRowLanes;   // D 64: rows past 15 are no lane's
+      if (row < 16 && ((mine >> row) & 1)) {
+        kb = *reinterpret_cast<const uint4*>(a.c.k + (row0 + row) * (D / 2) + 16 * (lane % kRowLanes));
+        vb = *reinterpret_cast<const uint4*>(a.c.v + (row0 + row) * (D / 2) + 16 * (lane % kRowLanes));
+        ke = a.c.ks[(row0 + row) * (D / 32) + lane % kRowLanes];
+        ve = a.c.vs[(row0 + row) * (D / 32) + lane % kRowLanes];
       }
-      __syncthreads();
+    } else {
+      const uint8_t *kp = a.c.k + row0 * (D * 2), *vp = a.c.v + row0 * (D * 2);
+#pragma unroll
+      for (int i = 0; i < kI; ++i)
+        if (mine == 0xFFFFu || ((mine >> (i * kRowsLoad + lane / kRowLanes)) & 1)) {
+          lds_load16(&lds[stage][0][wave * 16 * kC + i * 64], kp, off[i]);
+          lds_load16(&lds[stage][1][wave * 16 * kC + i * 64], vp, off[i]);
+        }
+    }
+  };
+  // What load() leaves out keeps its place in LDS: keys there are masked, values meet a weight of zero and must be
+  // finite.  So the stages start as zeros, and only tokens that some row sees come after.
+  auto store = [&](int stage) {
+    if (MX && lane / kRowLanes < 16) {
+      const int row = 16 * wave + lane / kRowLanes, c0 = 4 * (lane % kRowLanes);
+      const uint32_t kw[4] = {kb.x, kb.y, kb.z, kb.w}, vw[4] = {vb.x, vb.y, vb.z, vb.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        lds[stage][0][kv_chunk<D>(row, c0 + e)] = mx_bf16x8(kw[e], ke);
+        lds[stage][1][kv_chunk<D>(row, c0 + e)] = mx_bf16x8(vw[e], ve);
+      }
+    }
+  };
+  if (!MX) {
+    for (int i = tid; i < kT * kC; i += 256) lds[0][1][i] = lds[1][1][i] = make_uint4(0, 0, 0, 0);
+    __syncthreads();
+  }
+  int at = locate(first), next = locate(first + 1);
+  load(at, 0);
+  store(0);
+  lds_load_wait();
+  __syncthreads();
+  for (int ti = first; ti < end; ++ti) {
+    const int stage = (ti - first) & 1, ts = kv_tile_start(span, t0, ti, kT);
+    const unsigned long long live = __ballot(at >= 0);
+    at = next;
+    next = locate(ti + 2);
+    load(at, stage ^ 1);
+    if (ts <= w_hi) {
+      const uint4 *sk = lds[stage][0], *sv = lds[stage][1];
       v16f s[2] = {};
 #pragma unroll
       for (int mt = 0; mt < 2; ++mt)
@@ -161,32 +211,43 @@ __global__ __launch_bounds__(256, 2) void k_attn(AttnArgs a, int tiles, int chun
           const v8bf kf = *reinterpret_cast<const v8bf*>(&sk[kv_chunk<D>(mt * 32 + (lane & 31), 2 * i + half)]);
           s[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[i], s[mt], 0, 0, 0);
         }
-      float top = m;
+      // whether every row of the wavefront sees every token
+      if (live != ~0ull || ts + kT - 1 > w_lo || (w_hi - ts >= a.window && ts + kT > a.sinks)) {
 #pragma unroll
-      for (int mt = 0; mt < 2; ++mt)
+        for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int j = mt * 32 + 8 * (i >> 2) + 4 * half + (i & 3), tt = ts + j;
-          const bool seen = ((live >> j) & 1) && tt <= p && (p - tt < a.window || tt < a.sinks);
-          s[mt][i] = seen ? s[mt][i] : -__builtin_inff();
-          top = fmaxf(top, s[mt][i]);
-        }
+          for (int i = 0; i < 16; ++i) {
+            const int j = mt * 32 + 8 * (i >> 2) + 4 * half + (i & 3), tt = ts + j;
+            const bool seen = ((live >> j) & 1) && tt <= p && (p - tt < a.window || tt < a.sinks);
+            s[mt][i] = seen ? s[mt][i] : -__builtin_inff();
+          }
+      }
+      float top = fmaxf(s[0][0], s[1][0]);
+#pragma unroll
+      for (int i = 1; i < 16; ++i) top = fmaxf(top, fmaxf(s[0][i], s[1][i]));
       top = fmaxf(top, __shfl_xor(top, 32));
-      const float shift = attn_shift(top, a.scale), alpha = __builtin_amdgcn_exp2f((m - top) * a.scale);
-      m = top;
-      float sum = 0.0f;
+      // the state moves to the new maximum only where weights would pass 2^8: any reference serves that keeps them in range
+      if (__any((top - m) * a.scale > 8.0f)) {
+        top = fmaxf(top, m);
+        const float alpha = __builtin_amdgcn_exp2f((m - top) * a.scale);
+        m = top;
+        l *= alpha;
+#pragma unroll
+        for (int d = 0; d < kDT; ++d) o[d] *= alpha;
+      }
+      const float shift = attn_shift(m, a.scale);
       v8bf pf[4];
 #pragma unroll
-      for (int mt = 0; mt < 2; ++mt)
+      for (int st = 0; st < 4; ++st) {
+        float e[8];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[mt][i], a.scale, -shift));
-          sum += e;
-          pf[2 * mt + (i >> 3)][i & 7] = (__bf16)e;
+        for (int i = 0; i < 8; ++i) {
+          e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[st >> 1][8 * (st & 1) + i], a.scale, -shift));
+          l += e[i];
         }
-      l = l * alpha + sum;
-#pragma unroll
-      for (int d = 0; d < kDT; ++d) o[d] *= alpha;
+        pf[st] = __builtin_bit_cast(v8bf, make_uint4(bf16x2(e[0], e[1]), bf16x2(e[2], e[3]), bf16x2(e[4], e[5]),
+                                                     bf16x2(e[6], e[7])));
+      }
 #pragma unroll
       for (int st = 0; st < 4; ++st)
 #pragma unroll
@@ -198,6 +259,10 @@ __global__ __launch_bounds__(256, 2) void k_attn(AttnArgs a, int tiles, int chun
                                   lds_read_tr(at_lds + 16 * kv_chunk<D>(tok + 8, ch)));
           o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[st], o[d], 0, 0, 0);
         }
+    }
+    store(stage ^ 1);
+    lds_load_wait();
+    __syncthreads();
   }
   l += __shfl_xor(l, 32);
   if (rr >= rows) return;

@@ -50,6 +50,15 @@ __device__ __forceinline__ v4s lds_read_tr(const void* p) {
   return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)p);
 }
 
+// 16 bytes a lane from base + off straight to LDS, lane after lane from `lds` on
+// (both the same for the wavefront), and the wait for all of these loads.
+__device__ __forceinline__ void lds_load16(const void* lds, const uint8_t* base, uint32_t off) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+               :: "s"((uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)lds), "v"(off), "s"(base)
+               : "m0", "memory");
+}
+__device__ __forceinline__ void lds_load_wait() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
 __device__ __forceinline__ v8bf join_bf(v4s a, v4s b) {
   return __builtin_bit_cast(v8bf, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
