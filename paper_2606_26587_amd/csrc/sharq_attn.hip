@@ -21,6 +21,8 @@
 // P is rounded to bf16 for the second product (V is bf16, and so is the output);
 // m, l, o and the sum of P stay in fp32.
 
+#include <type_traits>
+
 #include "sharq_attn.hpp"
 
 namespace sharq {
@@ -95,17 +97,18 @@ __global__ __launch_bounds__(256, 2) void k_attn(AttnArgs a, int tiles, int chun
     w_lo = __builtin_amdgcn_readfirstlane(lo), w_hi = __builtin_amdgcn_readfirstlane(hi);
     if (lane == 0) lds_p[wave] = lo, lds_p[4 + wave] = hi;
     __syncthreads();
-    p_lo = lds_p[0], p_hi = lds_p[4];
+    p_lo = __builtin_amdgcn_readfirstlane(lds_p[0]), p_hi = __builtin_amdgcn_readfirstlane(lds_p[4]);
 #pragma unroll
     for (int i = 1; i < 4; ++i) {
-      p_lo = lds_p[i] < p_lo ? lds_p[i] : p_lo;
-      p_hi = lds_p[4 + i] > p_hi ? lds_p[4 + i] : p_hi;
+      const int u = __builtin_amdgcn_readfirstlane(lds_p[i]), w = __builtin_amdgcn_readfirstlane(lds_p[4 + i]);
+      p_lo = u < p_lo ? u : p_lo, p_hi = w > p_hi ? w : p_hi;
     }
     __syncthreads();
     t0 = 0, t1 = a.prefix_len;
   } else {
     int tile;
     if (!find_tile(a.b, a.group, unit, seq, tile)) return;
+    seq = __builtin_amdgcn_readfirstlane(seq), tile = __builtin_amdgcn_readfirstlane(tile);
     const SeqRows sr = seq_rows(a.b, seq);
     const int64_t r0 = (int64_t)tile * kRowsA, total = (int64_t)sr.n * a.group;
     const int base = sr.len - sr.n;   // position of the sequence's first row
@@ -124,6 +127,9 @@ __global__ __launch_bounds__(256, 2) void k_attn(AttnArgs a, int tiles, int chun
     const uint16_t* qp = a.q + (int64_t)row_g * a.ldq + (int64_t)qh * D + 8 * half;
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) qf[i] = *reinterpret_cast<const v8bf*>(qp + 16 * i);
+    // here, once: the loop's own waits would count the tiles' loads among these
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) asm volatile("" : "+v"(qf[i]));
   }
   v16f o[kDT] = {};
   float m = kNoMax, l = 0.0f;
@@ -190,37 +196,55 @@ __global__ __launch_bounds__(256, 2) void k_attn(AttnArgs a, int tiles, int chun
     for (int i = tid; i < kT * kC; i += 256) lds[0][1][i] = lds[1][1][i] = make_uint4(0, 0, 0, 0);
     __syncthreads();
   }
+  // Places of this lane's reads in a tile.  The exchange of chunks follows the token's last four bits, so 16 or 32
+  // tokens further on is a constant away.
+  int k_at[D / 16], v_at[kDT][2];
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i) k_at[i] = 16 * kv_chunk<D>(lane & 31, 2 * i + half);
+#pragma unroll
+  for (int d = 0; d < kDT; ++d)
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+      v_at[d][u] = 16 * kv_chunk<D>(8 * u + 4 * half + ((lane & 15) >> 2), 4 * d + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) +
+                   8 * (lane & 1);
+
   int at = locate(first), next = locate(first + 1);
   load(at, 0);
   store(0);
   lds_load_wait();
   __syncthreads();
-  for (int ti = first; ti < end; ++ti) {
-    const int stage = (ti - first) & 1, ts = kv_tile_start(span, t0, ti, kT);
+  auto step = [&](int ti, auto stage_c) {
+    constexpr int stage = decltype(stage_c)::value;
+    const int ts = kv_tile_start(span, t0, ti, kT);
     const unsigned long long live = __ballot(at >= 0);
     at = next;
     next = locate(ti + 2);
     load(at, stage ^ 1);
     if (ts <= w_hi) {
-      const uint4 *sk = lds[stage][0], *sv = lds[stage][1];
+      const char *sk = reinterpret_cast<const char*>(lds[stage][0]), *sv = reinterpret_cast<const char*>(lds[stage][1]);
       v16f s[2] = {};
 #pragma unroll
       for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) {
-          const v8bf kf = *reinterpret_cast<const v8bf*>(&sk[kv_chunk<D>(mt * 32 + (lane & 31), 2 * i + half)]);
+          const v8bf kf = *reinterpret_cast<const v8bf*>(sk + k_at[i] + mt * 32 * kC * 16);
           s[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[i], s[mt], 0, 0, 0);
         }
-      // whether every row of the wavefront sees every token
+      // unless every row of the wavefront sees every token
       if (live != ~0ull || ts + kT - 1 > w_lo || (w_hi - ts >= a.window && ts + kT > a.sinks)) {
+        // bit j: this lane's row sees token ts + 4 half + j
+        const int up = p - ts - 4 * half, from = a.window > up ? 0 : up - a.window + 1;
+        unsigned long long see = live >> (4 * half);
+        see &= up < 0 ? 0ull : up >= 63 ? ~0ull : (2ull << up) - 1;
+        const int sk_end = a.sinks - ts - 4 * half;
+        see &= (from <= 0 ? ~0ull : from > 63 ? 0ull : ~0ull << from) | (sk_end <= 0 ? 0ull : sk_end > 63 ? ~0ull : (1ull << sk_end) - 1);
 #pragma unroll
-        for (int mt = 0; mt < 2; ++mt)
+        for (int mt = 0; mt < 2; ++mt) {
+          const uint32_t bits = (uint32_t)(see >> (32 * mt));
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int j = mt * 32 + 8 * (i >> 2) + 4 * half + (i & 3), tt = ts + j;
-            const bool seen = ((live >> j) & 1) && tt <= p && (p - tt < a.window || tt < a.sinks);
-            s[mt][i] = seen ? s[mt][i] : -__builtin_inff();
-          }
+          for (int i = 0; i < 16; ++i)
+            s[mt][i] = bits & (1u << (8 * (i >> 2) + (i & 3))) ? s[mt][i] : -__builtin_inff();
+        }
       }
       float top = fmaxf(s[0][0], s[1][0]);
 #pragma unroll
@@ -252,17 +276,17 @@ __global__ __launch_bounds__(256, 2) void k_attn(AttnArgs a, int tiles, int chun
       for (int st = 0; st < 4; ++st)
 #pragma unroll
         for (int d = 0; d < kDT; ++d) {
-          const int tok = 16 * st + 4 * half + ((lane & 15) >> 2);
-          const int ch = 4 * d + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-          const char* at_lds = reinterpret_cast<const char*>(sv) + 8 * (lane & 1);
-          const v8bf vf = join_bf(lds_read_tr(at_lds + 16 * kv_chunk<D>(tok, ch)),
-                                  lds_read_tr(at_lds + 16 * kv_chunk<D>(tok + 8, ch)));
+          const v8bf vf = join_bf(lds_read_tr(sv + v_at[d][0] + st * 16 * kC * 16), lds_read_tr(sv + v_at[d][1] + st * 16 * kC * 16));
           o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[st], o[d], 0, 0, 0);
         }
     }
     store(stage ^ 1);
     lds_load_wait();
     __syncthreads();
+  };
+  for (int ti = first; ti < end; ti += 2) {
+    step(ti, std::integral_constant<int, 0>{});
+    if (ti + 1 < end) step(ti + 1, std::integral_constant<int, 1>{});
   }
   l += __shfl_xor(l, 32);
   if (rr >= rows) return;
