@@ -27,6 +27,7 @@
 
 namespace sharq {
 
+constexpr int kSchedMfma = 0x8, kSchedLdsRead = 0x100;   // kinds of instructions to the scheduler
 constexpr int kT = kAttnTile;        // tokens of a key/value tile
 constexpr int kRowsA = kAttnRows;    // rows of a workgroup: 32 a wavefront
 
@@ -223,13 +224,24 @@ __global__ __launch_bounds__(256, 2) void k_attn(AttnArgs a, int tiles, int chun
     if (ts <= w_hi) {
       const char *sk = reinterpret_cast<const char*>(lds[stage][0]), *sv = reinterpret_cast<const char*>(lds[stage][1]);
       v16f s[2] = {};
+      v8bf kf[2][D / 16];
 #pragma unroll
       for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
-        for (int i = 0; i < D / 16; ++i) {
-          const v8bf kf = *reinterpret_cast<const v8bf*>(sk + k_at[i] + mt * 32 * kC * 16);
-          s[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[i], s[mt], 0, 0, 0);
-        }
+        for (int i = 0; i < D / 16; ++i) kf[mt][i] = *reinterpret_cast<const v8bf*>(sk + k_at[i] + mt * 32 * kC * 16);
+#pragma unroll
+      for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i)
+          s[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[mt][i], qf[i], s[mt], 0, 0, 0);
+      // four keys ahead of the product that takes them
+      __builtin_amdgcn_sched_group_barrier(kSchedLdsRead, 4, 0);
+#pragma unroll
+      for (int i = 0; i < D / 8 - 4; ++i) {
+        __builtin_amdgcn_sched_group_barrier(kSchedMfma, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(kSchedLdsRead, 1, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(kSchedMfma, 4, 0);
       // unless every row of the wavefront sees every token
       if (live != ~0ull || ts + kT - 1 > w_lo || (w_hi - ts >= a.window && ts + kT > a.sinks)) {
         // bit j: this lane's row sees token ts + 4 half + j
@@ -246,9 +258,16 @@ __global__ __launch_bounds__(256, 2) void k_attn(AttnArgs a, int tiles, int chun
             s[mt][i] = bits & (1u << (8 * (i >> 2) + (i & 3))) ? s[mt][i] : -__builtin_inff();
         }
       }
-      float top = fmaxf(s[0][0], s[1][0]);
+      float tops[4] = {s[0][0], s[0][1], s[1][0], s[1][1]};
 #pragma unroll
-      for (int i = 1; i < 16; ++i) top = fmaxf(top, fmaxf(s[0][i], s[1][i]));
+      for (int i = 2; i < 16; i += 4)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {   // v_max3
+          const v16f& x = s[k >> 1];
+          const int at0 = i + 2 * (k & 1);
+          if (at0 < 16) tops[k] = fmaxf(fmaxf(tops[k], x[at0]), x[at0 + 1]);
+        }
+      float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
       top = fmaxf(top, __shfl_xor(top, 32));
       // the state moves to the new maximum only where weights would pass 2^8: any reference serves that keeps them in range
       if (__any((top - m) * a.scale > 8.0f)) {
