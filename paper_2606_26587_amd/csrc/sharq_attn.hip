@@ -135,6 +135,7 @@ __global__ __launch_bounds__(256, 2) void k_attn(AttnArgs a, int tiles, int chun
   v16f o[kDT] = {};
   float m = kNoMax, l = 0.0f;
 
+  if (wave * 32 >= rows) w_hi = -1;   // no rows: loads its share of the tiles, no more
   const KvSpan span = kv_span(t0, t1, p_lo, p_hi, a.window, a.sinks, kT);
   const int first = chunk * chunk_tiles, end = span.n < first + chunk_tiles ? span.n : first + chunk_tiles;
   // lane i: cache row of token i of a tile, -1 where no row sees it (it may hold anything)
@@ -244,12 +245,7 @@ __global__ __launch_bounds__(256, 2) void k_attn(AttnArgs a, int tiles, int chun
       __builtin_amdgcn_sched_group_barrier(kSchedMfma, 4, 0);
       // unless every row of the wavefront sees every token
       if (live != ~0ull || ts + kT - 1 > w_lo || (w_hi - ts >= a.window && ts + kT > a.sinks)) {
-        // bit j: this lane's row sees token ts + 4 half + j
-        const int up = p - ts - 4 * half, from = a.window > up ? 0 : up - a.window + 1;
-        unsigned long long see = live >> (4 * half);
-        see &= up < 0 ? 0ull : up >= 63 ? ~0ull : (2ull << up) - 1;
-        const int sk_end = a.sinks - ts - 4 * half;
-        see &= (from <= 0 ? ~0ull : from > 63 ? 0ull : ~0ull << from) | (sk_end <= 0 ? 0ull : sk_end > 63 ? ~0ull : (1ull << sk_end) - 1);
+        const unsigned long long see = row_sees(live, p, ts + 4 * half, 4 * half, a.window, a.sinks);
 #pragma unroll
         for (int mt = 0; mt < 2; ++mt) {
           const uint32_t bits = (uint32_t)(see >> (32 * mt));

@@ -76,6 +76,16 @@ __device__ __forceinline__ int token_row(const AttnArgs& a, int seq, int t, int 
   return kv_row(table[t >> a.c.page_shift], t, a.c.pages, a.c.heads, head, a.c.page_shift);
 }
 
+// Bit j: a row at position p sees token t + j; live: bit shift + j, that token is there.
+__device__ __forceinline__ unsigned long long row_sees(unsigned long long live, int p, int t, int shift, int window,
+                                                       int sinks) {
+  const int up = p - t, from = window > up ? 0 : up - window + 1, head = sinks - t;   // none of them wraps
+  const unsigned long long before = up < 0 ? 0ull : up >= 63 ? ~0ull : (2ull << up) - 1;
+  const unsigned long long after = from > 63 ? 0ull : ~0ull << from;
+  const unsigned long long first = head <= 0 ? 0ull : head > 63 ? ~0ull : (1ull << head) - 1;
+  return (live >> shift) & before & (after | first);
+}
+
 __device__ __forceinline__ float attn_lse(float m, float l, float scale) {
   return l > 0.0f ? (m * scale + __log2f(l)) * 0.69314718055994531f : -__builtin_inff();
 }

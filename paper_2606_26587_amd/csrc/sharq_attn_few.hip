@@ -36,10 +36,10 @@ template <int D, bool MX, int NQ, int NT>
 __global__ __launch_bounds__(256) void k_attn_few(AttnArgs a, int chunk_tiles, int first_slot) {
   constexpr int kC = D / 8, kJ = D / 32, kDT = D / 16;
   constexpr int kTok = kSub * NT;            // tokens of a wavefront's turn
-  constexpr int kKL = MX ? D / 64 : 0;       // dwordx2 loads of a lane's codes of a key
+  constexpr int kG16 = 2 * NT;               // 16-token groups of a turn: each lies in one page
   __shared__ uint4 lds[4][kSub * kC];
   __shared__ float2 lds_ml[4][16];
-  const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, col = lane & 15;
+  const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, col = lane & 15;
   const int head = (int)(blockIdx.x % (unsigned)a.c.heads);
   const int sc = (int)(blockIdx.x / (unsigned)a.c.heads), seq = sc % a.b.seqs, chunk = sc / a.b.seqs;
   const SeqRows sr = seq_rows(a.b, seq);
@@ -71,6 +71,10 @@ __global__ __launch_bounds__(256) void k_attn_few(AttnArgs a, int chunk_tiles, i
     return ti < last && t < span.hi && (t >= span.low || t < a.sinks) ? token_row(a, seq, t, head) : -1;
   };
   uint4* const v_lds = lds[wave];
+  int v_at[kDT];   // this lane's reads of the values' tile; 16 tokens further on is a constant away
+#pragma unroll
+  for (int d = 0; d < kDT; ++d)
+    v_at[d] = 16 * kv_chunk<D>(4 * g + (col >> 2), 2 * d + ((lane & 3) >> 1)) + 8 * (lane & 1);
   int next = locate(first + wave);
   for (int ti = first + wave; ti < last; ti += 4) {
     const int at = next, ts = kv_tile_start(span, a.t0, ti, kTok);
@@ -78,49 +82,39 @@ __global__ __launch_bounds__(256) void k_attn_few(AttnArgs a, int chunk_tiles, i
     // whether every row sees every token of the turn
     const bool whole = live == ~0ull && ts + kTok - 1 <= base &&
                        (p_hi - ts < a.window || ts + kTok <= a.sinks);
-    uint4 kb[NT][2][MX ? 1 : kJ], vb[NT][MX ? D / 64 : kC / 2];
-    uint32_t ke[NT][2], ve[NT][D / 64];
+    if (live == 0) {
+      next = locate(ti + 4);
+      continue;
+    }
+    // Every load is made: a token that no row sees takes its place in its page, and a group without a page takes
+    // another's.  Keys there are masked, values set to zero.
+    uint4 kb[kG16][MX ? 1 : kJ], vb[kG16][MX ? 1 : kC / 4];
+    uint32_t ke[kG16], ve[kG16];
+    const int l1 = __builtin_ctzll(live), any = __builtin_amdgcn_readlane(at, l1) - (l1 & 15);
 #pragma unroll
-    for (int u = 0; u < NT; ++u) {
-#pragma unroll
-      for (int mt = 0; mt < 2; ++mt) {
-        const int64_t row = __shfl(at, u * kSub + mt * 16 + col);
-        if (MX) {
-          kb[u][mt][0] = make_uint4(0, 0, 0, 0);
-          ke[u][mt] = 0;
-          if (row >= 0) {
-            const uint8_t* s = a.c.k + row * (D / 2) + g * (D / 8);
-            if (kKL == 2) kb[u][mt][0] = *reinterpret_cast<const uint4*>(s);
-            else reinterpret_cast<uint2&>(kb[u][mt][0]) = *reinterpret_cast<const uint2*>(s);
-            ke[u][mt] = a.c.ks[row * (D / 32) + g * (D / 32) / 4];
-          }
-        } else {
-#pragma unroll
-          for (int j = 0; j < kJ; ++j) {
-            kb[u][mt][j] = make_uint4(0, 0, 0, 0);
-            if (row >= 0) kb[u][mt][j] = *reinterpret_cast<const uint4*>(a.c.k + row * (D * 2) + 64 * j + 16 * g);
-          }
-        }
-      }
+    for (int i = 0; i < kG16; ++i) {
+      const unsigned mine = (unsigned)(live >> (16 * i)) & 0xFFFFu;
+      const int l0 = 16 * i + (mine ? __builtin_ctz(mine) : 0);
+      const int64_t row = mine ? __builtin_amdgcn_readlane(at, l0) - (l0 & 15) : any;
       if (MX) {
-        constexpr int kPer = D / 32;   // lanes of a row
-#pragma unroll
-        for (int i = 0; i < D / 64; ++i) {
-          const int64_t row = __shfl(at, u * kSub + i * (64 / kPer) + lane / kPer);
-          vb[u][i] = make_uint4(0, 0, 0, 0);
-          ve[u][i] = 0;
-          if (row >= 0) {
-            vb[u][i] = *reinterpret_cast<const uint4*>(a.c.v + row * (D / 2) + 16 * (lane % kPer));
-            ve[u][i] = a.c.vs[row * (D / 32) + lane % kPer];
-          }
+        const uint8_t *kp = a.c.k + row * (D / 2), *vp = a.c.v + row * (D / 2);
+        const uint8_t *kse = a.c.ks + row * (D / 32), *vse = a.c.vs + row * (D / 32);
+        const uint32_t ko = (uint32_t)(col * (D / 2) + g * (D / 8)), vo = (uint32_t)(lane * (D / 8));
+        if (D == 128) {
+          kb[i][0] = *reinterpret_cast<const uint4*>(kp + ko);
+          vb[i][0] = *reinterpret_cast<const uint4*>(vp + vo);
+        } else {
+          const uint2 x = *reinterpret_cast<const uint2*>(kp + ko), y = *reinterpret_cast<const uint2*>(vp + vo);
+          kb[i][0] = make_uint4(x.x, x.y, 0, 0), vb[i][0] = make_uint4(y.x, y.y, 0, 0);
         }
+        ke[i] = kse[(uint32_t)(col * (D / 32) + g * (D / 32) / 4)];
+        ve[i] = vse[(uint32_t)((lane >> 2) * (D / 32) + (lane & 3) * (D / 32) / 4)];
       } else {
+        const uint8_t *kp = a.c.k + row * (D * 2), *vp = a.c.v + row * (D * 2);
 #pragma unroll
-        for (int i = 0; i < kC / 2; ++i) {
-          const int64_t row = __shfl(at, u * kSub + i * (64 / kC) + lane / kC);
-          vb[u][i] = make_uint4(0, 0, 0, 0);
-          if (row >= 0) vb[u][i] = *reinterpret_cast<const uint4*>(a.c.v + row * (D * 2) + 16 * (lane % kC));
-        }
+        for (int j = 0; j < kJ; ++j) kb[i][j] = *reinterpret_cast<const uint4*>(kp + (uint32_t)(col * D * 2 + 16 * g) + 64 * j);
+#pragma unroll
+        for (int j = 0; j < kC / 4; ++j) vb[i][j] = *reinterpret_cast<const uint4*>(vp + (uint32_t)(lane * 16) + 1024 * j);
       }
     }
     next = locate(ti + 4);
@@ -133,28 +127,36 @@ __global__ __launch_bounds__(256) void k_attn_few(AttnArgs a, int chunk_tiles, i
         for (int j = 0; j < kJ; ++j) {
           uint4 kx;
           if (MX) {
-            const uint32_t w[4] = {kb[u][mt][0].x, kb[u][mt][0].y, kb[u][mt][0].z, kb[u][mt][0].w};
-            kx = mx_bf16x8(w[j], ke[u][mt]);
+            const uint4& w = kb[2 * u + mt][0];
+            kx = mx_bf16x8(j == 0 ? w.x : j == 1 ? w.y : j == 2 ? w.z : w.w, ke[2 * u + mt]);
           } else {
-            kx = kb[u][mt][j];
+            kx = kb[2 * u + mt][j];
           }
 #pragma unroll
           for (int n = 0; n < NQ; ++n)
             s[n][mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, kx), qf[n][j], s[n][mt], 0, 0, 0);
         }
       wave_sync();   // the reads of the turn before are done
-      if (MX) {
-        constexpr int kPer = D / 32;
 #pragma unroll
-        for (int i = 0; i < D / 64; ++i) {
-          const int t = i * (64 / kPer) + lane / kPer, c0 = 4 * (lane % kPer);
-          const uint32_t w[4] = {vb[u][i].x, vb[u][i].y, vb[u][i].z, vb[u][i].w};
+      for (int mt = 0; mt < 2; ++mt) {
+        const int i = 2 * u + mt;
+        const unsigned mine = (unsigned)(live >> (16 * i)) & 0xFFFFu;
+        if (MX) {
+          const int t = lane >> 2, c0 = (lane & 3) * (D / 32);
+          const uint32_t w[4] = {vb[i][0].x, vb[i][0].y, vb[i][0].z, vb[i][0].w};
+          const bool dead = !((mine >> t) & 1);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) v_lds[kv_chunk<D>(t, c0 + e)] = mx_bf16x8(w[e], ve[u][i]);
+          for (int e = 0; e < D / 32; ++e)   // zero codes times 2^-127
+            v_lds[16 * mt * kC + kv_chunk<D>(t, c0 + e)] = mx_bf16x8(dead ? 0 : w[e], dead ? 0 : ve[i]);
+        } else {
+#pragma unroll
+          for (int j = 0; j < kC / 4; ++j) {
+            const int t = j * (64 / kC) + lane / kC;
+            uint4 x = vb[i][j];
+            if (!((mine >> t) & 1)) x = make_uint4(0, 0, 0, 0);
+            v_lds[16 * mt * kC + kv_chunk<D>(t, lane % kC)] = x;
+          }
         }
-      } else {
-#pragma unroll
-        for (int i = 0; i < kC / 2; ++i) v_lds[kv_chunk<D>(i * (64 / kC) + lane / kC, lane % kC)] = vb[u][i];
       }
       wave_sync();
       v8bf pf[NQ];
@@ -163,14 +165,11 @@ __global__ __launch_bounds__(256) void k_attn_few(AttnArgs a, int chunk_tiles, i
 #pragma unroll
       for (int n = 0; n < NQ; ++n) {
         if (!whole) {
+          const uint32_t see = (uint32_t)(row_sees(live, p[n], ts + 4 * g, 4 * g, a.window, a.sinks) >> (kSub * u));
 #pragma unroll
           for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int j = u * kSub + mt * 16 + 4 * g + i, t = ts + j;
-              const bool seen = ((live >> j) & 1) && t <= p[n] && (p[n] - t < a.window || t < a.sinks);
-              s[n][mt][i] = seen ? s[n][mt][i] : -__builtin_inff();
-            }
+            for (int i = 0; i < 4; ++i) s[n][mt][i] = see & (1u << (16 * mt + i)) ? s[n][mt][i] : -__builtin_inff();
         }
         float top = fmaxf(fmaxf(fmaxf(s[n][0][0], s[n][0][1]), fmaxf(s[n][0][2], s[n][0][3])),
                           fmaxf(fmaxf(s[n][1][0], s[n][1][1]), fmaxf(s[n][1][2], s[n][1][3])));
@@ -198,10 +197,8 @@ __global__ __launch_bounds__(256) void k_attn_few(AttnArgs a, int chunk_tiles, i
       }
 #pragma unroll
       for (int d = 0; d < kDT; ++d) {
-        const int t = 4 * g + (col >> 2), ch = 2 * d + ((lane & 3) >> 1);
-        const char* base_lds = reinterpret_cast<const char*>(v_lds) + 8 * (lane & 1);
-        const v8bf vf = join_bf(lds_read_tr(base_lds + 16 * kv_chunk<D>(t, ch)),
-                                lds_read_tr(base_lds + 16 * kv_chunk<D>(t + 16, ch)));
+        const char* from = reinterpret_cast<const char*>(v_lds) + v_at[d];
+        const v8bf vf = join_bf(lds_read_tr(from), lds_read_tr(from + 16 * kC * 16));
 #pragma unroll
         for (int n = 0; n < NQ; ++n) o[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[n], o[n][d], 0, 0, 0);
       }
