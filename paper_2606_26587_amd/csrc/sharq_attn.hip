@@ -138,10 +138,13 @@ __global__ __launch_bounds__(256, 2) void k_attn(AttnArgs a, int tiles, int chun
   if (wave * 32 >= rows) w_hi = -1;   // no rows: loads its share of the tiles, no more
   const KvSpan span = kv_span(t0, t1, p_lo, p_hi, a.window, a.sinks, kT);
   const int first = chunk * chunk_tiles, end = span.n < first + chunk_tiles ? span.n : first + chunk_tiles;
-  // lane i: cache row of token i of a tile, -1 where no row sees it (it may hold anything)
-  auto locate = [&](int ti) {
+  // lane i: page of token i of a tile, -1 where no row sees it (it may hold anything), and its cache row
+  auto page_of = [&](int ti) {
     const int t = kv_tile_start(span, t0, ti, kT) + lane;
-    return ti < end && t < span.hi && (t >= span.low || t < a.sinks) ? token_row(a, seq, t, head) : -1;
+    return ti < end && t < span.hi && (t >= span.low || t < a.sinks) ? token_page(a, seq, t) : -1;
+  };
+  auto row_of = [&](int page, int ti) {
+    return kv_row(page, kv_tile_start(span, t0, ti, kT) + lane, a.c.pages, a.c.heads, head, a.c.page_shift);
   };
   // A wavefront stages 16 tokens of a tile, which lie in one page: tiles start at multiples of 16.
   constexpr int kI = MX ? 1 : kC / 4;   // 16-byte loads of a lane, keys or values
@@ -210,7 +213,7 @@ __global__ __launch_bounds__(256, 2) void k_attn(AttnArgs a, int tiles, int chun
       v_at[d][u] = 16 * kv_chunk<D>(8 * u + 4 * half + ((lane & 15) >> 2), 4 * d + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) +
                    8 * (lane & 1);
 
-  int at = locate(first), next = locate(first + 1);
+  int at = row_of(page_of(first), first), next = page_of(first + 1);   // rows of this tile, pages of the next
   load(at, 0);
   store(0);
   lds_load_wait();
@@ -219,9 +222,9 @@ __global__ __launch_bounds__(256, 2) void k_attn(AttnArgs a, int tiles, int chun
     constexpr int stage = decltype(stage_c)::value;
     const int ts = kv_tile_start(span, t0, ti, kT);
     const unsigned long long live = __ballot(at >= 0);
-    at = next;
-    next = locate(ti + 2);
+    at = row_of(next, ti + 1);
     load(at, stage ^ 1);
+    next = page_of(ti + 2);
     if (ts <= w_hi) {
       const char *sk = reinterpret_cast<const char*>(lds[stage][0]), *sv = reinterpret_cast<const char*>(lds[stage][1]);
       v16f s[2] = {};
@@ -265,8 +268,7 @@ __global__ __launch_bounds__(256, 2) void k_attn(AttnArgs a, int tiles, int chun
         }
       float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
       top = fmaxf(top, __shfl_xor(top, 32));
-      // the state moves to the new maximum only where weights would pass 2^8: any reference serves that keeps them in range
-      if (__any((top - m) * a.scale > 8.0f)) {
+      if (__any((top - m) * a.scale > kMaxStep)) {
         top = fmaxf(top, m);
         const float alpha = __builtin_amdgcn_exp2f((m - top) * a.scale);
         m = top;

@@ -67,13 +67,19 @@ __device__ __forceinline__ v8bf join_bf(v4s a, v4s b) {
 // number, so that no difference of maxima is a NaN.
 constexpr float kNoMax = -__FLT_MAX__;
 
+// The reference of a row's weights moves to a new maximum only when they would
+// pass 2^kMaxStep: any reference serves that keeps them in range, and moving it
+// costs a pass over the accumulators.
+constexpr float kMaxStep = 8.0f;
+
 // What scores, times scale, are taken less of before the exponential.
 __device__ __forceinline__ float attn_shift(float top, float scale) { return top == kNoMax ? 0.0f : top * scale; }
 
-// Cache row of token t of a sequence, -1 when its page is absent.
-__device__ __forceinline__ int token_row(const AttnArgs& a, int seq, int t, int head) {
+// Page of token t of a sequence.  Nothing is made of it here, so that it can be
+// on its way while a tile is worked on: kv_row() comes when the token's turn does.
+__device__ __forceinline__ int token_page(const AttnArgs& a, int seq, int t) {
   const int32_t* table = t < a.prefix_len ? a.prefix_table : a.b.table + seq * a.b.ldt;
-  return kv_row(table[t >> a.c.page_shift], t, a.c.pages, a.c.heads, head, a.c.page_shift);
+  return table[t >> a.c.page_shift];
 }
 
 // Bit j: a row at position p sees token t + j; live: bit shift + j, that token is there.

@@ -33,7 +33,7 @@ __device__ __forceinline__ void wave_sync() {
 }
 
 template <int D, bool MX, int NQ, int NT>
-__global__ __launch_bounds__(256) void k_attn_few(AttnArgs a, int chunk_tiles, int first_slot) {
+__global__ __launch_bounds__(256, 2) void k_attn_few(AttnArgs a, int chunk_tiles, int first_slot) {
   constexpr int kC = D / 8, kJ = D / 32, kDT = D / 16;
   constexpr int kTok = kSub * NT;            // tokens of a wavefront's turn
   constexpr int kG16 = 2 * NT;               // 16-token groups of a turn: each lies in one page
@@ -65,27 +65,26 @@ __global__ __launch_bounds__(256) void k_attn_few(AttnArgs a, int chunk_tiles, i
 #pragma unroll
   for (int n = 0; n < NQ; ++n) m[n] = kNoMax, l[n] = 0.0f;
 
-  // cache row of token (lane % kTok) of a turn, -1 where no row sees it (it may hold anything)
-  auto locate = [&](int ti) {
+  // page of token (lane % kTok) of a turn, -1 where no row sees it (it may hold anything)
+  auto page_of = [&](int ti) {
     const int t = kv_tile_start(span, a.t0, ti, kTok) + lane % kTok;
-    return ti < last && t < span.hi && (t >= span.low || t < a.sinks) ? token_row(a, seq, t, head) : -1;
+    return ti < last && t < span.hi && (t >= span.low || t < a.sinks) ? token_page(a, seq, t) : -1;
   };
   uint4* const v_lds = lds[wave];
   int v_at[kDT];   // this lane's reads of the values' tile; 16 tokens further on is a constant away
 #pragma unroll
   for (int d = 0; d < kDT; ++d)
     v_at[d] = 16 * kv_chunk<D>(4 * g + (col >> 2), 2 * d + ((lane & 3) >> 1)) + 8 * (lane & 1);
-  int next = locate(first + wave);
+  int next = page_of(first + wave);
   for (int ti = first + wave; ti < last; ti += 4) {
-    const int at = next, ts = kv_tile_start(span, a.t0, ti, kTok);
+    const int ts = kv_tile_start(span, a.t0, ti, kTok);
+    const int at = kv_row(next, ts + lane % kTok, a.c.pages, a.c.heads, head, a.c.page_shift);
     const unsigned long long live = __ballot(at >= 0);
     // whether every row sees every token of the turn
     const bool whole = live == ~0ull && ts + kTok - 1 <= base &&
                        (p_hi - ts < a.window || ts + kTok <= a.sinks);
-    if (live == 0) {
-      next = locate(ti + 4);
-      continue;
-    }
+    next = page_of(ti + 4);
+    if (live == 0) continue;
     // Every load is made: a token that no row sees takes its place in its page, and a group without a page takes
     // another's.  Keys there are masked, values set to zero.
     uint4 kb[kG16][MX ? 1 : kJ], vb[kG16][MX ? 1 : kC / 4];
@@ -117,7 +116,6 @@ __global__ __launch_bounds__(256) void k_attn_few(AttnArgs a, int chunk_tiles, i
         for (int j = 0; j < kC / 4; ++j) vb[i][j] = *reinterpret_cast<const uint4*>(vp + (uint32_t)(lane * 16) + 1024 * j);
       }
     }
-    next = locate(ti + 4);
 #pragma unroll
     for (int u = 0; u < NT; ++u) {
       v4f s[NQ][2] = {};
@@ -160,7 +158,7 @@ __global__ __launch_bounds__(256) void k_attn_few(AttnArgs a, int chunk_tiles, i
       }
       wave_sync();
       v8bf pf[NQ];
-      float alpha[NQ];
+      float top[NQ];
       bool moved = false;
 #pragma unroll
       for (int n = 0; n < NQ; ++n) {
@@ -171,29 +169,34 @@ __global__ __launch_bounds__(256) void k_attn_few(AttnArgs a, int chunk_tiles, i
 #pragma unroll
             for (int i = 0; i < 4; ++i) s[n][mt][i] = see & (1u << (16 * mt + i)) ? s[n][mt][i] : -__builtin_inff();
         }
-        float top = fmaxf(fmaxf(fmaxf(s[n][0][0], s[n][0][1]), fmaxf(s[n][0][2], s[n][0][3])),
-                          fmaxf(fmaxf(s[n][1][0], s[n][1][1]), fmaxf(s[n][1][2], s[n][1][3])));
-        top = fmaxf(top, __shfl_xor(top, 16));
-        top = fmaxf(fmaxf(top, __shfl_xor(top, 32)), m[n]);
-        moved |= top > m[n];
-        alpha[n] = __builtin_amdgcn_exp2f((m[n] - top) * a.scale);
-        m[n] = top;
-        const float shift = attn_shift(top, a.scale);
-        float sum = 0.0f, e[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][i >> 2][i & 3], a.scale, -shift));
-          sum += e[i];
-        }
-        pf[n] = __builtin_bit_cast(v8bf, make_uint4(bf16x2(e[0], e[1]), bf16x2(e[2], e[3]), bf16x2(e[4], e[5]),
-                                                    bf16x2(e[6], e[7])));
-        l[n] = l[n] * alpha[n] + sum;
+        top[n] = fmaxf(fmaxf(fmaxf(s[n][0][0], s[n][0][1]), fmaxf(s[n][0][2], s[n][0][3])),
+                       fmaxf(fmaxf(s[n][1][0], s[n][1][1]), fmaxf(s[n][1][2], s[n][1][3])));
+        top[n] = fmaxf(top[n], __shfl_xor(top[n], 16));
+        top[n] = fmaxf(top[n], __shfl_xor(top[n], 32));
+        moved |= (top[n] - m[n]) * a.scale > kMaxStep;
       }
       if (__any(moved)) {
 #pragma unroll
-        for (int n = 0; n < NQ; ++n)
+        for (int n = 0; n < NQ; ++n) {
+          top[n] = fmaxf(top[n], m[n]);
+          const float alpha = __builtin_amdgcn_exp2f((m[n] - top[n]) * a.scale);
+          m[n] = top[n];
+          l[n] *= alpha;
 #pragma unroll
-          for (int d = 0; d < kDT; ++d) o[n][d] *= alpha[n];
+          for (int d = 0; d < kDT; ++d) o[n][d] *= alpha;
+        }
+      }
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) {
+        const float shift = attn_shift(m[n], a.scale);
+        float e[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][i >> 2][i & 3], a.scale, -shift));
+          l[n] += e[i];
+        }
+        pf[n] = __builtin_bit_cast(v8bf, make_uint4(bf16x2(e[0], e[1]), bf16x2(e[2], e[3]), bf16x2(e[4], e[5]),
+                                                    bf16x2(e[6], e[7])));
       }
 #pragma unroll
       for (int d = 0; d < kDT; ++d) {
