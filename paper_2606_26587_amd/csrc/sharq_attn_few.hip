@@ -253,46 +253,67 @@ __global__ __launch_bounds__(256, 2) void k_attn_few(AttnArgs a, int chunk_tiles
   }
 }
 
-// Joins the partial results of a row and head: one workgroup, 256 / (D / 4)
-// groups of threads that take every slot in turn, so that a single long sequence
-// in 64 slots is read in a few trips.  Sums are formed in a fixed order: the same
-// call gives the same bits.
-template <int D>
+// Joins the partial results of a row and head.  D / 4 threads form a group; WIDE
+// false: a group for each item takes all of its few slots; true: all groups of a
+// workgroup share one item's many slots.  Eight slots' states and outputs are on
+// their way together (what a slot that saw nothing left unwritten is read and
+// dropped).  Sums are formed in a fixed order: the same call gives the same bits.
+template <int D, bool WIDE>
 __global__ __launch_bounds__(256) void k_attn_merge(AttnArgs a) {
-  constexpr int kPer = D / 4, kG = 256 / kPer;
-  __shared__ float4 lds_o[kG][kPer];
-  __shared__ float2 lds_s[kG];
+  constexpr int kPer = D / 4, kG = 256 / kPer, kTrip = 8;
+  __shared__ float4 lds_o[WIDE ? kG : 1][WIDE ? kPer : 1];
+  __shared__ float2 lds_s[WIDE ? kG : 1];
   const int64_t all = (int64_t)a.b.rows * a.q_heads;
   const int grp = (int)threadIdx.x / kPer, ch = (int)threadIdx.x % kPer;
   const int64_t items = (int64_t)kv_clamp(a.b.offs[a.b.seqs], 0, a.b.rows) * a.q_heads;   // without padding rows
-  for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+  for (int64_t i0 = blockIdx.x; i0 * (WIDE ? 1 : kG) < items; i0 += gridDim.x) {
+    const int64_t item = WIDE ? i0 : i0 * kG + grp;
     float top = kNoMax, sum = 0.0f;
     float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 4
-    for (int s = grp; s < a.slots; s += kG) {
-      const float2 t = a.ml[s * all + item];
-      if (!(t.y > 0.0f)) continue;   // that slot saw nothing: its output was not written
-      const float4 x = *reinterpret_cast<const float4*>(a.po + (s * all + item) * D + 4 * ch);
-      const float now = fmaxf(top, t.x), f = __builtin_amdgcn_exp2f((top - now) * a.scale),
-                  e = __builtin_amdgcn_exp2f((t.x - now) * a.scale);
-      sum = f * sum + e * t.y;
-      o.x = f * o.x + e * x.x, o.y = f * o.y + e * x.y, o.z = f * o.z + e * x.z, o.w = f * o.w + e * x.w;
-      top = now;
-    }
-    __syncthreads();   // the item before is done with
-    lds_o[grp][ch] = o;
-    if (ch == 0) lds_s[grp] = make_float2(top, sum);
-    __syncthreads();
-    if (grp != 0) continue;
-    top = kNoMax, sum = 0.0f, o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (WIDE || item < items)
+      for (int s0 = WIDE ? grp : 0; s0 < a.slots; s0 += kTrip * (WIDE ? kG : 1)) {
+        float2 t[kTrip];
+        float4 x[kTrip];
 #pragma unroll
-    for (int i = 0; i < kG; ++i) top = fmaxf(top, lds_s[i].x);
+        for (int i = 0; i < kTrip; ++i) {
+          const int s = s0 + i * (WIDE ? kG : 1);
+          const int64_t at = (s < a.slots ? s : s0) * all + item;
+          t[i] = a.ml[at];
+          x[i] = *reinterpret_cast<const float4*>(a.po + at * D + 4 * ch);
+          if (s >= a.slots) t[i].y = 0.0f;
+        }
+        float now = top;
 #pragma unroll
-    for (int i = 0; i < kG; ++i) {
-      const float e = __builtin_amdgcn_exp2f((lds_s[i].x - top) * a.scale);
-      const float4 x = lds_o[i][ch];
-      sum += e * lds_s[i].y;
-      o.x += e * x.x, o.y += e * x.y, o.z += e * x.z, o.w += e * x.w;
+        for (int i = 0; i < kTrip; ++i) now = t[i].y > 0.0f ? fmaxf(now, t[i].x) : now;
+        const float f = __builtin_amdgcn_exp2f((top - now) * a.scale);
+        sum *= f, o.x *= f, o.y *= f, o.z *= f, o.w *= f;
+        top = now;
+#pragma unroll
+        for (int i = 0; i < kTrip; ++i) {
+          if (!(t[i].y > 0.0f)) continue;
+          const float e = __builtin_amdgcn_exp2f((t[i].x - now) * a.scale);
+          sum += e * t[i].y;
+          o.x += e * x[i].x, o.y += e * x[i].y, o.z += e * x[i].z, o.w += e * x[i].w;
+        }
+      }
+    if (WIDE) {
+      __syncthreads();   // the item before is done with
+      lds_o[grp][ch] = o;
+      if (ch == 0) lds_s[grp] = make_float2(top, sum);
+      __syncthreads();
+      if (grp != 0) continue;
+      top = kNoMax, sum = 0.0f, o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+      for (int i = 0; i < kG; ++i) top = fmaxf(top, lds_s[i].x);
+#pragma unroll
+      for (int i = 0; i < kG; ++i) {
+        const float e = __builtin_amdgcn_exp2f((lds_s[i].x - top) * a.scale);
+        const float4 x = lds_o[i][ch];
+        sum += e * lds_s[i].y;
+        o.x += e * x.x, o.y += e * x.y, o.z += e * x.z, o.w += e * x.w;
+      }
+    } else if (item >= items) {
+      continue;
     }
     const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
     const int64_t row = item / a.q_heads, h = item % a.q_heads;
@@ -318,11 +339,19 @@ hipError_t launch_attn_few(const AttnArgs& a, int D, bool mx, int nq, int chunks
   return hipGetLastError();
 }
 
-hipError_t launch_attn_merge(const AttnArgs& a, int D, hipStream_t st) {
+template <int D>
+static void merge(const AttnArgs& a, hipStream_t st) {
   const int64_t items = (int64_t)a.b.rows * a.q_heads, most = 1 << 20;
-  const dim3 g((unsigned)(items < most ? items : most));
-  if (D == 128) k_attn_merge<128><<<g, 256, 0, st>>>(a);
-  else k_attn_merge<64><<<g, 256, 0, st>>>(a);
+  const bool wide = a.slots > 8;
+  const int64_t g = wide ? items : ceil_div(items, 256 / (D / 4));
+  const unsigned grid = (unsigned)(g < most ? g : most);
+  if (wide) k_attn_merge<D, true><<<grid, 256, 0, st>>>(a);
+  else k_attn_merge<D, false><<<grid, 256, 0, st>>>(a);
+}
+
+hipError_t launch_attn_merge(const AttnArgs& a, int D, hipStream_t st) {
+  if (D == 128) merge<128>(a, st);
+  else merge<64>(a, st);
   return hipGetLastError();
 }
 

@@ -109,7 +109,7 @@ constexpr AttnPlan attn_plan(int64_t seqs, int64_t rows, int64_t max_rows, int64
   if (p.few) {
     const int tok = mx ? 64 : 32;
     const int64_t kv = part > 0 ? ceil_div(part, tok) + (part < own ? 1 : 0) + ceil_div(s, tok) : 0;
-    p.own = attn_split(1, seqs * heads, kv, 1024, 4);
+    p.own = attn_split(1, seqs * heads, kv, 2048, 4);
   } else {
     // no sequence has more than max_rows rows, and all together have no more than rows
     const int64_t most = seqs * ceil_div(r, kAttnRows), packed = rows * group / kAttnRows + seqs;
