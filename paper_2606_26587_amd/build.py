@@ -39,7 +39,7 @@ HIP_FLAGS = [
 
 # The attention's running maxima: no canonicalisation of NaNs (none is an
 # operand that counts) in front of every v_max.
-SOURCE_FLAGS = {name: ["-fno-honor-nans"] for name in ("sharq_attn.hip", "sharq_attn_few.hip")}
+SOURCE_FLAGS = {name: ["-fno-honor-nans"] for name in ("sharq_attn.hip", "sharq_attn_few.hip", "sharq_attn_shared.hip")}
 
 
 def _compile(src: str) -> str:

@@ -1,339 +1,20 @@
-// Causal attention over the paged key/value cache, with a sliding window and
-// first tokens that stay visible (sinks).
-//
-// For a row at position p, o = sum_t w_t v_t over the tokens t <= p with
-// p - t < window or t < sinks, w = softmax(scale q.k).  One pass over the
-// tokens with the running maximum m and sum l of the softmax:
-//   m' = max(m, s_t), l' = l e^(m - m') + sum e^(s_t - m'), o' likewise.
-//
-// The rows of a key/value head's query heads are worked on together: row r of a
-// tile is token r / G, query head r % G of the G heads that share the cached
-// head, so a token's keys and values are read once for all of them.
-//
-// Both products are computed transposed, S^T = K Q^T and O^T = V^T P^T, with
-// 32x32x16 bf16 MFMAs.  A lane then holds one row of S (a column of S^T) and the
-// same row of O: maxima, sums and the rescaling by e^(m - m') need no broadcast,
-// and the accumulator registers of S^T, rounded to bf16, are the operand of the
-// second product as they stand, when the eight k slots of a lane half h are
-// taken as the tokens {4h..4h+3, 8+4h..8+4h+3} of each 16.  The matching V^T
-// operand comes from row-major V in LDS through the transposing LDS read.
-//
-// P is rounded to bf16 for the second product (V is bf16, and so is the output);
-// m, l, o and the sum of P stay in fp32.
+// Attention over the paged cache: the kernels for many rows, and the launches of
+// a call.
 
-#include <type_traits>
-
-#include "sharq_attn.hpp"
+#include "sharq_attn_rows.hpp"
 
 namespace sharq {
 
-constexpr int kSchedMfma = 0x8, kSchedLdsRead = 0x100;   // kinds of instructions to the scheduler
-constexpr int kT = kAttnTile;        // tokens of a key/value tile
-constexpr int kRowsA = kAttnRows;    // rows of a workgroup: 32 a wavefront
-
-// Sequence and tile of work unit `unit` of tiles of kRowsA rows; false: none.
-__device__ __forceinline__ bool find_tile(const KvBatchArgs& b, int group, int unit, int& seq, int& tile) {
-  const int lane = (int)(threadIdx.x & 63);
-  int base = 0;
-  for (int s0 = 0; s0 < b.seqs; s0 += 64) {
-    const int s = s0 + lane;
-    int n = 0;
-    if (s < b.seqs) n = (int)(((int64_t)seq_rows(b, s).n * group + kRowsA - 1) / kRowsA);
-    int sum = n;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const int o = __shfl_up(sum, d);
-      if (lane >= d) sum += o;
-    }
-    const unsigned long long past = __ballot(base + sum > unit);
-    if (past) {
-      const int l = __ffsll((unsigned long long)past) - 1;
-      seq = s0 + l;
-      tile = unit - base - (__shfl(sum, l) - __shfl(n, l));
-      return true;
-    }
-    base += __shfl(sum, 63);
-  }
-  return false;
-}
-
-// The rows of one tile: the sequences' own parts (ALL false: a tile's rows are
-// of one sequence) or the shared prefix (ALL: rows of all sequences).
 template <int D, bool MX, bool ALL>
-__global__ __launch_bounds__(256, 2) void k_attn(AttnArgs a, int tiles, int chunk_tiles, int first_slot) {
-  constexpr int kC = D / 8, kDT = D / 32;   // 16-byte chunks of a row, 32-wide tiles of D
-  __shared__ uint4 lds[2][2][kT * kC];      // two stages of keys and values
-  int* const lds_p = reinterpret_cast<int*>(lds);
-  const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
-  // heads fastest: workgroups are dealt to the XCDs in turn, so each L2 sees few heads' keys and values.
-  // Late tiles of a sequence, which see most tokens, first.
-  const int head = (int)(blockIdx.x % (unsigned)a.c.heads);
-  const int uc = (int)(blockIdx.x / (unsigned)a.c.heads), chunk = uc / tiles, unit = tiles - 1 - uc % tiles;
-  const int rr = wave * 32 + (lane & 31);
-  int seq = 0, rows, row_g, qh, p;                  // of this lane: row of the call, query head, position
-  int p_lo, p_hi, w_lo, w_hi, t0, t1;               // positions of the workgroup's and the wavefront's rows; tokens
-  if (ALL) {
-    const int64_t total = (int64_t)kv_clamp(a.b.offs[a.b.seqs], 0, a.b.rows) * a.group, r0 = (int64_t)unit * kRowsA;
-    if (r0 >= total) return;
-    rows = total - r0 < kRowsA ? (int)(total - r0) : kRowsA;
-    const int64_t r = r0 + (rr < rows ? rr : rows - 1);
-    row_g = (int)(r / a.group), qh = head * a.group + (int)(r % a.group);
-    const int last = (int)((r0 + rows - 1) / a.group);
-    // this lane's sequence: past those that end at or before its row, 64 offsets at a time
-    const int s0 = find_seq(a.b, (int)(r0 / a.group));
-    int s = s0;
-    for (int at = s0; at < a.b.seqs; at += 64) {
-      const int end = at + lane < a.b.seqs ? a.b.offs[at + lane + 1] : 0x7FFFFFFF;
-      for (int i = 0; i < 64; ++i) s += __builtin_amdgcn_readlane(end, i) <= row_g;
-      if (__builtin_amdgcn_readlane(end, 63) > last) break;
-    }
-    const SeqRows sr = seq_rows(a.b, s < a.b.seqs ? s : a.b.seqs - 1);
-    p = sr.len - sr.n + (row_g - sr.first);
-    int lo = p, hi = p;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-      const int u = __shfl_xor(lo, d), w = __shfl_xor(hi, d);
-      lo = u < lo ? u : lo, hi = w > hi ? w : hi;
-    }
-    w_lo = __builtin_amdgcn_readfirstlane(lo), w_hi = __builtin_amdgcn_readfirstlane(hi);
-    if (lane == 0) lds_p[wave] = lo, lds_p[4 + wave] = hi;
-    __syncthreads();
-    p_lo = __builtin_amdgcn_readfirstlane(lds_p[0]), p_hi = __builtin_amdgcn_readfirstlane(lds_p[4]);
-#pragma unroll
-    for (int i = 1; i < 4; ++i) {
-      const int u = __builtin_amdgcn_readfirstlane(lds_p[i]), w = __builtin_amdgcn_readfirstlane(lds_p[4 + i]);
-      p_lo = u < p_lo ? u : p_lo, p_hi = w > p_hi ? w : p_hi;
-    }
-    __syncthreads();
-    t0 = 0, t1 = a.prefix_len;
-  } else {
-    int tile;
-    if (!find_tile(a.b, a.group, unit, seq, tile)) return;
-    seq = __builtin_amdgcn_readfirstlane(seq), tile = __builtin_amdgcn_readfirstlane(tile);
-    const SeqRows sr = seq_rows(a.b, seq);
-    const int64_t r0 = (int64_t)tile * kRowsA, total = (int64_t)sr.n * a.group;
-    const int base = sr.len - sr.n;   // position of the sequence's first row
-    rows = total - r0 < kRowsA ? (int)(total - r0) : kRowsA;
-    const int64_t r = r0 + (rr < rows ? rr : rows - 1);
-    const int token = (int)(r / a.group);
-    row_g = sr.first + token, qh = head * a.group + (int)(r % a.group), p = base + token;
-    p_lo = base + (int)(r0 / a.group), p_hi = base + (int)((r0 + rows - 1) / a.group);
-    const int wr = wave * 32 < rows ? wave * 32 : rows - 1, we = wave * 32 + 31 < rows ? wave * 32 + 31 : rows - 1;
-    w_lo = base + (int)((r0 + wr) / a.group), w_hi = base + (int)((r0 + we) / a.group);
-    t0 = a.t0, t1 = sr.len;
-  }
-
-  v8bf qf[D / 16];
-  {
-    const uint16_t* qp = a.q + (int64_t)row_g * a.ldq + (int64_t)qh * D + 8 * half;
-#pragma unroll
-    for (int i = 0; i < D / 16; ++i) qf[i] = *reinterpret_cast<const v8bf*>(qp + 16 * i);
-    // here, once: the loop's own waits would count the tiles' loads among these
-#pragma unroll
-    for (int i = 0; i < D / 16; ++i) asm volatile("" : "+v"(qf[i]));
-  }
-  v16f o[kDT] = {};
-  float m = kNoMax, l = 0.0f;
-
-  if (wave * 32 >= rows) w_hi = -1;   // no rows: loads its share of the tiles, no more
-  const KvSpan span = kv_span(t0, t1, p_lo, p_hi, a.window, a.sinks, kT);
-  const int first = chunk * chunk_tiles, end = span.n < first + chunk_tiles ? span.n : first + chunk_tiles;
-  // lane i: page of token i of a tile, -1 where no row sees it (it may hold anything), and its cache row
-  auto page_of = [&](int ti) {
-    const int t = kv_tile_start(span, t0, ti, kT) + lane;
-    return ti < end && t < span.hi && (t >= span.low || t < a.sinks) ? token_page(a, seq, t) : -1;
-  };
-  auto row_of = [&](int page, int ti) {
-    return kv_row(page, kv_tile_start(span, t0, ti, kT) + lane, a.c.pages, a.c.heads, head, a.c.page_shift);
-  };
-  // A wavefront stages 16 tokens of a tile, which lie in one page: tiles start at multiples of 16.
-  constexpr int kI = MX ? 1 : kC / 4;   // 16-byte loads of a lane, keys or values
-  constexpr int kRowLanes = MX ? D / 32 : kC, kRowsLoad = 64 / kRowLanes;   // lanes of a row; rows of a load
-  uint4 kb, vb;        // MXFP4: the next tile's codes and scales on their way
-  uint32_t ke, ve;
-  uint32_t off[kI];    // bf16: this lane's place in the 16 tokens; the exchange of chunks is made here
-#pragma unroll
-  for (int i = 0; i < kI; ++i) {
-    const int row = i * kRowsLoad + lane / kRowLanes;
-    off[i] = (uint32_t)(row * D * 2 + 16 * (MX ? 0 : kv_chunk<D>(row, lane % kRowLanes) - row * kC));
-  }
-  auto load = [&](int at, int stage) {
-    const unsigned mine = (unsigned)(__ballot(at >= 0) >> (16 * wave)) & 0xFFFFu;
-    if (MX) {
-      kb = vb = make_uint4(0, 0, 0, 0);
-      ke = ve = 0;
-    }
-    if (mine == 0) return;
-    const int l0 = 16 * wave + __builtin_ctz(mine);
-    const int64_t row0 = __builtin_amdgcn_readlane(at, l0) - (l0 & 15);
-    if (MX) {
-      const int row = lane / kRowLanes;   // D 64: rows past 15 are no lane's
-      if (row < 16 && ((mine >> row) & 1)) {
-        kb = *reinterpret_cast<const uint4*>(a.c.k + (row0 + row) * (D / 2) + 16 * (lane % kRowLanes));
-        vb = *reinterpret_cast<const uint4*>(a.c.v + (row0 + row) * (D / 2) + 16 * (lane % kRowLanes));
-        ke = a.c.ks[(row0 + row) * (D / 32) + lane % kRowLanes];
-        ve = a.c.vs[(row0 + row) * (D / 32) + lane % kRowLanes];
-      }
-    } else {
-      const uint8_t *kp = a.c.k + row0 * (D * 2), *vp = a.c.v + row0 * (D * 2);
-#pragma unroll
-      for (int i = 0; i < kI; ++i)
-        if (mine == 0xFFFFu || ((mine >> (i * kRowsLoad + lane / kRowLanes)) & 1)) {
-          lds_load16(&lds[stage][0][wave * 16 * kC + i * 64], kp, off[i]);
-          lds_load16(&lds[stage][1][wave * 16 * kC + i * 64], vp, off[i]);
-        }
-    }
-  };
-  // What load() leaves out keeps its place in LDS: keys there are masked, values meet a weight of zero and must be
-  // finite.  So the stages start as zeros, and only tokens that some row sees come after.
-  auto store = [&](int stage) {
-    if (MX && lane / kRowLanes < 16) {
-      const int row = 16 * wave + lane / kRowLanes, c0 = 4 * (lane % kRowLanes);
-      const uint32_t kw[4] = {kb.x, kb.y, kb.z, kb.w}, vw[4] = {vb.x, vb.y, vb.z, vb.w};
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        lds[stage][0][kv_chunk<D>(row, c0 + e)] = mx_bf16x8(kw[e], ke);
-        lds[stage][1][kv_chunk<D>(row, c0 + e)] = mx_bf16x8(vw[e], ve);
-      }
-    }
-  };
-  if (!MX) {
-    for (int i = tid; i < kT * kC; i += 256) lds[0][1][i] = lds[1][1][i] = make_uint4(0, 0, 0, 0);
-    __syncthreads();
-  }
-  // Places of this lane's reads in a tile.  The exchange of chunks follows the token's last four bits, so 16 or 32
-  // tokens further on is a constant away.
-  int k_at[D / 16], v_at[kDT][2];
-#pragma unroll
-  for (int i = 0; i < D / 16; ++i) k_at[i] = 16 * kv_chunk<D>(lane & 31, 2 * i + half);
-#pragma unroll
-  for (int d = 0; d < kDT; ++d)
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-      v_at[d][u] = 16 * kv_chunk<D>(8 * u + 4 * half + ((lane & 15) >> 2), 4 * d + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) +
-                   8 * (lane & 1);
-
-  int at = row_of(page_of(first), first), next = page_of(first + 1);   // rows of this tile, pages of the next
-  load(at, 0);
-  store(0);
-  lds_load_wait();
-  __syncthreads();
-  auto step = [&](int ti, auto stage_c) {
-    constexpr int stage = decltype(stage_c)::value;
-    const int ts = kv_tile_start(span, t0, ti, kT);
-    const unsigned long long live = __ballot(at >= 0);
-    at = row_of(next, ti + 1);
-    load(at, stage ^ 1);
-    next = page_of(ti + 2);
-    if (ts <= w_hi) {
-      const char *sk = reinterpret_cast<const char*>(lds[stage][0]), *sv = reinterpret_cast<const char*>(lds[stage][1]);
-      v16f s[2] = {};
-      v8bf kf[2][D / 16];
-#pragma unroll
-      for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-        for (int i = 0; i < D / 16; ++i) kf[mt][i] = *reinterpret_cast<const v8bf*>(sk + k_at[i] + mt * 32 * kC * 16);
-#pragma unroll
-      for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-        for (int i = 0; i < D / 16; ++i)
-          s[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[mt][i], qf[i], s[mt], 0, 0, 0);
-      // four keys ahead of the product that takes them
-      __builtin_amdgcn_sched_group_barrier(kSchedLdsRead, 4, 0);
-#pragma unroll
-      for (int i = 0; i < D / 8 - 4; ++i) {
-        __builtin_amdgcn_sched_group_barrier(kSchedMfma, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(kSchedLdsRead, 1, 0);
-      }
-      __builtin_amdgcn_sched_group_barrier(kSchedMfma, 4, 0);
-      // unless every row of the wavefront sees every token
-      if (live != ~0ull || ts + kT - 1 > w_lo || (w_hi - ts >= a.window && ts + kT > a.sinks)) {
-        const unsigned long long see = row_sees(live, p, ts + 4 * half, 4 * half, a.window, a.sinks);
-#pragma unroll
-        for (int mt = 0; mt < 2; ++mt) {
-          const uint32_t bits = (uint32_t)(see >> (32 * mt));
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            s[mt][i] = bits & (1u << (8 * (i >> 2) + (i & 3))) ? s[mt][i] : -__builtin_inff();
-        }
-      }
-      float tops[4] = {s[0][0], s[0][1], s[1][0], s[1][1]};
-#pragma unroll
-      for (int i = 2; i < 16; i += 4)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {   // v_max3
-          const v16f& x = s[k >> 1];
-          const int at0 = i + 2 * (k & 1);
-          if (at0 < 16) tops[k] = fmaxf(fmaxf(tops[k], x[at0]), x[at0 + 1]);
-        }
-      float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-      top = fmaxf(top, __shfl_xor(top, 32));
-      if (__any((top - m) * a.scale > kMaxStep)) {
-        top = fmaxf(top, m);
-        const float alpha = __builtin_amdgcn_exp2f((m - top) * a.scale);
-        m = top;
-        l *= alpha;
-#pragma unroll
-        for (int d = 0; d < kDT; ++d) o[d] *= alpha;
-      }
-      const float shift = attn_shift(m, a.scale);
-      v8bf pf[4];
-#pragma unroll
-      for (int st = 0; st < 4; ++st) {
-        float e[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[st >> 1][8 * (st & 1) + i], a.scale, -shift));
-          l += e[i];
-        }
-        pf[st] = __builtin_bit_cast(v8bf, make_uint4(bf16x2(e[0], e[1]), bf16x2(e[2], e[3]), bf16x2(e[4], e[5]),
-                                                     bf16x2(e[6], e[7])));
-      }
-#pragma unroll
-      for (int st = 0; st < 4; ++st)
-#pragma unroll
-        for (int d = 0; d < kDT; ++d) {
-          const v8bf vf = join_bf(lds_read_tr(sv + v_at[d][0] + st * 16 * kC * 16), lds_read_tr(sv + v_at[d][1] + st * 16 * kC * 16));
-          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[st], o[d], 0, 0, 0);
-        }
-    }
-    store(stage ^ 1);
-    lds_load_wait();
-    __syncthreads();
-  };
-  for (int ti = first; ti < end; ti += 2) {
-    step(ti, std::integral_constant<int, 0>{});
-    if (ti + 1 < end) step(ti + 1, std::integral_constant<int, 1>{});
-  }
-  l += __shfl_xor(l, 32);
-  if (rr >= rows) return;
-  if (a.slots) {
-    const int64_t at = ((int64_t)(first_slot + chunk) * a.b.rows + row_g) * a.q_heads + qh;
-    if (half == 0) a.ml[at] = make_float2(m, l);
-    if (!(l > 0.0f)) return;
-#pragma unroll
-    for (int d = 0; d < kDT; ++d)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        *reinterpret_cast<float4*>(a.po + at * D + 32 * d + 8 * i + 4 * half) =
-            make_float4(o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]);
-    return;
-  }
-  const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-  uint16_t* op = a.o + (int64_t)row_g * a.ldo + (int64_t)qh * D;
-#pragma unroll
-  for (int d = 0; d < kDT; ++d)
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      *reinterpret_cast<uint2*>(op + 32 * d + 8 * i + 4 * half) =
-          make_uint2(bf16x2(o[d][4 * i] * inv, o[d][4 * i + 1] * inv), bf16x2(o[d][4 * i + 2] * inv, o[d][4 * i + 3] * inv));
-  if (a.lse && half == 0) a.lse[(int64_t)row_g * a.q_heads + qh] = attn_lse(m, l, a.scale);
+__global__ __launch_bounds__(256, 2) void k_attn_rows(AttnArgs a, int tiles, int chunk_tiles, int first_slot) {
+  __shared__ RowsLds<D> lds;
+  attn_rows<D, MX, ALL>(a, (int)blockIdx.x, tiles, chunk_tiles, first_slot, lds);
 }
 
 template <int D, bool MX>
 static void rows(bool all, dim3 g, const AttnArgs& a, int tiles, int chunk_tiles, int first_slot, hipStream_t st) {
-  if (all) k_attn<D, MX, true><<<g, 256, 0, st>>>(a, tiles, chunk_tiles, first_slot);
-  else k_attn<D, MX, false><<<g, 256, 0, st>>>(a, tiles, chunk_tiles, first_slot);
+  if (all) k_attn_rows<D, MX, true><<<g, 256, 0, st>>>(a, tiles, chunk_tiles, first_slot);
+  else k_attn_rows<D, MX, false><<<g, 256, 0, st>>>(a, tiles, chunk_tiles, first_slot);
 }
 
 static hipError_t launch_attn_rows(const AttnArgs& a, int D, bool mx, bool all, const AttnSplit& s, int first_slot,
@@ -348,8 +29,8 @@ static hipError_t launch_attn_rows(const AttnArgs& a, int D, bool mx, bool all, 
   return hipGetLastError();
 }
 
-hipError_t launch_attn_few(const AttnArgs& a, int D, bool mx, int nq, int chunks, int chunk_tiles, int first_slot,
-                           hipStream_t st);
+hipError_t launch_attn_few(const AttnArgs& a, int D, bool mx, const AttnPlan& plan, hipStream_t st);
+hipError_t launch_attn_shared(const AttnArgs& a, int D, bool mx, const AttnPlan& plan, hipStream_t st);
 hipError_t launch_attn_merge(const AttnArgs& a, int D, hipStream_t st);
 
 hipError_t launch_attention(const uint16_t* q, int64_t ldq, uint16_t* o, int64_t ldo, float* lse,
@@ -362,10 +43,13 @@ hipError_t launch_attention(const uint16_t* q, int64_t ldq, uint16_t* o, int64_t
              static_cast<float2*>(ws), nullptr, plan.slots};
   if (plan.slots) a.po = reinterpret_cast<float*>(static_cast<char*>(ws) + attn_ml_bytes(items, plan.slots));
   hipError_t e = hipSuccess;
-  if (plan.shared) e = launch_attn_rows(a, D, mx, true, plan.prefix, plan.own.chunks, st);
-  if (e != hipSuccess) return e;
-  e = plan.few ? launch_attn_few(a, D, mx, plan.few, plan.own.chunks, plan.own.chunk_tiles, 0, st)
-               : launch_attn_rows(a, D, mx, false, plan.own, 0, st);
+  if (plan.shared && plan.few) {
+    e = launch_attn_shared(a, D, mx, plan, st);
+  } else {
+    if (plan.shared) e = launch_attn_rows(a, D, mx, true, plan.prefix, plan.own.chunks, st);
+    if (e != hipSuccess) return e;
+    e = plan.few ? launch_attn_few(a, D, mx, plan, st) : launch_attn_rows(a, D, mx, false, plan.own, 0, st);
+  }
   if (e != hipSuccess || plan.slots == 0) return e;
   return launch_attn_merge(a, D, st);
 }

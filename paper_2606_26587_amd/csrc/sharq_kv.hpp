@@ -94,14 +94,14 @@ constexpr AttnSplit attn_split(int64_t tiles, int64_t units, int64_t kv_tiles, i
   return {(int)tiles, (int)chunks, (int)each};
 }
 
-constexpr AttnPlan attn_plan(int64_t seqs, int64_t rows, int64_t max_rows, int64_t max_len, int heads, int group,
+constexpr AttnPlan attn_plan(int64_t seqs, int64_t rows, int64_t max_rows, int64_t max_len, int heads, int group, int D,
                              bool mx, int64_t window, int64_t sinks, int64_t prefix_len) {
   AttnPlan p{};
   if (max_rows > rows) max_rows = rows;
   // a window leaves little of a prefix, and rows that see different parts of it
   p.shared = prefix_len > 0 && window >= max_len;
   const int64_t r = max_rows * group, own = max_len - (p.shared ? prefix_len : 0);
-  p.few = r <= 16 ? 1 : r <= 32 ? 2 : r <= 64 ? 4 : 0;
+  p.few = r <= 16 ? 1 : r <= 32 ? 2 : r <= 64 && D == 64 ? 4 : 0;   // (heads of 128: 64 rows' states fill the registers)
   // tokens that a tile of rows sees at most: its window and its own positions, and the sinks
   const int64_t span = p.few ? max_rows : kAttnRows / group + 2;
   const int64_t w = window < max_len ? window + span : own, part = w < own ? w : own;
@@ -120,7 +120,7 @@ constexpr AttnPlan attn_plan(int64_t seqs, int64_t rows, int64_t max_rows, int64
   p.slots = p.own.chunks > 1 ? p.own.chunks : 0;
   if (p.shared) {
     const int64_t tiles = ceil_div(rows * group, kAttnRows);
-    p.prefix = attn_split(tiles, tiles * heads, ceil_div(prefix_len, kAttnTile), 512, 4);
+    p.prefix = attn_split(tiles, tiles * heads, ceil_div(prefix_len, kAttnTile), 256, 4);
     p.slots = p.own.chunks + p.prefix.chunks;
   }
   return p;

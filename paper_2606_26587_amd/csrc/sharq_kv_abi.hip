@@ -99,7 +99,7 @@ int attn_window(const sharq_attn* t) { return t->window == 0 || t->window > INT_
 int attn_sinks(const sharq_attn* t) { return t->sinks > INT_MAX ? INT_MAX : (int)t->sinks; }
 
 sharq::AttnPlan plan_of(const sharq_kv_cache* c, const sharq_kv_batch* b, const sharq_attn* t, int64_t q_heads) {
-  return sharq::attn_plan(b->seqs, b->rows, b->max_rows, b->max_len, c->kv_heads, (int)(q_heads / c->kv_heads),
+  return sharq::attn_plan(b->seqs, b->rows, b->max_rows, b->max_len, c->kv_heads, (int)(q_heads / c->kv_heads), c->head_dim,
                           c->fmt == SHARQ_KV_MXFP4, attn_window(t), attn_sinks(t), t->prefix_len);
 }
 
