@@ -63,6 +63,17 @@ __device__ __forceinline__ v8bf join_bf(v4s a, v4s b) {
   return __builtin_bit_cast(v8bf, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
+// A wavefront's LDS writes before, its reads (of other lanes' data) after.
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+__device__ __forceinline__ int64_t shfl64(int64_t v, int lane) {
+  return (int64_t)((uint64_t)(uint32_t)__shfl((int)v, lane) | (uint64_t)(uint32_t)__shfl((int)(v >> 32), lane) << 32);
+}
+
 // A row that saw nothing has sum 0 and the running maximum's start, a finite
 // number, so that no difference of maxima is a NaN.
 constexpr float kNoMax = -__FLT_MAX__;

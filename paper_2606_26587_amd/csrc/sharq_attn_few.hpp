@@ -27,13 +27,6 @@ namespace sharq {
 
 constexpr int kSub = 32;   // tokens of one pass through the two products
 
-// The wavefronts' LDS writes before, its reads after (other lanes' data, one wavefront).
-__device__ __forceinline__ void wave_sync() {
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-}
-
 template <int D>
 struct FewLds {
   uint4 v[4][kSub * D / 8];   // a wavefront's values; at the end the wavefronts' outputs

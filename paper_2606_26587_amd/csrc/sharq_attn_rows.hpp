@@ -328,28 +328,49 @@ __device__ __forceinline__ void attn_rows(const AttnArgs& a, int block, int tile
     if (ti + 1 < end) step(ti + 1, std::integral_constant<int, 1>{});
   }
   l += __shfl_xor(l, 32);
-  if (rr >= rows) return;
+  const int mine = rows - wave * 32 < 32 ? rows - wave * 32 : 32;   // rows of this wavefront
+  if (mine <= 0) return;
+  // A lane has four neighbouring values of its row at a time; through this wavefront's own quarter of LDS (the tiles
+  // are done with) they leave as whole rows.  Chunks are exchanged by row, so that 32 rows at one chunk use all banks.
+  const int64_t item = (int64_t)row_g * a.q_heads + qh;
+  char* const mem = reinterpret_cast<char*>(&lds[0][0][0]) + wave * (32 * D * 4);
   if (a.slots) {
-    const int64_t at = ((int64_t)(first_slot + chunk) * a.b.rows + row_g) * a.q_heads + qh;
-    if (half == 0) a.ml[at] = make_float2(m, l);
-    if (!(l > 0.0f)) return;
+    const int64_t slot = (int64_t)(first_slot + chunk) * a.b.rows * a.q_heads + item;
+    if (half == 0 && lane < mine) a.ml[slot] = make_float2(m, l);
+    constexpr int kR = D / 4;   // 16-byte chunks of a row
 #pragma unroll
     for (int d = 0; d < kDT; ++d)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        *reinterpret_cast<float4*>(a.po + at * D + 32 * d + 8 * i + 4 * half) =
+        *reinterpret_cast<float4*>(mem + 16 * ((lane & 31) * kR + ((8 * d + 2 * i + half) ^ (lane & (kR - 1) & 31)))) =
             make_float4(o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]);
+    wave_sync();
+#pragma unroll
+    for (int k = 0; k < kR / 2; ++k) {
+      const int row = k * (64 / kR) + lane / kR, ch = lane % kR;
+      const int64_t to = shfl64(slot, row);
+      const float4 x = *reinterpret_cast<const float4*>(mem + 16 * (row * kR + (ch ^ (row & (kR - 1)))));
+      if (row < mine) *reinterpret_cast<float4*>(a.po + to * D + 4 * ch) = x;
+    }
     return;
   }
   const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-  uint16_t* op = a.o + (int64_t)row_g * a.ldo + (int64_t)qh * D;
+  const int64_t out = (int64_t)row_g * a.ldo + (int64_t)qh * D;
 #pragma unroll
   for (int d = 0; d < kDT; ++d)
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      *reinterpret_cast<uint2*>(op + 32 * d + 8 * i + 4 * half) =
+      *reinterpret_cast<uint2*>(mem + 16 * ((lane & 31) * kC + ((4 * d + i) ^ (lane & (kC - 1)))) + 8 * half) =
           make_uint2(bf16x2(o[d][4 * i] * inv, o[d][4 * i + 1] * inv), bf16x2(o[d][4 * i + 2] * inv, o[d][4 * i + 3] * inv));
-  if (a.lse && half == 0) a.lse[(int64_t)row_g * a.q_heads + qh] = attn_lse(m, l, a.scale);
+  wave_sync();
+#pragma unroll
+  for (int k = 0; k < kC / 2; ++k) {
+    const int row = k * (64 / kC) + lane / kC, ch = lane % kC;
+    const int64_t to = shfl64(out, row);
+    const uint4 x = *reinterpret_cast<const uint4*>(mem + 16 * (row * kC + (ch ^ (row & (kC - 1)))));
+    if (row < mine) *reinterpret_cast<uint4*>(a.o + to + 8 * ch) = x;
+  }
+  if (a.lse && half == 0 && lane < mine) a.lse[item] = attn_lse(m, l, a.scale);
 }
 
 }  // namespace sharq
