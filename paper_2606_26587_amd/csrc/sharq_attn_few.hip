@@ -35,10 +35,12 @@ __global__ __launch_bounds__(256) void k_attn_merge(AttnArgs a) {
 #pragma unroll
         for (int i = 0; i < kTrip; ++i) {
           const int s = s0 + i * (WIDE ? kG : 1);
-          const int64_t at = (s < a.slots ? s : s0) * all + item;
-          t[i] = a.ml[at];
-          x[i] = *reinterpret_cast<const float4*>(a.po + at * D + 4 * ch);
-          if (s >= a.slots) t[i].y = 0.0f;
+          t[i] = make_float2(kNoMax, 0.0f);
+          if (s < a.slots) {
+            const int64_t at = s * all + item;
+            t[i] = a.ml[at];
+            x[i] = *reinterpret_cast<const float4*>(a.po + at * D + 4 * ch);
+          }
         }
         float now = top;
 #pragma unroll
@@ -97,10 +99,12 @@ hipError_t launch_attn_few(const AttnArgs& a, int D, bool mx, const AttnPlan& pl
   return hipGetLastError();
 }
 
+constexpr int64_t kWideItems = 1024;
+
 template <int D>
 static void merge(const AttnArgs& a, hipStream_t st) {
   const int64_t items = (int64_t)a.b.rows * a.q_heads, most = 1 << 20;
-  const bool wide = a.slots > 8;
+  const bool wide = a.slots > 8 && items <= kWideItems;
   const int64_t g = wide ? items : ceil_div(items, 256 / (D / 4));
   const unsigned grid = (unsigned)(g < most ? g : most);
   if (wide) k_attn_merge<D, true><<<grid, 256, 0, st>>>(a);

@@ -109,18 +109,18 @@ constexpr AttnPlan attn_plan(int64_t seqs, int64_t rows, int64_t max_rows, int64
   if (p.few) {
     const int tok = mx ? 64 : 32;
     const int64_t kv = part > 0 ? ceil_div(part, tok) + (part < own ? 1 : 0) + ceil_div(s, tok) : 0;
-    p.own = attn_split(1, seqs * heads, kv, 2048, 4);
+    p.own = attn_split(1, seqs * heads, kv, p.shared ? 512 : 2048, 4);
   } else {
     // no sequence has more than max_rows rows, and all together have no more than rows
     const int64_t most = seqs * ceil_div(r, kAttnRows), packed = rows * group / kAttnRows + seqs;
     const int64_t tiles = most < packed ? most : packed;
     const int64_t kv = part > 0 ? ceil_div(part, kAttnTile) + (part < own ? 1 : 0) + ceil_div(s, kAttnTile) : 0;
-    p.own = attn_split(tiles, tiles * heads, kv, 512, 4);
+    p.own = attn_split(tiles, tiles * heads, kv, D == 64 ? 1024 : 512, 4);
   }
   p.slots = p.own.chunks > 1 ? p.own.chunks : 0;
   if (p.shared) {
     const int64_t tiles = ceil_div(rows * group, kAttnRows);
-    p.prefix = attn_split(tiles, tiles * heads, ceil_div(prefix_len, kAttnTile), 256, 4);
+    p.prefix = attn_split(tiles, tiles * heads, ceil_div(prefix_len, kAttnTile), 256, 2);
     p.slots = p.own.chunks + p.prefix.chunks;
   }
   return p;
