@@ -453,18 +453,20 @@ _BF = torch.bfloat16
 
 def _rows(t: torch.Tensor, rows: int, width: int, dev: int, where: str) -> int:
     """Row stride of a row tensor [rows, width], bf16 on device `dev`, its rows contiguous."""
-    if t.dtype is not _BF or t.shape != (rows, width) or t.get_device() != dev:
-        raise SharqError(EINVAL, where)
-    ld, inner = t.stride()
-    if inner != 1 and width > 1:
-        raise SharqError(EINVAL, where)
-    return ld if rows > 1 else width   # the stride of a single row means nothing
+    if t.dtype is _BF and t.shape == (rows, width) and t.get_device() == dev:
+        ld, inner = t.stride()
+        if inner == 1 or width <= 1:
+            return ld if rows > 1 else width   # the stride of a single row means nothing
+    raise SharqError(EINVAL, where)
+
+
+_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def _here(cache: KVCache, batch: KVBatch, where: str):
     """The kernels are launched on the current device: the buffers must be its own."""
     dev = cache.device_index
-    if dev < 0 or dev != batch.device_index or dev != torch.cuda.current_device():
+    if dev < 0 or dev != batch.device_index or dev != _device():
         raise SharqError(EINVAL, where)
 
 
@@ -493,16 +495,18 @@ def sharq_kv_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor,
         raise SharqError(EINVAL, where)
     if cos is not None:
         angles = cos.shape[0]
-        for t in (cos, sin):
-            if (t.dtype is not torch.float32 or t.shape != (angles, cache.head_dim // 2) or not t.is_contiguous()
-                    or t.get_device() != dev):
-                raise SharqError(EINVAL, where)
+        shape = (angles, cache.head_dim // 2)
+        if not (cos.dtype is sin.dtype is torch.float32 and cos.shape == sin.shape == shape and cos.is_contiguous()
+                and sin.is_contiguous() and cos.get_device() == sin.get_device() == dev):
+            raise SharqError(EINVAL, where)
     if positions is not None and (positions.dtype is not torch.int32 or positions.shape != (rows,)
                                   or not positions.is_contiguous() or positions.get_device() != dev):
         raise SharqError(EINVAL, where)
-    _check(lib.sharq_kv_append(_ptr(q), k.data_ptr(), v.data_ptr(), BF16, heads, ldq, ldk, ldv, _ptr(cos), _ptr(sin),
-                               angles, _ptr(positions), cache.ref, batch.ref, None if q is None else q_out.data_ptr(),
-                               ldo, _stream(stream)), where)
+    status = lib.sharq_kv_append(_ptr(q), k.data_ptr(), v.data_ptr(), BF16, heads, ldq, ldk, ldv, _ptr(cos), _ptr(sin),
+                                 angles, _ptr(positions), cache.ref, batch.ref, None if q is None else q_out.data_ptr(),
+                                 ldo, _stream(stream))
+    if status:
+        raise SharqError(status, where)
     return None if q is None else q_out
 
 

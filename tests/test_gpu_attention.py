@@ -196,3 +196,181 @@ def test_large_scale_where_a_wavefront_sees_nothing(per, fmt):
     """The running maximum's start times a scale above 1 is not a number that may enter a sum."""
     run([per], [500], 16, 4, 1, 128, fmt, scale=3.0, bad_pages=[(0, j, -1) for j in range(24)], peak=0.3)
     run([per, per], [per, 70], 16, 4, 1, 128, fmt, scale=3.0, window=20, prefix_len=32, peak=0.3)
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("count", [65, 130, 200])
+def test_more_sequences_than_a_wavefront(count, fmt):
+    rng = np.random.default_rng(count)
+    lens = [int(x) for x in rng.integers(0, 90, count)]
+    run([min(n, 1) for n in lens], lens, 16, 4, 2, 64, fmt, pad=3, seed=count)
+    per = [int(rng.integers(0, n + 1)) for n in lens]
+    per[7], lens[7] = 40, 60                            # (more rows than the kernel for few rows takes)
+    run(per, lens, 16, 4, 2, 64, fmt, pad=3, seed=count)
+    lens = [64 + n for n in lens]
+    run([1] * count, lens, 16, 8, 2, 64, fmt, prefix_len=64, seed=count)
+    run([int(x) for x in rng.integers(0, 40, count)], lens, 16, 2, 1, 64, fmt, prefix_len=64, seed=count)
+
+
+def setup(per, lens, page, hq, hkv, D, fmt, slack=0, more_rows=0, pad=0, seed=3):
+    batch, offsets, lens, table, pages = make_batch(per, lens, page, pad, spare=2 + slack // page, seed=seed)
+    if slack or more_rows:
+        batch = S.KVBatch(batch.row_offsets, batch.lens, batch.page_table, batch.rows, batch.max_rows + more_rows,
+                          batch.max_len + slack)
+    cache = filled_cache(pages, page, hkv, D, fmt, seed)
+    q = R.bf16(np.random.default_rng(seed).standard_normal((batch.rows, hq * D))).to(DEV)
+    return batch, offsets, lens, table, cache, q
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("per,lens", [([1, 1], [300, 40]), ([50, 3], [300, 40])])
+def test_loose_bounds_of_the_batch(per, lens, fmt):
+    """max_len and max_rows bound the sequences; how far above they are changes the split, not the result."""
+    for slack, more in ((0, 0), (160, 0), (16000, 3), (16, 100)):
+        batch, offsets, ln, table, cache, q = setup(per, lens, 16, 4, 2, 128, fmt, slack, more)
+        out = torch.full((batch.rows, 4 * 128), 9.0, dtype=torch.bfloat16, device=DEV)
+        lse = torch.full((batch.rows, 4), 9.0, device=DEV)
+        S.sharq_attention(q, cache, batch, out=out, lse=lse)
+        check(q, cache, batch, offsets, ln, table, out, lse)
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+def test_strided_rows_default_output_and_repeated_calls(fmt):
+    per, lens = [1, 1, 1, 2], [4000, 17, 256, 2000]
+    batch, offsets, ln, table, cache, q = setup(per, lens, 64, 8, 2, 128, fmt)
+    wide = torch.zeros((batch.rows, 8 * 128 + 64), dtype=torch.bfloat16, device=DEV)
+    wide[:, 32:-32] = q
+    first = S.sharq_attention(q, cache, batch)
+    again = S.sharq_attention(wide[:, 32:-32], cache, batch, out=wide[:, 32:-32].clone())
+    assert torch.equal(first, again)
+    outw = torch.full_like(wide, 5.0)
+    S.sharq_attention(wide[:, 32:-32], cache, batch, out=outw[:, 32:-32])
+    assert torch.equal(outw[:, 32:-32], first) and (outw[:, :32] == 5).all() and (outw[:, -32:] == 5).all()
+    # the table as a slice of a wider one, and a workspace full of NaN
+    big = torch.full((4, 200), -1, dtype=torch.int32, device=DEV)
+    big[:, :table.shape[1]] = batch.page_table
+    sliced = S.KVBatch(batch.row_offsets, batch.lens, big[:, :table.shape[1] + 1], batch.rows, batch.max_rows, batch.max_len)
+    ws = torch.full((S.attention_workspace_bytes(cache, sliced, 8),), 255, dtype=torch.uint8, device=DEV)
+    assert ws.numel() > 0
+    assert torch.equal(S.sharq_attention(q, cache, sliced, workspace=ws), first)
+    with pytest.raises(S.SharqError):
+        S.sharq_attention(q, cache, sliced, workspace=ws[:-16])
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+def test_streams_and_graphs(fmt):
+    """A call on a stream of its own, and one captured decode step (append, attention, behind a shared prefix too)
+    replayed on changed inputs, with eager calls between the replays."""
+    per, lens, page, hq, hkv, D = [1] * 6, [300, 290, 4000, 256, 257, 310], 64, 8, 2, 128
+    batch, offsets, ln, table, cache, q = setup(per, lens, page, hq, hkv, D, fmt)
+    rows = batch.rows
+    gen = torch.Generator(device=DEV).manual_seed(0)
+    x = torch.randn((rows, (hq + 2 * hkv) * D), generator=gen, device=DEV).to(torch.bfloat16)
+    cos, sin = (torch.from_numpy(t).to(DEV) for t in np_tables(5000, D))
+    pt = batch.page_table[2, :4].contiguous()
+    q_out, out, out2 = (torch.zeros((rows, hq * D), dtype=torch.bfloat16, device=DEV) for _ in range(3))
+    ws = torch.empty(max(S.attention_workspace_bytes(cache, batch, hq),
+                         S.attention_workspace_bytes(cache, batch, hq, prefix_len=256)), dtype=torch.uint8, device=DEV)
+
+    def step(stream=None):
+        w = hq * D, (hq + hkv) * D
+        S.sharq_kv_append(x[:, :w[0]], x[:, w[0]:w[1]], x[:, w[1]:], cache, batch, cos, sin, q_out=q_out, stream=stream)
+        S.sharq_attention(q_out, cache, batch, out=out, workspace=ws, stream=stream)
+        S.sharq_attention(q_out, cache, batch, prefix_table=pt, prefix_len=256, out=out2, workspace=ws, stream=stream)
+
+    step()
+    torch.cuda.synchronize()
+    want, want2 = out.clone(), out2.clone()
+    side = torch.cuda.Stream()
+    out.zero_()
+    out2.zero_()
+    side.wait_stream(torch.cuda.current_stream())
+    step(side)
+    # (a workspace that the call allocates itself is taken on that stream)
+    mine = S.sharq_attention(q_out, cache, batch, stream=side, out=torch.empty_like(out))
+    side.synchronize()
+    assert torch.equal(out, want) and torch.equal(out2, want2) and torch.equal(mine, want)
+
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for i in range(4):
+        x.copy_(torch.randn(x.shape, generator=gen, device=DEV))
+        batch.lens.copy_(torch.tensor([n - i for n in lens], dtype=torch.int32))
+        out.zero_()
+        out2.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        got, got2, pools = out.clone(), out2.clone(), (cache.k.clone(), cache.v.clone())
+        step()
+        torch.cuda.synchronize()
+        assert torch.equal(got, out) and torch.equal(got2, out2)
+        assert torch.equal(pools[0].view(torch.uint8), cache.k.view(torch.uint8))
+        assert torch.equal(pools[1].view(torch.uint8), cache.v.view(torch.uint8))
+        assert not torch.equal(got, want)
+
+
+def np_tables(n, D):
+    a = np.arange(n)[:, None] * 10000.0 ** (-2.0 * np.arange(D // 2) / D)
+    return np.cos(a).astype(np.float32), np.sin(a).astype(np.float32)
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+def test_offsets_past_32_bits(fmt):
+    """Pools whose byte offsets (and, in bf16, element offsets) pass 2^32: the pages at the far end."""
+    page, hkv, D, hq = 64, 8, 128, 16
+    row = D * 2 if fmt == "bf16" else D // 2
+    pages = (5 << 30) // (page * hkv * row) if fmt == "mx" else (9 << 30) // (page * hkv * row)
+    cache = S.alloc_kv_cache(pages, page, hkv, D, fmt, DEV)
+    assert cache.k.numel() * cache.k.element_size() > 1 << 32
+    lens, per = [300, 70], [300, 3]
+    near = np.arange(pages - 7, pages).astype(np.int32)
+    table = np.stack([near[:5], np.array([near[5], near[6], 0, 0, 0], np.int32)])
+    offsets = np.array([0, 300, 370], np.int32)
+    rng = np.random.default_rng(0)
+    x = R.bf16(rng.standard_normal((370, 2 * hkv * D)))
+    t = [torch.from_numpy(a).to(DEV) for a in (offsets, np.array([300, 70], np.int32), table)]
+    S.sharq_kv_append(None, x[:, :hkv * D].to(DEV), x[:, hkv * D:].to(DEV), cache, S.KVBatch(*t, 370, 300, 300))
+    k, v = S.sharq_kv_read(cache, S.KVBatch(*t, 370, 300, 300))
+    if fmt == "bf16":
+        assert torch.equal(k.cpu(), x[:, :hkv * D]) and torch.equal(v.cpu(), x[:, hkv * D:])
+    # the same pages at the front of a small pool
+    small = S.KVCache(fmt, *(None if p is None else p[-7:].clone() for p in
+                             (cache.k, cache.v, cache.k_scale, cache.v_scale)))
+    q = R.bf16(rng.standard_normal((370, hq * D))).to(DEV)
+    for per, rows in (([300, 70], 370), ([1, 3], 4)):
+        o = torch.tensor(np.concatenate([[0], np.cumsum(per)]), dtype=torch.int32, device=DEV)
+        far = S.KVBatch(o, t[1], t[2], rows, max(per), 300)
+        low = S.KVBatch(o, t[1], t[2] - (pages - 7), rows, max(per), 300)
+        assert torch.equal(S.sharq_attention(q[:rows], cache, far), S.sharq_attention(q[:rows], small, low))
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+def test_a_sequence_served_step_by_step(fmt):
+    """A prompt in chunks and then single tokens through append and attention, as a program serves it, against the whole
+    prompt in one call: the same keys are read, so the outputs agree to the roundings of two calls."""
+    hq, hkv, D, page, n = 8, 2, 128, 16, 150
+    rng = np.random.default_rng(9)
+    x = R.bf16(rng.standard_normal((n, (hq + 2 * hkv) * D))).to(DEV)
+    cos, sin = (torch.from_numpy(t).to(DEV) for t in np_tables(n, D))
+    table = torch.randperm(12, generator=torch.Generator().manual_seed(1)).to(torch.int32)[None].to(DEV)
+    cache = S.alloc_kv_cache(12, page, hkv, D, fmt, DEV)
+    w = hq * D, (hq + hkv) * D
+    got, lses = [], []
+    at = 0
+    for m in [64, 33, 20] + [1] * 33:
+        batch = S.KVBatch(torch.tensor([0, m], dtype=torch.int32, device=DEV),
+                          torch.tensor([at + m], dtype=torch.int32, device=DEV), table, m, m, 12 * page)
+        y = x[at:at + m]
+        q = S.sharq_kv_append(y[:, :w[0]], y[:, w[0]:w[1]], y[:, w[1]:], cache, batch, cos, sin)
+        lse = torch.empty((m, hq), device=DEV)
+        got.append(S.sharq_attention(q, cache, batch, lse=lse))
+        lses.append(lse)
+        at += m
+    offsets, lens = [0, n], [n]
+    whole = S.KVBatch(torch.tensor(offsets, dtype=torch.int32, device=DEV),
+                      torch.tensor(lens, dtype=torch.int32, device=DEV), table, n, n, 12 * page)
+    q = S.sharq_kv_append(x[:, :w[0]], x[:, w[0]:w[1]], x[:, w[1]:], cache, whole, cos, sin)
+    check(q, cache, whole, offsets, lens, table.cpu().numpy(), torch.cat(got), torch.cat(lses))
+    lse = torch.empty((n, hq), device=DEV)
+    check(q, cache, whole, offsets, lens, table.cpu().numpy(), S.sharq_attention(q, cache, whole, lse=lse), lse)
