@@ -35,6 +35,12 @@ Other workloads (--workload), one JSON line each:
                 flow: the residual add fused into the qkv and gate/up
                 preparations and SiLU.mul into the down projection's, whose
                 input is the gate/up GEMM's own output
+  llama-layer   a whole Llama-3.1-8B decoder layer: the linears with those
+                fusions, the o projection, and between qkv and o the rotation
+                and append to the paged key/value cache and the attention that
+                reads it; a prompt of 2048 tokens, and 64 single tokens over
+                4096 cached ones each, with the cache in bf16 and in MXFP4 (one
+                line each, in tokens per second of one layer)
   ablation      the path combinations (Sparse, plain FP4 RTN, Dense+Dense,
                 Sparse+Sparse, SharQ) on the Llama prefill linears, MXFP4 2:4
                 and NVFP4 4:8 in pairs, and SharQ with HiF4 2:4: time per step
@@ -785,6 +791,104 @@ def llama_fused(args, torch, S, synth, dev, stream):
     return out
 
 
+LAYER_HEADS = (32, 8, 128)       # query heads, key/value heads, their width
+LAYER_PAGE = 64
+LAYER_CASES = (("prompt of 2048 tokens", 1, T_TOKENS, T_TOKENS), ("64 tokens over 4096 each", 64, 1, 4096))
+LAYER_OPS = ("prep_residual_qkv", "gemm_qkv", "kv_append", "attention", "prep_o", "gemm_o", "prep_residual_gate_up",
+             "gemm_gate_up", "prep_silu_mul_down", "gemm_down")
+
+
+def attention_work(seqs, new, length, kv_fmt):
+    """(flops, bytes) of causal attention for the last `new` of `length` tokens of each sequence: 4 D per query head
+    and visible pair; queries and outputs, and every cached key and value once."""
+    hq, hkv, D = LAYER_HEADS
+    pairs = seqs * (new * (length - new) + new * (new + 1) // 2)
+    held = 2.0 if kv_fmt == "bf16" else 0.5 + 1.0 / 32
+    return 4.0 * D * hq * pairs, seqs * (new * hq * D * 4.0 + 2.0 * length * hkv * D * held)
+
+
+def llama_layer(args, torch, S, synth, dev, stream):
+    """One Llama-3.1-8B decoder layer per step: residual add and RMSNorm into the qkv preparation, qkv, rotation and
+    append, attention, o projection, residual add and RMSNorm into the gate/up preparation, gate/up, SiLU.mul into
+    the down preparation, down.  MXFP4 2:4 linears on the dense backbone copy."""
+    def to_dev(u16):
+        return torch.from_numpy(np.ascontiguousarray(u16).view(np.int16)).view(torch.bfloat16).to(dev)
+
+    hq, hkv, D = LAYER_HEADS
+    eps, H, I = synth.LLAMA_EPS, synth.LLAMA_LINEARS["qkv"][0], synth.LLAMA_LINEARS["down"][0]
+    shapes = dict(synth.LLAMA_LINEARS, o=(hq * D, H, False))
+    weights = {n: S.sharq_quantize_weight(to_dev(synth.weight(N, K, seed=0))) for n, (K, N, _) in shapes.items()}
+    gammas = {n: to_dev(synth.gamma(K, seed=0)) for n, (K, _, norm) in shapes.items() if norm}
+    angle = np.arange(8192)[:, None] * 500000.0 ** (-2.0 * np.arange(D // 2) / D)
+    cos, sin = (torch.from_numpy(f(angle).astype(np.float32)).to(dev) for f in (np.cos, np.sin))
+    for what, seqs, new, length in LAYER_CASES:
+        T = seqs * new
+        x_in = [to_dev(synth.activations(T, H, seed=s)) for s in range(N_INPUT_SETS)]
+        res0 = to_dev(synth.activations(T, H, seed=20))
+        act = {n: S.alloc_act(T, K, 2, 4, "mx", dev, dense_only=True) for n, (K, _, _) in shapes.items()}
+        y = {n: torch.empty((T, N), dtype=torch.bfloat16, device=dev) for n, (_, N, _) in shapes.items()}
+        per = -(-length // LAYER_PAGE)
+        table = torch.randperm(seqs * per, generator=torch.Generator().manual_seed(0)).to(torch.int32)
+        batch = S.KVBatch(torch.arange(seqs + 1, dtype=torch.int32, device=dev) * new,
+                          torch.full((seqs,), length, dtype=torch.int32, device=dev),
+                          table.view(seqs, per).to(dev), T, new, length)
+        for fmt in ("bf16", "mx"):
+            # cached tokens: rows of a normal distribution, appended by the library itself
+            cache = S.alloc_kv_cache(seqs * per, LAYER_PAGE, hkv, D, fmt, dev)
+            whole = S.KVBatch(torch.arange(seqs + 1, dtype=torch.int32, device=dev) * length, batch.lens,
+                              batch.page_table, seqs * length, length, length)
+            kv = torch.randn((seqs * length, hkv * D), device=dev).to(torch.bfloat16)
+            S.sharq_kv_append(None, kv, kv, cache, whole)
+            del kv, whole
+            res = res0.clone()
+            q, a = (torch.empty((T, hq * D), dtype=torch.bfloat16, device=dev) for _ in range(2))
+            ws = torch.empty(S.attention_workspace_bytes(cache, batch, hq), dtype=torch.uint8, device=dev)
+            q_w, k_w = hq * D, (hq + hkv) * D
+
+            def step(i, mark):
+                x = x_in[i % N_INPUT_SETS]
+                res.copy_(res0)
+                mark(0)
+                S.sharq_prepare_residual(x, res, gammas["qkv"], eps, 2, 4, "mx", h_out=res, out=act["qkv"],
+                                         stream=stream)
+                mark(1)
+                z = S.sharq_linear(act["qkv"], weights["qkv"], out=y["qkv"], stream=stream)
+                mark(2)
+                S.sharq_kv_append(z[:, :q_w], z[:, q_w:k_w], z[:, k_w:], cache, batch, cos, sin, q_out=q,
+                                  stream=stream)
+                mark(3)
+                S.sharq_attention(q, cache, batch, out=a, workspace=ws, stream=stream)
+                mark(4)
+                S.sharq_prepare(a, None, eps, 2, 4, "mx", out=act["o"], stream=stream)
+                mark(5)
+                S.sharq_linear(act["o"], weights["o"], out=y["o"], stream=stream)
+                mark(6)
+                S.sharq_prepare_residual(y["o"], res, gammas["gate_up"], eps, 2, 4, "mx", h_out=res,
+                                         out=act["gate_up"], stream=stream)
+                mark(7)
+                g = S.sharq_linear(act["gate_up"], weights["gate_up"], out=y["gate_up"], stream=stream)
+                mark(8)
+                S.sharq_prepare_silu_mul(g[:, :I], g[:, I:], 2, 4, "mx", out=act["down"], stream=stream)
+                mark(9)
+                S.sharq_linear(act["down"], weights["down"], out=y["down"], stream=stream)
+                mark(10)
+
+            ms_step, _, tm = run_steps(torch, stream, step, len(LAYER_OPS), args.steps, args.warmup)
+            ops = {f"{n}_us": tm.op_ms(i) * 1e3 for i, n in enumerate(LAYER_OPS)}
+            flops, nbytes = attention_work(seqs, new, length, fmt)
+            t = ops["attention_us"] * 1e-6
+            ops["attention_TFLOPs"], ops["attention_GBps"] = flops / t / 1e12, nbytes / t / 1e9
+            log(f"[bench] layer, {what}, {fmt} cache: {ms_step:.4f} ms/step: "
+                + ", ".join(f"{k} {v:.1f}" for k, v in ops.items()))
+            out = base_record(args, "Llama-8B decoder layer tokens/s (SharQ linears, paged attention)",
+                              T / (ms_step * 1e-3), "tokens/s", ms_step, "mxfp4",
+                              {"workload": f"one Llama-3.1-8B decoder layer, {what}; linears MXFP4 2:4, bf16 out; "
+                                           f"key/value cache {fmt}, pages of {LAYER_PAGE}", "tokens": T,
+                               "seq_len": length, "cache": fmt})
+            out["ops"] = ops
+            yield out
+
+
 ABLATION_MODES = ["sharq", "sparse", "dense", "dense_dense", "sparse_sparse"]
 MODE_PATHS = {"sharq": 2, "sparse": 1, "dense": 1, "dense_dense": 2, "sparse_sparse": 2}
 
@@ -887,7 +991,7 @@ def main():
                          "clocks (the step time over the warmup is reported by tenths)")
     ap.add_argument("--workload", default="llama-prefill",
                     choices=["llama-prefill", "llama-decode", "qwen-nvfp4", "llama-nvfp4-pairs", "moe",
-                             "ablation", "llama-fused"])
+                             "ablation", "llama-fused", "llama-layer"])
     ap.add_argument("--no-cpu-baseline", action="store_true")
     ap.add_argument("--backbone", default="dense-only", choices=["dense-only", "both", "compressed"],
                     help="prefill and the NVFP4 workloads: how the preparation stores the backbone for the "
@@ -929,6 +1033,9 @@ def main():
         print(json.dumps(llama_nvfp4_pairs(args, torch, S, synth, dev, stream)), flush=True)
     elif args.workload == "llama-fused":
         print(json.dumps(llama_fused(args, torch, S, synth, dev, stream)), flush=True)
+    elif args.workload == "llama-layer":
+        for o in llama_layer(args, torch, S, synth, dev, stream):
+            print(json.dumps(o), flush=True)
     elif args.workload == "ablation":
         for o in ablation(args, torch, S, synth, dev, stream):
             print(json.dumps(o), flush=True)

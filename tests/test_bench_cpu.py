@@ -55,3 +55,12 @@ def test_warmup_tenths():
     assert bench.tenths([1.0, 3.0, 5.0]) == [1.0, 3.0, 5.0]
     t = bench.tenths(list(range(200)))
     assert len(t) == 10 and t[0] == 9.5 and t[-1] == 189.5
+
+
+def test_attention_work():
+    hq, hkv, D = bench.LAYER_HEADS
+    # a whole prompt of 3: 1 + 2 + 3 pairs; keys, values, queries and outputs in bf16
+    assert bench.attention_work(1, 3, 3, "bf16") == (4.0 * D * hq * 6, 3 * hq * D * 4.0 + 2.0 * 3 * hkv * D * 2)
+    # two single tokens over 10: MXFP4 holds a value in 17 / 32 bytes
+    assert bench.attention_work(2, 1, 10, "mx") == (4.0 * D * hq * 20,
+                                                    2 * (hq * D * 4.0 + 2.0 * 10 * hkv * D * 17 / 32))

@@ -374,3 +374,40 @@ def test_a_sequence_served_step_by_step(fmt):
     check(q, cache, whole, offsets, lens, table.cpu().numpy(), torch.cat(got), torch.cat(lses))
     lse = torch.empty((n, hq), device=DEV)
     check(q, cache, whole, offsets, lens, table.cpu().numpy(), S.sharq_attention(q, cache, whole, lse=lse), lse)
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("seqs,new,length", [(1, 130, 130), (5, 1, 300)])
+def test_between_the_linears_of_a_layer(seqs, new, length, fmt):
+    """qkv linear, append, attention and the o projection's preparation, each on the output of the one before: the
+    append on slices of the linear's output, the attention against the definition on what was appended, and the
+    preparation byte by byte as on a copy of the attention's output."""
+    hq, hkv, D, page, H = 8, 2, 64, 16, 256
+    rng = np.random.default_rng(seqs)
+    batch, offsets, lens, table, pages = make_batch([new] * seqs, [length] * seqs, page)
+    cache = filled_cache(pages, page, hkv, D, fmt)
+    rows = batch.rows
+    h = R.bf16(rng.standard_normal((rows, H))).to(DEV)
+    w = S.sharq_quantize_weight(R.bf16(rng.standard_normal(((hq + 2 * hkv) * D, H)) * 0.05).to(DEV))
+    gamma = R.bf16(1 + 0.1 * rng.standard_normal(H)).to(DEV)
+    cos, sin = np_tables(length, D)
+    act, z = S.sharq_prepare_linear(h, gamma, w, 1e-5)
+    qw, kw = hq * D, (hq + hkv) * D
+    q = S.sharq_kv_append(z[:, :qw], z[:, qw:kw], z[:, kw:], cache, batch, torch.from_numpy(cos).to(DEV),
+                          torch.from_numpy(sin).to(DEV))
+    lse = torch.empty((rows, hq), device=DEV)
+    a = S.sharq_attention(q, cache, batch, lse=lse)
+    p = S.sharq_prepare(a, None)
+    p2 = S.sharq_prepare(a.clone(), None)
+    torch.cuda.synchronize()
+    zs = z.float().cpu().numpy().reshape(rows, -1, D)
+    seq, pos = R.positions(offsets, lens, rows)
+    y = R.rotate32(zs[:, :hq + hkv], cos[pos], sin[pos])
+    assert np.array_equal(q.float().cpu().numpy(), R.bf16(y[:, :hq].reshape(rows, -1)).float().numpy())
+    k, v = S.sharq_kv_read(cache, batch)
+    for got, src in ((k, y[:, hq:]), (v, zs[:, hq + hkv:])):
+        val = R.bf16(src).double().numpy() if fmt == "bf16" else R.mx_values(*R.mx_quantize(src))
+        assert np.array_equal(got.double().cpu().numpy(), val.reshape(rows, -1))
+    check(q, cache, batch, offsets, lens, table, a, lse)
+    for name in ("sp_codes", "sp_meta", "sp_scale", "dn_codes", "dn_scale"):
+        assert torch.equal(getattr(p, name), getattr(p2, name))
