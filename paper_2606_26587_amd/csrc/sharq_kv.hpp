@@ -109,7 +109,12 @@ constexpr AttnPlan attn_plan(int64_t seqs, int64_t rows, int64_t max_rows, int64
   if (p.few) {
     const int tok = mx ? 64 : 32;
     const int64_t kv = part > 0 ? ceil_div(part, tok) + (part < own ? 1 : 0) + ceil_div(s, tok) : 0;
-    p.own = attn_split(1, seqs * heads, kv, p.shared ? 512 : 2048, 4);
+    // One round of workgroups (2 or, of the leanest kernel, 3 a CU) where a wavefront has few turns of its tiles, four
+    // where it has many: then what sequences of different lengths leave idle counts for more than starting up.  Single
+    // tokens, 8 heads of 128, bf16, one round against four: 8 x 8191 tokens 44.8 and 47.2 us, 64 x 1000 40.3 and 45.1,
+    // 64 x 4000 135 and 124, 24 x 32768 502 and 420.  Beside a shared prefix's workgroups: one round.
+    const int64_t units = seqs * heads, turns = units * ceil_div(kv, 4);
+    p.own = attn_split(1, units, kv, p.shared ? 512 : turns >= 6144 ? 2048 : mx && p.few == 1 ? 768 : 512, 4);
   } else {
     // no sequence has more than max_rows rows, and all together have no more than rows
     const int64_t most = seqs * ceil_div(r, kAttnRows), packed = rows * group / kAttnRows + seqs;
