@@ -41,7 +41,7 @@ __device__ __forceinline__ bool find_tile(const KvBatchArgs& b, int group, int u
     const int s = s0 + lane;
     SeqRows r{0, 0, 0};
     if (s < b.seqs) r = seq_rows(b, s);
-    const int n = (int)(((int64_t)r.n * group + kRowsA - 1) / kRowsA);
+    const int n = (r.n * group + kRowsA - 1) / kRowsA;
     int sum = n;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
@@ -81,6 +81,7 @@ __device__ __forceinline__ void attn_rows(const AttnArgs& a, int block, int tile
   const int head = block % a.c.heads;
   const int uc = block / a.c.heads, chunk = uc / tiles, unit = tiles - 1 - uc % tiles;
   const int rr = wave * 32 + (lane & 31);
+  const unsigned group = (unsigned)a.group;   // rows times heads of a call fit 27 bits
   int seq = 0, rows, row_g, qh, p;                  // of this lane: row of the call, query head, position
   int p_lo, p_hi, w_lo, w_hi, t0, t1;               // positions of the workgroup's and the wavefront's rows; tokens
   if (ALL) {
@@ -90,11 +91,11 @@ __device__ __forceinline__ void attn_rows(const AttnArgs& a, int block, int tile
     if (once && lane < a.b.seqs) mine = seq_rows(a.b, lane);
     const int all = once ? __builtin_amdgcn_readlane(mine.first + mine.n, a.b.seqs - 1)
                          : __builtin_amdgcn_readfirstlane(kv_clamp(a.b.offs[a.b.seqs], 0, a.b.rows));
-    const int64_t total = (int64_t)all * a.group, r0 = (int64_t)unit * kRowsA;
+    const int total = all * a.group, r0 = unit * kRowsA;
     if (r0 >= total) return;
-    rows = total - r0 < kRowsA ? (int)(total - r0) : kRowsA;
-    const int64_t r = r0 + (rr < rows ? rr : rows - 1);
-    row_g = (int)(r / a.group), qh = head * a.group + (int)(r % a.group);
+    rows = total - r0 < kRowsA ? total - r0 : kRowsA;
+    const unsigned r = (unsigned)(r0 + (rr < rows ? rr : rows - 1));
+    row_g = (int)(r / group), qh = head * a.group + (int)(r % group);
     // this lane's sequence: past those that end at or before its row, 64 of them at a time
     if (once) {
       const int end = lane < a.b.seqs ? mine.first + mine.n : 0x7FFFFFFF;
@@ -102,7 +103,7 @@ __device__ __forceinline__ void attn_rows(const AttnArgs& a, int block, int tile
       for (int i = 0; i < a.b.seqs; ++i) s += __builtin_amdgcn_readlane(end, i) <= row_g;
       p = row_g + __shfl(mine.len - mine.n - mine.first, s);
     } else {
-      const int last = (int)((r0 + rows - 1) / a.group), s0 = find_seq(a.b, (int)(r0 / a.group));
+      const int last = (int)((unsigned)(r0 + rows - 1) / group), s0 = find_seq(a.b, (int)((unsigned)r0 / group));
       int s = s0;
       for (int at = s0; at < a.b.seqs; at += 64) {
         const int end = at + lane < a.b.seqs ? a.b.offs[at + lane + 1] : 0x7FFFFFFF;
@@ -133,15 +134,15 @@ __device__ __forceinline__ void attn_rows(const AttnArgs& a, int block, int tile
     int tile;
     SeqRows sr;
     if (!find_tile(a.b, a.group, unit, seq, sr, tile)) return;
-    const int64_t r0 = (int64_t)tile * kRowsA, total = (int64_t)sr.n * a.group;
+    const int r0 = tile * kRowsA, total = sr.n * a.group;
     const int base = sr.len - sr.n;   // position of the sequence's first row
-    rows = total - r0 < kRowsA ? (int)(total - r0) : kRowsA;
-    const int64_t r = r0 + (rr < rows ? rr : rows - 1);
-    const int token = (int)(r / a.group);
-    row_g = sr.first + token, qh = head * a.group + (int)(r % a.group), p = base + token;
-    p_lo = base + (int)(r0 / a.group), p_hi = base + (int)((r0 + rows - 1) / a.group);
-    const int wr = wave * 32 < rows ? wave * 32 : rows - 1, we = wave * 32 + 31 < rows ? wave * 32 + 31 : rows - 1;
-    w_lo = base + (int)((r0 + wr) / a.group), w_hi = base + (int)((r0 + we) / a.group);
+    rows = total - r0 < kRowsA ? total - r0 : kRowsA;
+    const unsigned r = (unsigned)(r0 + (rr < rows ? rr : rows - 1));
+    const int token = (int)(r / group);
+    row_g = sr.first + token, qh = head * a.group + (int)(r % group), p = base + token;
+    const unsigned wr = wave * 32 < rows ? wave * 32 : rows - 1, we = wave * 32 + 31 < rows ? wave * 32 + 31 : rows - 1;
+    p_lo = base + (int)((unsigned)r0 / group), p_hi = base + (int)((unsigned)(r0 + rows - 1) / group);
+    w_lo = base + (int)((r0 + wr) / group), w_hi = base + (int)((r0 + we) / group);
     t0 = a.t0, t1 = sr.len;
   }
 
