@@ -85,50 +85,13 @@ __device__ __forceinline__ void attn_rows(const AttnArgs& a, int block, int tile
   int seq = 0, rows, row_g, qh, p;                  // of this lane: row of the call, query head, position
   int p_lo, p_hi, w_lo, w_hi, t0, t1;               // positions of the workgroup's and the wavefront's rows; tokens
   if (ALL) {
-    // up to 64 sequences are looked up in one trip: lane s holds sequence s
-    const bool once = a.b.seqs <= 64;
-    SeqRows mine{0, 0, 0};
-    if (once && lane < a.b.seqs) mine = seq_rows(a.b, lane);
-    const int all = once ? __builtin_amdgcn_readlane(mine.first + mine.n, a.b.seqs - 1)
-                         : __builtin_amdgcn_readfirstlane(kv_clamp(a.b.offs[a.b.seqs], 0, a.b.rows));
-    const int total = all * a.group, r0 = unit * kRowsA;
+    const int all = kv_clamp(a.b.offs[a.b.seqs], 0, a.b.rows), total = all * a.group, r0 = unit * kRowsA;
     if (r0 >= total) return;
     rows = total - r0 < kRowsA ? total - r0 : kRowsA;
     const unsigned r = (unsigned)(r0 + (rr < rows ? rr : rows - 1));
     row_g = (int)(r / group), qh = head * a.group + (int)(r % group);
-    // this lane's sequence: past those that end at or before its row, 64 of them at a time
-    if (once) {
-      const int end = lane < a.b.seqs ? mine.first + mine.n : 0x7FFFFFFF;
-      int s = 0;
-      for (int i = 0; i < a.b.seqs; ++i) s += __builtin_amdgcn_readlane(end, i) <= row_g;
-      p = row_g + __shfl(mine.len - mine.n - mine.first, s);
-    } else {
-      const int last = (int)((unsigned)(r0 + rows - 1) / group), s0 = find_seq(a.b, (int)((unsigned)r0 / group));
-      int s = s0;
-      for (int at = s0; at < a.b.seqs; at += 64) {
-        const int end = at + lane < a.b.seqs ? a.b.offs[at + lane + 1] : 0x7FFFFFFF;
-        for (int i = 0; i < 64; ++i) s += __builtin_amdgcn_readlane(end, i) <= row_g;
-        if (__builtin_amdgcn_readlane(end, 63) > last) break;
-      }
-      const SeqRows sr = seq_rows(a.b, s < a.b.seqs ? s : a.b.seqs - 1);
-      p = sr.len - sr.n + (row_g - sr.first);
-    }
-    int lo = p, hi = p;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-      const int u = __shfl_xor(lo, d), w = __shfl_xor(hi, d);
-      lo = u < lo ? u : lo, hi = w > hi ? w : hi;
-    }
-    w_lo = __builtin_amdgcn_readfirstlane(lo), w_hi = __builtin_amdgcn_readfirstlane(hi);
-    if (lane == 0) lds_p[wave] = lo, lds_p[4 + wave] = hi;
-    __syncthreads();
-    p_lo = __builtin_amdgcn_readfirstlane(lds_p[0]), p_hi = __builtin_amdgcn_readfirstlane(lds_p[4]);
-#pragma unroll
-    for (int i = 1; i < 4; ++i) {
-      const int u = __builtin_amdgcn_readfirstlane(lds_p[i]), w = __builtin_amdgcn_readfirstlane(lds_p[4 + i]);
-      p_lo = u < p_lo ? u : p_lo, p_hi = w > p_hi ? w : p_hi;
-    }
-    __syncthreads();
+    // Rows past the prefix see all of it, wherever they are.
+    p = p_lo = p_hi = w_lo = w_hi = a.prefix_len;
     t0 = 0, t1 = a.prefix_len;
   } else {
     int tile;
@@ -151,9 +114,41 @@ __device__ __forceinline__ void attn_rows(const AttnArgs& a, int block, int tile
     const uint16_t* qp = a.q + (int64_t)row_g * a.ldq + (int64_t)qh * D + 8 * half;
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) qf[i] = *reinterpret_cast<const v8bf*>(qp + 16 * i);
-    // here, once: the loop's own waits would count the tiles' loads among these
+  }
+  if (ALL) {   // unless a sequence has rows inside the prefix: then every lane looks for its row's sequence
+    bool inside = false;
+    for (int s = lane; s - lane < a.b.seqs; s += 64) {
+      SeqRows sr{0, 0, 0};
+      if (s < a.b.seqs) sr = seq_rows(a.b, s);
+      inside |= __any(sr.n > 0 && sr.len - sr.n < a.prefix_len);
+    }
+    if (inside) {
+      const int last = (int)((unsigned)(unit * kRowsA + rows - 1) / group);
+      int s = find_seq(a.b, (int)((unsigned)(unit * kRowsA) / group));   // of the first row
+      for (int at = s; at < a.b.seqs; at += 64) {   // past those that end at or before this lane's, 64 at a time
+        const int end = at + lane < a.b.seqs ? a.b.offs[at + lane + 1] : 0x7FFFFFFF;
+        for (int i = 0; i < 64; ++i) s += __builtin_amdgcn_readlane(end, i) <= row_g;
+        if (__builtin_amdgcn_readlane(end, 63) > last) break;
+      }
+      const SeqRows sr = seq_rows(a.b, s < a.b.seqs ? s : a.b.seqs - 1);
+      p = sr.len - sr.n + (row_g - sr.first);
+      int lo = p, hi = p;
 #pragma unroll
-    for (int i = 0; i < D / 16; ++i) asm volatile("" : "+v"(qf[i]));
+      for (int d = 1; d < 32; d <<= 1) {
+        const int u = __shfl_xor(lo, d), w = __shfl_xor(hi, d);
+        lo = u < lo ? u : lo, hi = w > hi ? w : hi;
+      }
+      w_lo = __builtin_amdgcn_readfirstlane(lo), w_hi = __builtin_amdgcn_readfirstlane(hi);
+      if (lane == 0) lds_p[wave] = lo, lds_p[4 + wave] = hi;
+      __syncthreads();
+      p_lo = __builtin_amdgcn_readfirstlane(lds_p[0]), p_hi = __builtin_amdgcn_readfirstlane(lds_p[4]);
+#pragma unroll
+      for (int i = 1; i < 4; ++i) {
+        const int u = __builtin_amdgcn_readfirstlane(lds_p[i]), w = __builtin_amdgcn_readfirstlane(lds_p[4 + i]);
+        p_lo = u < p_lo ? u : p_lo, p_hi = w > p_hi ? w : p_hi;
+      }
+      __syncthreads();
+    }
   }
   v16f o[kDT] = {};
   float m = kNoMax, l = 0.0f;
@@ -239,6 +234,9 @@ __device__ __forceinline__ void attn_rows(const AttnArgs& a, int block, int tile
   int at = row_of(page_of(first), first), next = page_of(first + 1);   // rows of this tile, pages of the next
   load(at, 0);
   store(0);
+  // the queries, here and once: the loop's own waits would count the tiles' loads among theirs
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i) asm volatile("" : "+v"(qf[i]));
   lds_load_wait();
   __syncthreads();
   auto step = [&](int ti, auto stage_c) {
