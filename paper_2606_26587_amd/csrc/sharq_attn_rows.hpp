@@ -165,16 +165,19 @@ __device__ __forceinline__ void attn_rows(const AttnArgs& a, int block, int tile
     return kv_row(page, kv_tile_start(span, t0, ti, kT) + lane, a.c.pages, a.c.heads, head, a.c.page_shift);
   };
   // A wavefront stages 16 tokens of a tile, which lie in one page: tiles start at multiples of 16.
-  constexpr int kI = MX ? 1 : kC / 4;   // 16-byte loads of a lane, keys or values
-  constexpr int kRowLanes = MX ? D / 32 : kC, kRowsLoad = 64 / kRowLanes;   // lanes of a row; rows of a load
-  uint4 kb, vb;        // MXFP4: the next tile's codes and scales on their way
-  uint32_t ke, ve;
-  uint32_t off[kI];    // bf16: this lane's place in the 16 tokens; the exchange of chunks is made here
+  constexpr int kI = kC / 4, kRowsLoad = 64 / kC;   // bf16: 16-byte loads of a lane, keys or values; rows of a load
+  uint32_t off[kI];   // this lane's place in the 16 tokens; the exchange of chunks is made here
 #pragma unroll
   for (int i = 0; i < kI; ++i) {
-    const int row = i * kRowsLoad + lane / kRowLanes;
-    off[i] = (uint32_t)(row * D * 2 + 16 * (MX ? 0 : kv_chunk<D>(row, lane % kRowLanes) - row * kC));
+    const int row = i * kRowsLoad + lane / kC;
+    off[i] = (uint32_t)(row * D * 2 + 16 * (kv_chunk<D>(row, lane % kC) - row * kC));
   }
+  // MXFP4: the next tile's codes and scales on their way, 32 values a lane: 16 tokens at one place of their rows, so
+  // that they go to LDS over all banks
+  uint4 kb, vb;
+  uint32_t ke, ve;
+  const int mx_row = lane & 15, mx_block = lane >> 4;
+  const bool mx_lane = mx_block < D / 32;
   auto load = [&](int at, int stage) {
     const unsigned mine = (unsigned)(__ballot(at >= 0) >> (16 * wave)) & 0xFFFFu;
     if (MX) {
@@ -185,18 +188,18 @@ __device__ __forceinline__ void attn_rows(const AttnArgs& a, int block, int tile
     const int l0 = 16 * wave + __builtin_ctz(mine);
     const int64_t row0 = __builtin_amdgcn_readlane(at, l0) - (l0 & 15);
     if (MX) {
-      const int row = lane / kRowLanes;   // D 64: rows past 15 are no lane's
-      if (row < 16 && ((mine >> row) & 1)) {
-        kb = *reinterpret_cast<const uint4*>(a.c.k + (row0 + row) * (D / 2) + 16 * (lane % kRowLanes));
-        vb = *reinterpret_cast<const uint4*>(a.c.v + (row0 + row) * (D / 2) + 16 * (lane % kRowLanes));
-        ke = a.c.ks[(row0 + row) * (D / 32) + lane % kRowLanes];
-        ve = a.c.vs[(row0 + row) * (D / 32) + lane % kRowLanes];
+      if (mx_lane && ((mine >> mx_row) & 1)) {
+        const int64_t block = (row0 + mx_row) * (D / 32) + mx_block;
+        kb = *reinterpret_cast<const uint4*>(a.c.k + block * 16);
+        vb = *reinterpret_cast<const uint4*>(a.c.v + block * 16);
+        ke = a.c.ks[block];
+        ve = a.c.vs[block];
       }
     } else {
       const uint8_t *kp = a.c.k + row0 * (D * 2), *vp = a.c.v + row0 * (D * 2);
 #pragma unroll
       for (int i = 0; i < kI; ++i)
-        if (mine == 0xFFFFu || ((mine >> (i * kRowsLoad + lane / kRowLanes)) & 1)) {
+        if (mine == 0xFFFFu || ((mine >> (i * kRowsLoad + lane / kC)) & 1)) {
           lds_load16(&lds[stage][0][wave * 16 * kC + i * 64], kp, off[i]);
           lds_load16(&lds[stage][1][wave * 16 * kC + i * 64], vp, off[i]);
         }
@@ -205,8 +208,8 @@ __device__ __forceinline__ void attn_rows(const AttnArgs& a, int block, int tile
   // What load() leaves out keeps its place in LDS: keys there are masked, values meet a weight of zero and must be
   // finite.  So the stages start as zeros, and only tokens that some row sees come after.
   auto store = [&](int stage) {
-    if (MX && lane / kRowLanes < 16) {
-      const int row = 16 * wave + lane / kRowLanes, c0 = 4 * (lane % kRowLanes);
+    if (MX && mx_lane) {
+      const int row = 16 * wave + mx_row, c0 = 4 * mx_block;
       const uint32_t kw[4] = {kb.x, kb.y, kb.z, kb.w}, vw[4] = {vb.x, vb.y, vb.z, vb.w};
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
