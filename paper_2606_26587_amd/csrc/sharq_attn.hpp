@@ -43,6 +43,15 @@ __device__ __forceinline__ int kv_chunk(int t, int c) {
   return t * kC + (c ^ f);
 }
 
+// The token of 16 that a lane (of each 16) writes to LDS from an MXFP4 cache:
+// 8 lanes in a row, which are written together, reach 8 different 16-byte places
+// of 128 bytes under kv_chunk's exchange.
+template <int D>
+__device__ __forceinline__ int mx_token(int lane) {
+  const int l = lane & 15;
+  return D == 128 ? (l & 1) | (l & 6) << 1 | (l & 8) >> 2 : (l & 7) << 1 | l >> 3;
+}
+
 // Transposing LDS read: a group of 16 lanes reads 4 rows of 16 values, lane i
 // giving the address of values 4 (i % 4) .. + 3 of row i / 4, and gets value i
 // of the 4 rows.

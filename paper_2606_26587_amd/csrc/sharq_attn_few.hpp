@@ -73,6 +73,7 @@ __device__ __forceinline__ void attn_few(const AttnArgs& a, int block, int chunk
     return ti < last && t < span.hi && (t >= span.low || t < a.sinks) ? token_page(a, seq, t) : -1;
   };
   uint4* const v_lds = lds[wave];
+  const int v_tok = mx_token<D>(lane);   // MXFP4: the token of 16 whose values this lane brings
   int v_at[kDT];   // this lane's reads of the values' tile; 16 tokens further on is a constant away
 #pragma unroll
   for (int d = 0; d < kDT; ++d)
@@ -100,16 +101,17 @@ __device__ __forceinline__ void attn_few(const AttnArgs& a, int block, int chunk
       if (MX) {
         const uint8_t *kp = a.c.k + row * (D / 2), *vp = a.c.v + row * (D / 2);
         const uint8_t *kse = a.c.ks + row * (D / 32), *vse = a.c.vs + row * (D / 32);
-        const uint32_t at16 = (uint32_t)(col * (D / 2) + g * (D / 8));   // token col, quarter g: keys and values alike
+        // a quarter g of a token: the operand's for the keys, for the values one that suits the LDS
+        const uint32_t ko = (uint32_t)(col * (D / 2) + g * (D / 8)), vo = (uint32_t)(v_tok * (D / 2) + g * (D / 8));
         if (D == 128) {
-          kb[i][0] = *reinterpret_cast<const uint4*>(kp + at16);
-          vb[i][0] = *reinterpret_cast<const uint4*>(vp + at16);
+          kb[i][0] = *reinterpret_cast<const uint4*>(kp + ko);
+          vb[i][0] = *reinterpret_cast<const uint4*>(vp + vo);
         } else {
-          const uint2 x = *reinterpret_cast<const uint2*>(kp + at16), y = *reinterpret_cast<const uint2*>(vp + at16);
+          const uint2 x = *reinterpret_cast<const uint2*>(kp + ko), y = *reinterpret_cast<const uint2*>(vp + vo);
           kb[i][0] = make_uint4(x.x, x.y, 0, 0), vb[i][0] = make_uint4(y.x, y.y, 0, 0);
         }
         ke[i] = kse[(uint32_t)(col * (D / 32) + g * (D / 32) / 4)];
-        ve[i] = vse[(uint32_t)(col * (D / 32) + g * (D / 32) / 4)];
+        ve[i] = vse[(uint32_t)(v_tok * (D / 32) + g * (D / 32) / 4)];
       } else {
         const uint8_t *kp = a.c.k + row * (D * 2), *vp = a.c.v + row * (D * 2);
 #pragma unroll
@@ -142,7 +144,7 @@ __device__ __forceinline__ void attn_few(const AttnArgs& a, int block, int chunk
         const int i = 2 * u + mt;
         const unsigned mine = (unsigned)(live >> (16 * i)) & 0xFFFFu;
         if (MX) {
-          const int t = col, c0 = g * (D / 32);   // 16 tokens at one chunk: all banks
+          const int t = v_tok, c0 = g * (D / 32);
           const uint32_t w[4] = {vb[i][0].x, vb[i][0].y, vb[i][0].z, vb[i][0].w};
           const bool dead = !((mine >> t) & 1);
 #pragma unroll

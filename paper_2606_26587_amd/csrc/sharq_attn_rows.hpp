@@ -176,7 +176,7 @@ __device__ __forceinline__ void attn_rows(const AttnArgs& a, int block, int tile
   // that they go to LDS over all banks
   uint4 kb, vb;
   uint32_t ke, ve;
-  const int mx_row = lane & 15, mx_block = lane >> 4;
+  const int mx_row = mx_token<D>(lane), mx_block = lane >> 4;
   const bool mx_lane = mx_block < D / 32;
   auto load = [&](int at, int stage) {
     const unsigned mine = (unsigned)(__ballot(at >= 0) >> (16 * wave)) & 0xFFFFu;
