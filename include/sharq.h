@@ -7,11 +7,14 @@
  * residual taken against the *dequantized* backbone, then summing two FP4
  * GEMMs that read one shared FP4 weight payload (Sec. 3.3 eqs.
  * "sharq-sparse-backbone", "sharq-quantized-backbone", "sharq-residual",
- * "sharq-output"; Sec. 3.4).
+ * "sharq-output"; Sec. 3.4).  Between a decoder layer's qkv linear and its o
+ * linear stand a paged key/value cache, in bf16 or in the library's MXFP4, and
+ * the attention that reads it (sharq_kv_append, sharq_kv_read, sharq_attention).
  *
  * Conventions for every entry point
  *   - Tensor pointers are DEVICE pointers owned by the caller; the library
- *     allocates nothing, keeps no global state and never synchronizes.
+ *     allocates nothing, keeps no global state and never synchronizes.  The one
+ *     call that needs scratch memory, sharq_attention, takes it as an argument.
  *   - `stream` is a hipStream_t passed as void* (NULL = the default stream);
  *     all work is enqueued asynchronously on it.
  *   - Errors are returned, never thrown.  Arguments are validated before any

@@ -16,6 +16,8 @@ __global__ __launch_bounds__(256, 2) void k_attn_few(AttnArgs a, int chunk_tiles
 // workgroup share one item's many slots.  Eight slots' states and outputs are on
 // their way together (what a slot that saw nothing left unwritten is read and
 // dropped).  Sums are formed in a fixed order: the same call gives the same bits.
+// 32 items of 64 slots: 3.6 us (7.0 with a slot's output read only once its state
+// had come); 2048 items of 17 slots: 6.2 us, 8.8 MB of states and outputs.
 template <int D, bool WIDE>
 __global__ __launch_bounds__(256) void k_attn_merge(AttnArgs a) {
   constexpr int kPer = D / 4, kG = 256 / kPer, kTrip = 8;
@@ -99,6 +101,8 @@ hipError_t launch_attn_few(const AttnArgs& a, int D, bool mx, const AttnPlan& pl
   return hipGetLastError();
 }
 
+// Many items fill the chip with a group each: with 8 or 9 slots, 12000 items took
+// 31 us wide and 6 us otherwise; 32 items of 64 slots are the other end.
 constexpr int64_t kWideItems = 1024;
 
 template <int D>

@@ -20,6 +20,25 @@
 //
 // P is rounded to bf16 for the second product (V is bf16, and so is the output);
 // m, l, o and the sum of P stay in fp32.
+//
+// A workgroup holds 128 rows, 32 a wavefront (o 64, q 32, S^T 32 registers of 256:
+// two wavefronts a SIMD, of two workgroups that run apart, so one's exponentials
+// can run beside the other's products), and walks tiles of 64 tokens in two LDS
+// stages: while one is worked on, the next is on its way, bf16 straight from
+// global memory to LDS, MXFP4 through registers, where it becomes bf16 once for
+// all rows.  Rows of consecutive tokens share the tiles: with 4 query heads a
+// key/value head a tile is 32 tokens, so little of a causal or windowed tile is
+// masked, and masks are formed only in tiles that need one.
+//
+// Measured (8192 tokens, 32 query and 8 key/value heads of 128, causal): 537 us,
+// 1.02 PFLOP/s, 0.84 of what a library bf16 product of 8192^3 reaches on the same
+// card.  The matrix cores are busy half of the cycles and so is the VALU; what
+// bounds it is power: on zeros the same launch takes 424 us.  Tiles of 32 tokens
+// with three wavefronts a SIMD (586 us), the first half's exponentials beside the
+// second half's products (544, and with the maximum left out 546 against 540),
+// halves of masked tiles skipped (571) and raised priority around the products
+// (550) were measured and not kept.  Heads of 64: 830 TFLOP/s, the exponentials
+// weigh twice as much; an MXFP4 cache costs 5 to 10% here.
 
 #pragma once
 

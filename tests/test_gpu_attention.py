@@ -411,3 +411,17 @@ def test_between_the_linears_of_a_layer(seqs, new, length, fmt):
     check(q, cache, batch, offsets, lens, table, a, lse)
     for name in ("sp_codes", "sp_meta", "sp_scale", "dn_codes", "dn_scale"):
         assert torch.equal(getattr(p, name), getattr(p2, name))
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("per,lens", [([1, 2], [40, 20]), ([60], [60])])
+def test_pool_without_pages(per, lens, fmt):
+    batch, offsets, ln, table, pages = make_batch(per, lens, 16)
+    cache = S.alloc_kv_cache(0, 16, 2, 128, fmt, DEV)
+    x = torch.randn((batch.rows, 256), device=DEV).to(torch.bfloat16)
+    assert torch.equal(S.sharq_kv_append(x, x, x, cache, batch), x)
+    k, v = S.sharq_kv_read(cache, batch)
+    assert not k.any() and not v.any()
+    lse = torch.zeros((batch.rows, 2), device=DEV)
+    out = S.sharq_attention(x, cache, batch, lse=lse)
+    assert not out.any() and torch.isneginf(lse).all()

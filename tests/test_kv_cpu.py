@@ -27,6 +27,17 @@ int span(int t0, int t1, int p_lo, int p_hi, int window, int sinks, int T, int* 
   for (int i = 0; i < s.n && i < most; ++i) start[i] = kv_tile_start(s, t0, i, T);
   return s.n;
 }
+// {few, shared, own tiles, chunks, tiles of a chunk, prefix ..., slots}; workspace bytes
+int64_t plan(int64_t seqs, int64_t rows, int64_t max_rows, int64_t max_len, int heads, int group, int D, int mx,
+             int64_t window, int64_t sinks, int64_t prefix, int64_t* out) {
+  const AttnPlan p = attn_plan(seqs, rows, max_rows, max_len, heads, group, D, mx, window, sinks, prefix);
+  const int64_t v[] = {p.few, p.shared, p.own.tiles, p.own.chunks, p.own.chunk_tiles, p.prefix.tiles, p.prefix.chunks,
+                       p.prefix.chunk_tiles, p.slots};
+  for (int i = 0; i < 9; ++i) out[i] = v[i];
+  return attn_workspace(rows * heads * group, p.slots, D);
+}
+int tile_rows() { return kAttnRows; }
+int tile_tokens() { return kAttnTile; }
 }
 """
 
@@ -99,6 +110,65 @@ def test_span_at_the_ends_of_the_range(kv):
     assert kv.span(0, 2 ** 30, 2 ** 30 - 1, 2 ** 30 - 1, 1, 0, 64, start, rg, 4) == 1 and start[0] == 2 ** 30 - 64
     assert kv.span(0, 0, -5, -1, 1, 7, 64, start, rg, 4) == 0
     assert kv.span(0, 5, -2 ** 31 + 8, -1, big, big, 64, start, rg, 4) == 0
+
+
+def test_plans_cover_every_tile_of_every_row(kv):
+    """Whatever the sequences within the batch's bounds, the plan's workgroups take all tiles of tokens that any tile of
+    rows sees, have a tile of rows each, and fit the workspace."""
+    kv.plan.restype = ctypes.c_int64
+    kv.plan.argtypes = [ctypes.c_int64] * 4 + [ctypes.c_int] * 4 + [ctypes.c_int64] * 3 + [ctypes.POINTER(ctypes.c_int64)]
+    R, T = kv.tile_rows(), kv.tile_tokens()
+    rng = np.random.default_rng(11)
+    start, rg, out = (ctypes.c_int * 1)(), (ctypes.c_int * 2)(), (ctypes.c_int64 * 9)()
+    big = 2 ** 31 - 1
+
+    def tiles(t0, length, p_lo, p_hi, window, sinks, tok):
+        return kv.span(t0, length, p_lo, p_hi, window, sinks, tok, start, rg, 0)
+
+    kinds = set()
+    for _ in range(1500):
+        seqs = int(rng.integers(1, 40))
+        most = int(rng.choice([1, 2, 4, 9, 40, 300, 2000]))
+        n = rng.integers(0, most + 1, seqs)
+        n[int(rng.integers(seqs))] = most
+        lens = np.maximum(n + rng.integers(0, int(rng.choice([2, 100, 5000])), seqs), 0)
+        max_len = int(lens.max()) + int(rng.choice([0, 0, 17, 3000]))
+        rows = int(n.sum()) + int(rng.integers(0, 5))
+        max_rows = most + int(rng.choice([0, 0, 3, 100]))
+        heads, group = [(8, 4), (4, 7), (1, 1), (2, 16), (1, 128), (4, 8), (3, 3)][int(rng.integers(7))]
+        D, mx = int(rng.choice([64, 128])), int(rng.integers(2))
+        window = int(rng.choice([big, big, 1, 16, 100, 1000]))
+        sinks = int(rng.choice([0, 1, 4, 64, 300, big]))
+        prefix = int(rng.choice([0, 0, 16, 256, 1024]))
+        prefix = prefix if prefix <= max_len else 0
+        size = kv.plan(seqs, rows, max_rows, max_len, heads, group, D, mx, window, sinks, prefix, out)
+        few, shared, own_tiles, own_chunks, own_each, pre_tiles, pre_chunks, pre_each, slots = out
+        kinds.add((few, shared, slots > 0))
+        assert own_chunks >= 1 and own_each >= 1 and own_chunks * own_tiles * heads < 2 ** 23
+        assert slots == (own_chunks + pre_chunks if shared else own_chunks if own_chunks > 1 else 0)
+        assert size == (0 if slots == 0 else -(-rows * heads * group * slots * 8 // 16) * 16
+                        + rows * heads * group * slots * D * 4)
+        t0 = prefix if shared else 0
+        used = 0
+        for i in range(seqs):
+            base = int(lens[i] - n[i])
+            if few:
+                assert n[i] * group <= 16 * few
+                if n[i]:
+                    tok = 64 if mx else 32
+                    assert tiles(t0, int(lens[i]), base, int(lens[i]) - 1, window, sinks, tok) <= own_chunks * own_each
+                continue
+            all_rows = int(n[i]) * group
+            for r0 in range(0, all_rows, R):
+                last = min(all_rows, r0 + R) - 1
+                used += 1
+                got = tiles(t0, int(lens[i]), base + r0 // group, base + last // group, window, sinks, T)
+                assert got <= own_chunks * own_each
+        assert few or used <= own_tiles
+        if shared:
+            assert window >= max_len and pre_tiles * R >= int(n.sum()) * group
+            assert -(-prefix // T) <= pre_chunks * pre_each
+    assert {k[0] for k in kinds} == {0, 1, 2, 4} and {k[1:] for k in kinds} == {(0, False), (0, True), (1, True)}
 
 
 # ---------------------------------------------------------------------------
