@@ -101,7 +101,7 @@ constexpr AttnPlan attn_plan(int64_t seqs, int64_t rows, int64_t max_rows, int64
   // a window leaves little of a prefix, and rows that see different parts of it
   p.shared = prefix_len > 0 && window >= max_len;
   const int64_t r = max_rows * group, own = max_len - (p.shared ? prefix_len : 0);
-  p.few = r <= 16 ? 1 : r <= 32 ? 2 : r <= 64 && D == 64 ? 4 : 0;   // (heads of 128: 64 rows' states fill the registers)
+  p.few = r <= 16 ? 1 : r <= 32 ? 2 : r <= 64 && D == 64 ? 4 : 0;   // (64 rows' states over heads of 128 fill the registers)
   // tokens that a tile of rows sees at most: its window and its own positions, and the sinks
   const int64_t span = p.few ? max_rows : kAttnRows / group + 2;
   const int64_t w = window < max_len ? window + span : own, part = w < own ? w : own;
@@ -109,12 +109,14 @@ constexpr AttnPlan attn_plan(int64_t seqs, int64_t rows, int64_t max_rows, int64
   if (p.few) {
     const int tok = mx ? 64 : 32;
     const int64_t kv = part > 0 ? ceil_div(part, tok) + (part < own ? 1 : 0) + ceil_div(s, tok) : 0;
-    // One round of workgroups (2 or, of the leanest kernel, 3 a CU) where a wavefront has few turns of its tiles, four
-    // where it has many: then what sequences of different lengths leave idle counts for more than starting up.  Single
-    // tokens, 8 heads of 128, bf16, one round against four: 8 x 8191 tokens 44.8 and 47.2 us, 64 x 1000 40.3 and 45.1,
-    // 64 x 4000 135 and 124, 24 x 32768 502 and 420.  Beside a shared prefix's workgroups: one round.
+    // One round of workgroups where a wavefront has few turns of its tiles.  Where it has many, and the kernel's states
+    // leave room for three workgroups a CU, four rounds: then what sequences of different lengths leave idle counts for
+    // more than starting up and joining.  One round against four, 8 heads: single tokens in bf16, 8 x 8191 44.8 and
+    // 47.2 us, 64 x 1000 40.3 and 45.1, 64 x 4000 135 and 124, 24 x 32768 502 and 420; 5 tokens a sequence, 20 rows,
+    // over 16 x 16000: heads of 64 98.8 and 82.6, of 128 146 and 158.  Beside a shared prefix's workgroups: one round.
+    const bool lean = p.few == 1 || (p.few == 2 && D == 64);
     const int64_t units = seqs * heads, turns = units * ceil_div(kv, 4);
-    p.own = attn_split(1, units, kv, p.shared ? 512 : turns >= 6144 ? 2048 : mx && p.few == 1 ? 768 : 512, 4);
+    p.own = attn_split(1, units, kv, p.shared ? 512 : lean && turns >= 6144 ? 2048 : mx && p.few == 1 ? 768 : 512, 4);
   } else {
     // no sequence has more than max_rows rows, and all together have no more than rows
     const int64_t most = seqs * ceil_div(r, kAttnRows), packed = rows * group / kAttnRows + seqs;
