@@ -9,6 +9,7 @@ there is no fallback path.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from dataclasses import dataclass
 from typing import Optional, Sequence
@@ -526,6 +527,12 @@ def sharq_kv_read(cache: KVCache, batch: KVBatch, k_out: Optional[torch.Tensor] 
     return k_out, v_out
 
 
+@functools.lru_cache(maxsize=64)
+def _attn_ref(scale: float, window: int, sinks: int):
+    """A reference to the C structure of a call without a shared prefix: a layer's are always the same."""
+    return ctypes.byref(AttnStruct(scale, window, sinks, None, 0))
+
+
 def attention_workspace_bytes(cache: KVCache, batch: KVBatch, q_heads: int, window: int = 0, sinks: int = 0,
                               prefix_len: int = 0) -> int:
     """Bytes of workspace of sharq_attention for these sizes."""
@@ -558,10 +565,15 @@ def sharq_attention(q: torch.Tensor, cache: KVCache, batch: KVBatch, scale: Opti
                                      or prefix_table.numel() * cache.page_size < prefix_len
                                      or prefix_table.get_device() != dev):
         raise SharqError(EINVAL, where)
-    ts = AttnStruct(cache.head_dim ** -0.5 if scale is None else scale, window, sinks, _ptr(prefix_table), prefix_len)
+    if scale is None:
+        scale = cache.head_dim ** -0.5
+    if prefix_len or prefix_table is not None:
+        ts = ctypes.byref(AttnStruct(scale, window, sinks, _ptr(prefix_table), prefix_len))
+    else:
+        ts = _attn_ref(scale, window, sinks)
     size = 0
     if workspace is None:
-        size = lib.sharq_attention_workspace_bytes(cache.ref, batch.ref, ctypes.byref(ts), heads)
+        size = lib.sharq_attention_workspace_bytes(cache.ref, batch.ref, ts, heads)
         if size:   # on the stream that uses it: freed on return, and taken again only behind the call
             with torch.cuda.stream(stream):
                 workspace = torch.empty(size, dtype=torch.uint8, device=q.device)
@@ -569,8 +581,10 @@ def sharq_attention(q: torch.Tensor, cache: KVCache, batch: KVBatch, scale: Opti
         raise SharqError(EINVAL, where)
     else:
         size = workspace.nbytes
-    _check(lib.sharq_attention(q.data_ptr(), BF16, heads, ldq, cache.ref, batch.ref, ctypes.byref(ts), out.data_ptr(),
-                               ldo, _ptr(lse), _ptr(workspace), size, _stream(stream)), where)
+    status = lib.sharq_attention(q.data_ptr(), BF16, heads, ldq, cache.ref, batch.ref, ts, out.data_ptr(), ldo,
+                                 _ptr(lse), _ptr(workspace), size, _stream(stream))
+    if status:
+        raise SharqError(status, where)
     return out
 
 
