@@ -78,8 +78,13 @@ sharq::KvCacheArgs cache_args(const sharq_kv_cache* c) {
           c->kv_heads, __builtin_ctz((unsigned)c->page_size)};
 }
 
-sharq::KvBatchArgs batch_args(const sharq_kv_batch* b) {
-  return {b->row_offsets, b->lens, b->page_table, b->ld_table, (int)b->seqs, (int)b->rows, (int)b->max_len};
+sharq::KvBatchArgs batch_args(const sharq_kv_batch* b, int64_t rows) {
+  return {b->row_offsets, b->lens, b->page_table, b->ld_table, (int)b->seqs, (int)rows, (int)b->max_len};
+}
+
+// Rows that sequences can own: those behind are padding, which the attention keeps no partial results of.
+int64_t owned_rows(const sharq_kv_batch* b) {
+  return b->max_rows < b->rows && b->seqs * b->max_rows < b->rows ? b->seqs * b->max_rows : b->rows;
 }
 
 sharq_status check_attn(const sharq_attn* t, const sharq_kv_cache* c, const sharq_kv_batch* b, int64_t q_heads,
@@ -99,8 +104,8 @@ int attn_window(const sharq_attn* t) { return t->window == 0 || t->window > INT_
 int attn_sinks(const sharq_attn* t) { return t->sinks > INT_MAX ? INT_MAX : (int)t->sinks; }
 
 sharq::AttnPlan plan_of(const sharq_kv_cache* c, const sharq_kv_batch* b, const sharq_attn* t, int64_t q_heads) {
-  return sharq::attn_plan(b->seqs, b->rows, b->max_rows, b->max_len, c->kv_heads, (int)(q_heads / c->kv_heads), c->head_dim,
-                          c->fmt == SHARQ_KV_MXFP4, attn_window(t), attn_sinks(t), t->prefix_len);
+  return sharq::attn_plan(b->seqs, owned_rows(b), b->max_rows, b->max_len, c->kv_heads, (int)(q_heads / c->kv_heads),
+                          c->head_dim, c->fmt == SHARQ_KV_MXFP4, attn_window(t), attn_sinks(t), t->prefix_len);
 }
 
 }  // namespace
@@ -138,8 +143,8 @@ sharq_status sharq_kv_append(const void* Q, const void* K, const void* V, sharq_
   return hip_status(sharq::launch_kv_append(
       static_cast<const uint16_t*>(Q), static_cast<const uint16_t*>(K), static_cast<const uint16_t*>(V), ldq, ldk, ldv,
       (int)q_heads, static_cast<uint16_t*>(Q_out), ldqo, cos, sin, (int)angles, positions,
-      cache->scale_rule == SHARQ_SCALE_CEIL ? sharq::kE8Ceil : sharq::kE8Floor, batch_args(batch), cache_args(cache),
-      (int)D, cache->fmt == SHARQ_KV_MXFP4, reinterpret_cast<hipStream_t>(stream)));
+      cache->scale_rule == SHARQ_SCALE_CEIL ? sharq::kE8Ceil : sharq::kE8Floor, batch_args(batch, batch->rows),
+      cache_args(cache), (int)D, cache->fmt == SHARQ_KV_MXFP4, reinterpret_cast<hipStream_t>(stream)));
 }
 
 sharq_status sharq_kv_read(const sharq_kv_cache* cache, const sharq_kv_batch* batch, void* K, int64_t ldk, void* V,
@@ -155,7 +160,7 @@ sharq_status sharq_kv_read(const sharq_kv_cache* cache, const sharq_kv_batch* ba
   if (!K || !V) return SHARQ_EINVAL;
   if (!row_aligned(K, ldk) || !row_aligned(V, ldv)) return SHARQ_EALIGN;
   return hip_status(sharq::launch_kv_read(static_cast<uint16_t*>(K), ldk, static_cast<uint16_t*>(V), ldv,
-                                          batch_args(batch), cache_args(cache), cache->head_dim,
+                                          batch_args(batch, batch->rows), cache_args(cache), cache->head_dim,
                                           cache->fmt == SHARQ_KV_MXFP4, reinterpret_cast<hipStream_t>(stream)));
 }
 
@@ -165,7 +170,7 @@ size_t sharq_attention_workspace_bytes(const sharq_kv_cache* cache, const sharq_
       check_attn(attn, cache, batch, q_heads, false) != SHARQ_OK)
     return 0;
   if (batch->rows == 0 || batch->seqs == 0 || batch->max_rows == 0) return 0;
-  return (size_t)sharq::attn_workspace(batch->rows * q_heads, plan_of(cache, batch, attn, q_heads).slots,
+  return (size_t)sharq::attn_workspace(owned_rows(batch) * q_heads, plan_of(cache, batch, attn, q_heads).slots,
                                        cache->head_dim);
 }
 
@@ -185,12 +190,12 @@ sharq_status sharq_attention(const void* Q, sharq_dtype xdt, int64_t q_heads, in
   if (!Q || !O) return SHARQ_EINVAL;
   if (!row_aligned(Q, ldq) || !row_aligned(O, ldo) || !aligned(lse, 4) || !aligned(workspace, 16)) return SHARQ_EALIGN;
   const sharq::AttnPlan plan = plan_of(cache, batch, attn, q_heads);
-  const size_t need = (size_t)sharq::attn_workspace(batch->rows * q_heads, plan.slots, (int)D);
+  const size_t need = (size_t)sharq::attn_workspace(owned_rows(batch) * q_heads, plan.slots, (int)D);
   if (need > 0 && (!workspace || workspace_bytes < need)) return SHARQ_EINVAL;
   return hip_status(sharq::launch_attention(
-      static_cast<const uint16_t*>(Q), ldq, static_cast<uint16_t*>(O), ldo, lse, batch_args(batch), cache_args(cache),
-      plan, attn->prefix_table, (int)attn->prefix_len, (int)q_heads, (int)D, cache->fmt == SHARQ_KV_MXFP4,
-      attn_window(attn), attn_sinks(attn), attn->scale, workspace, reinterpret_cast<hipStream_t>(stream)));
+      static_cast<const uint16_t*>(Q), ldq, static_cast<uint16_t*>(O), ldo, lse, batch_args(batch, owned_rows(batch)),
+      cache_args(cache), plan, attn->prefix_table, (int)attn->prefix_len, (int)q_heads, (int)D,
+      cache->fmt == SHARQ_KV_MXFP4, attn_window(attn), attn_sinks(attn), attn->scale, workspace, reinterpret_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -235,6 +235,31 @@ def test_loose_bounds_of_the_batch(per, lens, fmt):
 
 
 @pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("per,lens,prefix", [([1], [3000], 0), ([1, 1], [900, 1500], 256), ([5, 2], [3000, 40], 0),
+                                             ([200], [1500], 0)])
+def test_many_padding_rows(per, lens, prefix, fmt):
+    """More rows than the sequences can own: the workspace is that of the call without them, and they stay as they are."""
+    batch, offsets, ln, table, cache, q = setup(per, lens, 16, 4, 2, 128, fmt)
+    pt = batch.page_table[0, :prefix // 16].contiguous() if prefix else None
+    q = q[:sum(per)]
+    rows = len(per) * max(per) + 1000
+    wide = S.KVBatch(batch.row_offsets, batch.lens, batch.page_table, rows, max(per), batch.max_len)
+    qw = torch.full((rows, 512), float("nan"), dtype=torch.bfloat16, device=DEV)
+    qw[:sum(per)] = q
+    out = torch.full((rows, 512), 9.0, dtype=torch.bfloat16, device=DEV)
+    lw = torch.full((rows, 4), 9.0, device=DEV)
+    most = S.KVBatch(batch.row_offsets, batch.lens, batch.page_table, len(per) * max(per), max(per), batch.max_len)
+    size = S.attention_workspace_bytes(cache, wide, 4, prefix_len=prefix)
+    assert size == S.attention_workspace_bytes(cache, most, 4, prefix_len=prefix)
+    ws = torch.full((size + 256,), 255, dtype=torch.uint8, device=DEV)
+    S.sharq_attention(qw, cache, wide, prefix_table=pt, prefix_len=prefix, out=out, lse=lw, workspace=ws[:size])
+    assert (ws[size:] == 255).all() and (out[sum(per):] == 9).all() and (lw[sum(per):] == 9).all()
+    bare = S.KVBatch(batch.row_offsets, batch.lens, batch.page_table, sum(per), max(per), batch.max_len)
+    check(q, cache, bare, offsets, ln, table, out[:sum(per)], lw[:sum(per)], prefix_len=prefix,
+          prefix_table=None if pt is None else pt.cpu().numpy())
+
+
+@pytest.mark.parametrize("fmt", FMTS)
 def test_strided_rows_default_output_and_repeated_calls(fmt):
     per, lens = [1, 1, 1, 2], [4000, 17, 256, 2000]
     batch, offsets, ln, table, cache, q = setup(per, lens, 64, 8, 2, 128, fmt)

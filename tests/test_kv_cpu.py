@@ -317,6 +317,20 @@ def test_empty_calls_do_nothing(L):
     assert attention(L, b=batch(max_rows=0), q=None, o=None, ws=None, size=0) == OK
 
 
+def test_padding_rows_take_no_workspace(L):
+    """Only rows that sequences can own (seqs times max_rows) have partial results."""
+    def size(c=cache(), heads=4, **kw):
+        return L.sharq_attention_workspace_bytes(ctypes.byref(c), ctypes.byref(batch(max_len=4096, ld_table=256, **kw)),
+                                                 ctypes.byref(attn()), heads)
+    for seqs, max_rows in ((1, 1), (3, 1), (2, 8), (1, 300)):
+        want = size(seqs=seqs, rows=seqs * max_rows, max_rows=max_rows)
+        assert want > 0
+        for rows in (seqs * max_rows + 1, 5000, 1 << 20):
+            assert size(seqs=seqs, rows=rows, max_rows=max_rows) == want
+        assert size(seqs=seqs, rows=seqs * max_rows, max_rows=1 << 40) == size(seqs=seqs, rows=seqs * max_rows,
+                                                                               max_rows=seqs * max_rows)
+
+
 def test_null_structs(L):
     c, b, t = cache(), batch(), attn()
     r = ctypes.byref
