@@ -495,7 +495,7 @@ SHARQ_API sharq_status sharq_kv_read(const sharq_kv_cache *cache, const sharq_kv
 /*
  * What a row sees of its sequence: the row at position p sees the tokens
  * t <= p with p - t < window (window 0: all of them) or t < sinks.
- *   scale         factor of the scores q.k, positive and finite.
+ *   scale         factor of the scores q.k, positive, from 2^-100 to 2^100.
  *   prefix_table, prefix_len
  *                 tokens that all sequences of the call share: those at the
  *                 positions below prefix_len (a multiple of page_size, at most

@@ -27,6 +27,7 @@ constexpr int64_t kMaxLen = (int64_t)1 << 30;
 constexpr int64_t kMaxSeqs = (int64_t)1 << 16;
 constexpr int64_t kMaxHeads = 1024;
 constexpr int64_t kMaxGroup = 128;
+constexpr float kMinScale = 0x1p-100f, kMaxScale = 0x1p100f;   // scale times log2 e and times a maximum's start stay normal
 constexpr int64_t kMaxHeadRows = (int64_t)1 << 26;   // rows times heads of a call: launches stay below 2^31 threads
 
 bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
@@ -94,6 +95,7 @@ sharq_status check_attn(const sharq_attn* t, const sharq_kv_cache* c, const shar
     return SHARQ_EUNSUPPORTED;
   if (!(t->scale > 0.0f) || __builtin_isinf(t->scale) || t->window < 0 || t->sinks < 0) return SHARQ_EINVAL;
   if (t->prefix_len < 0 || t->prefix_len > b->max_len || t->prefix_len % c->page_size != 0) return SHARQ_EINVAL;
+  if (t->scale < kMinScale || t->scale > kMaxScale) return SHARQ_EUNSUPPORTED;
   if (!arrays) return SHARQ_OK;
   if (t->prefix_len > 0 && !t->prefix_table) return SHARQ_EINVAL;
   if (!aligned(t->prefix_table, 4)) return SHARQ_EALIGN;

@@ -199,6 +199,14 @@ def test_large_scale_where_a_wavefront_sees_nothing(per, fmt):
 
 
 @pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("per,lens,prefix", [([1, 1], [3000, 20], 0), ([70], [90], 0), ([2, 1], [300, 600], 256)])
+@pytest.mark.parametrize("scale", [2.0 ** -100, 2.0 ** -60])
+def test_smallest_scales(scale, per, lens, prefix, fmt):
+    """Scores of nearly nothing: the outputs are means of the visible values."""
+    run(per, lens, 16, 4, 2, 128, fmt, scale=scale, prefix_len=prefix)
+
+
+@pytest.mark.parametrize("fmt", FMTS)
 @pytest.mark.parametrize("count", [65, 130, 200])
 def test_more_sequences_than_a_wavefront(count, fmt):
     rng = np.random.default_rng(count)

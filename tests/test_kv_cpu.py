@@ -309,6 +309,14 @@ def test_bad_attention_arguments(L):
         assert attention(L, **kw) == status, kw
 
 
+def test_scales_out_of_range(L):
+    """A scale whose product with log2 e, or with the running maximum's start, is no normal fp32 number."""
+    for scale in (1e-45, 2.0 ** -126, 1.5e-38, 2.0 ** -101, 2.0 ** 101, 3e38):
+        assert attention(L, t=attn(scale=scale)) == EUNSUPPORTED, scale
+        assert L.sharq_attention_workspace_bytes(ctypes.byref(cache()), ctypes.byref(batch(max_len=4096, ld_table=256)),
+                                                 ctypes.byref(attn(scale=scale)), 4) == 0
+
+
 def test_empty_calls_do_nothing(L):
     for b in (batch(seqs=0), batch(rows=0), batch(seqs=0, rows=0, ld_table=0, row_offsets=None, lens=None, page_table=None)):
         assert append(L, b=b, q=None, k=None, v=None, out=None) == OK
