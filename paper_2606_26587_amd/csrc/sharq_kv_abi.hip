@@ -194,6 +194,7 @@ sharq_status sharq_attention(const void* Q, sharq_dtype xdt, int64_t q_heads, in
   const sharq::AttnPlan plan = plan_of(cache, batch, attn, q_heads);
   const size_t need = (size_t)sharq::attn_workspace(owned_rows(batch) * q_heads, plan.slots, (int)D);
   if (need > 0 && (!workspace || workspace_bytes < need)) return SHARQ_EINVAL;
+  if (O == Q) return SHARQ_EINVAL;   // several workgroups read a row's queries
   return hip_status(sharq::launch_attention(
       static_cast<const uint16_t*>(Q), ldq, static_cast<uint16_t*>(O), ldo, lse, batch_args(batch, owned_rows(batch)),
       cache_args(cache), plan, attn->prefix_table, (int)attn->prefix_len, (int)q_heads, (int)D,

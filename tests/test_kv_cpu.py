@@ -317,6 +317,10 @@ def test_scales_out_of_range(L):
                                                  ctypes.byref(attn(scale=scale)), 4) == 0
 
 
+def test_attention_in_place_is_refused(L):
+    assert attention(L, q=FAKE, o=FAKE, ws=FAKE, size=1 << 30) == EINVAL
+
+
 def test_empty_calls_do_nothing(L):
     for b in (batch(seqs=0), batch(rows=0), batch(seqs=0, rows=0, ld_table=0, row_offsets=None, lens=None, page_table=None)):
         assert append(L, b=b, q=None, k=None, v=None, out=None) == OK
