@@ -6,7 +6,7 @@
 namespace sharq {
 
 template <int D, bool MX, bool ALL>
-__global__ __launch_bounds__(256, 2) void k_attn_rows(AttnArgs a, int tiles, int chunk_tiles, int first_slot) {
+__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void k_attn_rows(AttnArgs a, int tiles, int chunk_tiles, int first_slot) {
   __shared__ RowsLds<D> lds;
   attn_rows<D, MX, ALL>(a, (int)blockIdx.x, tiles, chunk_tiles, first_slot, lds);
 }

@@ -25,10 +25,10 @@
 // two wavefronts a SIMD, of two workgroups that run apart, so one's exponentials
 // can run beside the other's products), and walks tiles of 64 tokens in two LDS
 // stages: while one is worked on, the next is on its way, bf16 straight from
-// global memory to LDS, MXFP4 through registers, where it becomes bf16 once for
-// all rows.  Rows of consecutive tokens share the tiles: with 4 query heads a
-// key/value head a tile is 32 tokens, so little of a causal or windowed tile is
-// masked, and masks are formed only in tiles that need one.
+// global memory to LDS; of MXFP4 the next two, through registers, from where it
+// becomes bf16 once for all rows.  Rows of consecutive tokens share the tiles:
+// with 4 query heads a key/value head a tile is 32 tokens, so little of a causal
+// or windowed tile is masked, and masks are formed only in tiles that need one.
 //
 // Measured (8192 tokens, 32 query and 8 key/value heads of 128, causal): 537 us,
 // 1.02 PFLOP/s, 0.84 of what a library bf16 product of 8192^3 reaches on the same
@@ -38,7 +38,7 @@
 // second half's products (544, and with the maximum left out 546 against 540),
 // halves of masked tiles skipped (571) and raised priority around the products
 // (550) were measured and not kept.  Heads of 64: 830 TFLOP/s, the exponentials
-// weigh twice as much; an MXFP4 cache costs 5 to 10% here.
+// weigh twice as much.  An MXFP4 cache costs 1% here.
 
 #pragma once
 
@@ -175,13 +175,16 @@ __device__ __forceinline__ void attn_rows(const AttnArgs& a, int block, int tile
   if (wave * 32 >= rows) w_hi = -1;   // no rows: loads its share of the tiles, no more
   const KvSpan span = kv_span(t0, t1, p_lo, p_hi, a.window, a.sinks, kT);
   const int first = chunk * chunk_tiles, end = span.n < first + chunk_tiles ? span.n : first + chunk_tiles;
-  // lane i: page of token i of a tile, -1 where no row sees it (it may hold anything), and its cache row
+  // lane i: page of token i of a tile (of another that is seen where it is not: the load has no condition), and its
+  // cache row, -1 where no row sees it (its page may hold anything)
   auto page_of = [&](int ti) {
     const int t = kv_tile_start(span, t0, ti, kT) + lane;
-    return ti < end && t < span.hi && (t >= span.low || t < a.sinks) ? token_page(a, seq, t) : -1;
+    return token_page(a, seq, t < span.hi ? t : span.hi - 1);
   };
   auto row_of = [&](int page, int ti) {
-    return kv_row(page, kv_tile_start(span, t0, ti, kT) + lane, a.c.pages, a.c.heads, head, a.c.page_shift);
+    const int t = kv_tile_start(span, t0, ti, kT) + lane;
+    const bool seen = ti < end && t < span.hi && (t >= span.low || t < a.sinks);
+    return seen ? kv_row(page, t, a.c.pages, a.c.heads, head, a.c.page_shift) : -1;
   };
   // A wavefront stages 16 tokens of a tile, which lie in one page: tiles start at multiples of 16.
   constexpr int kI = kC / 4, kRowsLoad = 64 / kC;   // bf16: 16-byte loads of a lane, keys or values; rows of a load
@@ -191,49 +194,52 @@ __device__ __forceinline__ void attn_rows(const AttnArgs& a, int block, int tile
     const int row = i * kRowsLoad + lane / kC;
     off[i] = (uint32_t)(row * D * 2 + 16 * (kv_chunk<D>(row, lane % kC) - row * kC));
   }
-  // MXFP4: the next tile's codes and scales on their way, 32 values a lane: 16 tokens at one place of their rows, so
-  // that they go to LDS over all banks
-  uint4 kb, vb;
-  uint32_t ke, ve;
-  const int mx_row = mx_token<D>(lane), mx_block = lane >> 4;
-  const bool mx_lane = mx_block < D / 32;
-  auto load = [&](int at, int stage) {
+  // MXFP4: two tiles' codes and scales on their way, 32 values a lane: 16 tokens at one place of their rows, so that
+  // they go to LDS over all banks.  A step of few rows is shorter than the way from HBM: with one tile on its way
+  // 16 x 9 tokens, 4 query heads a key/value head, over 8000 took 80 us, with two 69; a prompt of 5759, heads of 64,
+  // 210 and 191.
+  struct Codes {
+    uint4 k, v;
+    uint32_t ks, vs;
+  } ahead[MX ? 2 : 1];
+  const int mx_row = mx_token<D>(lane), mx_block = (lane >> 4) % (D / 32);
+  const int mx_byte = mx_row * (D / 32) + mx_block;   // of the 16 tokens' scales; loaded as the dword that holds it
+  auto load = [&](int at, int to) {
     const unsigned mine = (unsigned)(__ballot(at >= 0) >> (16 * wave)) & 0xFFFFu;
-    if (MX) {
-      kb = vb = make_uint4(0, 0, 0, 0);
-      ke = ve = 0;
-    }
-    if (mine == 0) return;
-    const int l0 = 16 * wave + __builtin_ctz(mine);
-    const int64_t row0 = __builtin_amdgcn_readlane(at, l0) - (l0 & 15);
-    if (MX) {
-      if (mx_lane && ((mine >> mx_row) & 1)) {
-        const int64_t block = (row0 + mx_row) * (D / 32) + mx_block;
-        kb = *reinterpret_cast<const uint4*>(a.c.k + block * 16);
-        vb = *reinterpret_cast<const uint4*>(a.c.v + block * 16);
-        ke = a.c.ks[block];
-        ve = a.c.vs[block];
-      }
-    } else {
+    const int l0 = 16 * wave + (mine ? __builtin_ctz(mine) : 0);
+    if (MX) {   // without conditions, so that later waits can count these loads; 16 tokens that no row sees: any others
+      const int64_t row0 = mine ? __builtin_amdgcn_readlane(at, l0) - (l0 & 15) : 0;
+      const uint32_t block = (uint32_t)mx_byte;
+      Codes& x = ahead[to];
+      x.k = *reinterpret_cast<const uint4*>(a.c.k + row0 * (D / 2) + block * 16);
+      x.v = *reinterpret_cast<const uint4*>(a.c.v + row0 * (D / 2) + block * 16);
+      x.ks = reinterpret_cast<const uint32_t*>(a.c.ks + row0 * (D / 32))[block / 4];
+      x.vs = reinterpret_cast<const uint32_t*>(a.c.vs + row0 * (D / 32))[block / 4];
+    } else if (mine) {
+      const int64_t row0 = __builtin_amdgcn_readlane(at, l0) - (l0 & 15);
       const uint8_t *kp = a.c.k + row0 * (D * 2), *vp = a.c.v + row0 * (D * 2);
 #pragma unroll
       for (int i = 0; i < kI; ++i)
         if (mine == 0xFFFFu || ((mine >> (i * kRowsLoad + lane / kC)) & 1)) {
-          lds_load16(&lds[stage][0][wave * 16 * kC + i * 64], kp, off[i]);
-          lds_load16(&lds[stage][1][wave * 16 * kC + i * 64], vp, off[i]);
+          lds_load16(&lds[to][0][wave * 16 * kC + i * 64], kp, off[i]);
+          lds_load16(&lds[to][1][wave * 16 * kC + i * 64], vp, off[i]);
         }
     }
   };
-  // What load() leaves out keeps its place in LDS: keys there are masked, values meet a weight of zero and must be
-  // finite.  So the stages start as zeros, and only tokens that some row sees come after.
-  auto store = [&](int stage) {
-    if (MX && mx_lane) {
+  // Keys that no row sees are masked; their values meet a weight of zero and must be finite.  MXFP4: zeros go to LDS.
+  // bf16: what load() leaves out keeps its place there, so the stages start as zeros, and only tokens that some row
+  // sees come after.
+  auto store = [&](int stage, unsigned long long live) {
+    if (MX && lane >> 4 < D / 32) {
       const int row = 16 * wave + mx_row, c0 = 4 * mx_block;
-      const uint32_t kw[4] = {kb.x, kb.y, kb.z, kb.w}, vw[4] = {vb.x, vb.y, vb.z, vb.w};
+      const Codes& x = ahead[stage];
+      const bool dead = !((live >> row) & 1);
+      const uint32_t ks = dead ? 0 : x.ks >> (8 * (mx_byte & 3)) & 0xFF, vs = dead ? 0 : x.vs >> (8 * (mx_byte & 3)) & 0xFF;
+      const uint32_t kw[4] = {x.k.x, x.k.y, x.k.z, x.k.w}, vw[4] = {x.v.x, x.v.y, x.v.z, x.v.w};
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        lds[stage][0][kv_chunk<D>(row, c0 + e)] = mx_bf16x8(kw[e], ke);
-        lds[stage][1][kv_chunk<D>(row, c0 + e)] = mx_bf16x8(vw[e], ve);
+      for (int e = 0; e < 4; ++e) {   // zero codes times 2^-127
+        lds[stage][0][kv_chunk<D>(row, c0 + e)] = mx_bf16x8(dead ? 0 : kw[e], ks);
+        lds[stage][1][kv_chunk<D>(row, c0 + e)] = mx_bf16x8(dead ? 0 : vw[e], vs);
       }
     }
   };
@@ -253,22 +259,38 @@ __device__ __forceinline__ void attn_rows(const AttnArgs& a, int block, int tile
       v_at[d][u] = 16 * kv_chunk<D>(8 * u + 4 * half + ((lane & 15) >> 2), 4 * d + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) +
                    8 * (lane & 1);
 
-  int at = row_of(page_of(first), first), next = page_of(first + 1);   // rows of this tile, pages of the next
-  load(at, 0);
-  store(0);
+  // Tiles and pages of a tile on their way while one is worked on.  MXFP4: tile ti is in ahead[] and in LDS at the
+  // parity of ti - first.
+  constexpr int kAhead = MX ? 2 : 1;
+  unsigned long long live[kAhead + 1] = {};   // of this tile and the next ones, token by token: whether it is there
+  int next = 0;
+  const bool any = first < end && a.c.pages > 0;
+  if (any) {
+    int page[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) page[i] = page_of(first + i);
+    next = page_of(first + kAhead);
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int at = row_of(page[i], first + i);
+      live[i] = __ballot(at >= 0);
+      load(at, i);
+    }
+    store(0, live[0]);
+  }
   // the queries, here and once: the loop's own waits would count the tiles' loads among theirs
 #pragma unroll
   for (int i = 0; i < D / 16; ++i) asm volatile("" : "+v"(qf[i]));
-  lds_load_wait();
+  if (!MX) lds_load_wait();
   __syncthreads();
   auto step = [&](int ti, auto stage_c) {
     constexpr int stage = decltype(stage_c)::value;
     const int ts = kv_tile_start(span, t0, ti, kT);
-    const unsigned long long live = __ballot(at >= 0);
-    at = row_of(next, ti + 1);
-    load(at, stage ^ 1);
-    next = page_of(ti + 2);
-    if (ts <= w_hi) {
+    const int at = row_of(next, ti + kAhead);
+    live[kAhead] = __ballot(at >= 0);
+    next = page_of(ti + kAhead + 1);
+    load(at, MX ? stage : stage ^ 1);
+    if (ts <= w_hi && live[0] != 0) {
       const char *sk = reinterpret_cast<const char*>(lds[stage][0]), *sv = reinterpret_cast<const char*>(lds[stage][1]);
       v16f s[2] = {};
       v8bf kf[2][D / 16];
@@ -290,8 +312,8 @@ __device__ __forceinline__ void attn_rows(const AttnArgs& a, int block, int tile
       }
       __builtin_amdgcn_sched_group_barrier(kSchedMfma, 4, 0);
       // unless every row of the wavefront sees every token
-      if (live != ~0ull || ts + kT - 1 > w_lo || (w_hi - ts >= a.window && ts + kT > a.sinks)) {
-        const unsigned long long see = row_sees(live, p, ts + 4 * half, 4 * half, a.window, a.sinks);
+      if (live[0] != ~0ull || ts + kT - 1 > w_lo || (w_hi - ts >= a.window && ts + kT > a.sinks)) {
+        const unsigned long long see = row_sees(live[0], p, ts + 4 * half, 4 * half, a.window, a.sinks);
 #pragma unroll
         for (int mt = 0; mt < 2; ++mt) {
           const uint32_t bits = (uint32_t)(see >> (32 * mt));
@@ -340,14 +362,17 @@ __device__ __forceinline__ void attn_rows(const AttnArgs& a, int block, int tile
           o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[st], o[d], 0, 0, 0);
         }
     }
-    store(stage ^ 1);
-    lds_load_wait();
+    store(stage ^ 1, live[1]);
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) live[i] = live[i + 1];
+    if (!MX) lds_load_wait();
     __syncthreads();
   };
-  for (int ti = first; ti < end; ti += 2) {
-    step(ti, std::integral_constant<int, 0>{});
-    if (ti + 1 < end) step(ti + 1, std::integral_constant<int, 1>{});
-  }
+  if (any)
+    for (int ti = first; ti < end; ti += 2) {   // (MXFP4: in pairs, so that waits stay counted; past the end are no tokens)
+      step(ti, std::integral_constant<int, 0>{});
+      if (MX || ti + 1 < end) step(ti + 1, std::integral_constant<int, 1>{});
+    }
   l += __shfl_xor(l, 32);
   const int mine = rows - wave * 32 < 32 ? rows - wave * 32 : 32;   // rows of this wavefront
   if (mine <= 0) return;
