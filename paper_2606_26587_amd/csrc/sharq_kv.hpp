@@ -122,9 +122,14 @@ constexpr AttnPlan attn_plan(int64_t seqs, int64_t rows, int64_t max_rows, int64
     const int64_t most = seqs * ceil_div(r, kAttnRows), packed = rows * group / kAttnRows + seqs;
     const int64_t tiles = most < packed ? most : packed;
     const int64_t kv = part > 0 ? ceil_div(part, kAttnTile) + (part < own ? 1 : 0) + ceil_div(s, kAttnTile) : 0;
-    // about as many workgroups as the chip holds (2 a CU; heads of 64: 3): 500 rows over 12000 tokens, 4 heads of 64:
-    // 70.8 us with 512, 66.2 with 1024; of 128: 101 and 112, where the partial results weigh more
-    p.own = attn_split(tiles, tiles * heads, kv, D == 64 ? 1024 : 512, 4);
+    // About as many workgroups as the chip holds (2 a CU; heads of 64: 3): 500 rows over 12000 tokens, 4 heads of 64:
+    // 70.8 us with 512, 66.2 with 1024; of 128: 101 and 112, where the partial results weigh more.  Sequences of
+    // different lengths fill half of their last tiles: 32 x up to 17 tokens over 8000, 4 x 8 heads of 128, 130 us with
+    // whole last tiles counted, 106 with halves; 6 x 100 over 6000, 8 x 4 heads, 73 and 63.
+    int64_t likely = rows * group / kAttnRows + seqs / 2 + 1;
+    likely = likely < seqs ? seqs : likely;
+    const int64_t units = (likely < tiles ? likely : tiles) * heads;
+    p.own = attn_split(tiles, units, kv, D == 64 ? 1024 : 512, 4);
   }
   p.slots = p.own.chunks > 1 ? p.own.chunks : 0;
   if (p.shared) {
