@@ -5,27 +5,20 @@
 
 namespace sharq {
 
-template <int D, bool MX, bool ALL>
-__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void k_attn_rows(AttnArgs a, int tiles, int chunk_tiles, int first_slot) {
-  __shared__ RowsLds<D> lds;
-  attn_rows<D, MX, ALL>(a, (int)blockIdx.x, tiles, chunk_tiles, first_slot, lds);
-}
-
 template <int D, bool MX>
-static void rows(bool all, dim3 g, const AttnArgs& a, int tiles, int chunk_tiles, int first_slot, hipStream_t st) {
-  if (all) k_attn_rows<D, MX, true><<<g, 256, 0, st>>>(a, tiles, chunk_tiles, first_slot);
-  else k_attn_rows<D, MX, false><<<g, 256, 0, st>>>(a, tiles, chunk_tiles, first_slot);
+__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void k_attn_rows(AttnArgs a, int tiles, int chunk_tiles) {
+  __shared__ RowsLds<D> lds;
+  attn_rows<D, MX, false>(a, (int)blockIdx.x, tiles, chunk_tiles, 0, lds);
 }
 
-static hipError_t launch_attn_rows(const AttnArgs& a, int D, bool mx, bool all, const AttnSplit& s, int first_slot,
-                                   hipStream_t st) {
+static hipError_t launch_attn_rows(const AttnArgs& a, int D, bool mx, const AttnSplit& s, hipStream_t st) {
   const dim3 g((unsigned)s.tiles * (unsigned)a.c.heads * (unsigned)s.chunks);
   if (D == 128)
-    mx ? rows<128, true>(all, g, a, s.tiles, s.chunk_tiles, first_slot, st)
-       : rows<128, false>(all, g, a, s.tiles, s.chunk_tiles, first_slot, st);
+    mx ? k_attn_rows<128, true><<<g, 256, 0, st>>>(a, s.tiles, s.chunk_tiles)
+       : k_attn_rows<128, false><<<g, 256, 0, st>>>(a, s.tiles, s.chunk_tiles);
   else
-    mx ? rows<64, true>(all, g, a, s.tiles, s.chunk_tiles, first_slot, st)
-       : rows<64, false>(all, g, a, s.tiles, s.chunk_tiles, first_slot, st);
+    mx ? k_attn_rows<64, true><<<g, 256, 0, st>>>(a, s.tiles, s.chunk_tiles)
+       : k_attn_rows<64, false><<<g, 256, 0, st>>>(a, s.tiles, s.chunk_tiles);
   return hipGetLastError();
 }
 
@@ -42,14 +35,9 @@ hipError_t launch_attention(const uint16_t* q, int64_t ldq, uint16_t* o, int64_t
              q_heads, window, sinks, (float)((double)scale * 1.4426950408889634),
              static_cast<float2*>(ws), nullptr, plan.slots};
   if (plan.slots) a.po = reinterpret_cast<float*>(static_cast<char*>(ws) + attn_ml_bytes(items, plan.slots));
-  hipError_t e = hipSuccess;
-  if (plan.shared && plan.few) {
-    e = launch_attn_shared(a, D, mx, plan, st);
-  } else {
-    if (plan.shared) e = launch_attn_rows(a, D, mx, true, plan.prefix, plan.own.chunks, st);
-    if (e != hipSuccess) return e;
-    e = plan.few ? launch_attn_few(a, D, mx, plan, st) : launch_attn_rows(a, D, mx, false, plan.own, 0, st);
-  }
+  const hipError_t e = plan.shared ? launch_attn_shared(a, D, mx, plan, st)
+                       : plan.few  ? launch_attn_few(a, D, mx, plan, st)
+                                   : launch_attn_rows(a, D, mx, plan.own, st);
   if (e != hipSuccess || plan.slots == 0) return e;
   return launch_attn_merge(a, D, st);
 }

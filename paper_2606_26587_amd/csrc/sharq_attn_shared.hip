@@ -1,14 +1,25 @@
-// Attention behind a shared prefix, where the sequences have few rows: one launch
-// whose first workgroups take all rows' part over the prefix and whose others
-// take the sequences' own parts.  Neither fills the chip by itself (the prefix is
-// a few tiles of rows, bound by its latencies; the own parts stream HBM), so they
-// run side by side: in two launches one after the other, 64 tokens behind 8192
-// shared ones with 130 to 400 of their own took 25 + 20 us.
+// Attention behind a shared prefix: one launch whose first workgroups take all
+// rows' part over the prefix and whose others take the sequences' own parts.
+// Neither fills the chip by itself (the prefix is a few tiles of rows, bound by
+// its latencies; the own parts stream HBM), so they run side by side: in two
+// launches one after the other, 64 tokens behind 8192 shared ones with 130 to 400
+// of their own took 25 + 20 us, now 33; 43 x up to 10 tokens, 16 heads a
+// key/value head, behind 4160 39.5, now 29.7.
 
 #include "sharq_attn_few.hpp"
 #include "sharq_attn_rows.hpp"
 
 namespace sharq {
+
+// Where the sequences have more rows than the kernel for few takes: prefix first as well.
+template <int D, bool MX>
+__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void k_attn_shared_rows(AttnArgs a, AttnSplit prefix,
+                                                                          int prefix_blocks, AttnSplit own) {
+  __shared__ RowsLds<D> lds;
+  const int block = (int)blockIdx.x;
+  if (block < prefix_blocks) attn_rows<D, MX, true>(a, block, prefix.tiles, prefix.chunk_tiles, own.chunks, lds);
+  else attn_rows<D, MX, false>(a, block - prefix_blocks, own.tiles, own.chunk_tiles, 0, lds);
+}
 
 template <int D, bool MX, int NQ, int NT>
 __global__ __launch_bounds__(256, 2) void k_attn_shared(AttnArgs a, AttnSplit prefix, int prefix_blocks, int chunk_tiles,
@@ -26,8 +37,10 @@ template <int D, bool MX>
 static void shared(const AttnArgs& a, const AttnPlan& p, hipStream_t st) {
   constexpr int NT = MX ? 2 : 1;
   const int first = p.prefix.tiles * p.prefix.chunks * a.c.heads, ct = p.own.chunk_tiles, oc = p.own.chunks;
-  const dim3 g((unsigned)first + (unsigned)oc * (unsigned)a.b.seqs * (unsigned)a.c.heads);
-  if (p.few == 1) k_attn_shared<D, MX, 1, NT><<<g, 256, 0, st>>>(a, p.prefix, first, ct, oc);
+  const unsigned units = p.few ? (unsigned)a.b.seqs : (unsigned)p.own.tiles;
+  const dim3 g((unsigned)first + (unsigned)oc * units * (unsigned)a.c.heads);
+  if (!p.few) k_attn_shared_rows<D, MX><<<g, 256, 0, st>>>(a, p.prefix, first, p.own);
+  else if (p.few == 1) k_attn_shared<D, MX, 1, NT><<<g, 256, 0, st>>>(a, p.prefix, first, ct, oc);
   else if (p.few == 2) k_attn_shared<D, MX, 2, NT><<<g, 256, 0, st>>>(a, p.prefix, first, ct, oc);
   else if constexpr (D == 64) k_attn_shared<D, MX, 4, NT><<<g, 256, 0, st>>>(a, p.prefix, first, ct, oc);
 }
