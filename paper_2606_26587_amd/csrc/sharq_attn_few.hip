@@ -89,8 +89,10 @@ template <int D, bool MX>
 static void few(int nq, dim3 g, const AttnArgs& a, int chunk_tiles, hipStream_t st) {
   constexpr int NT = MX ? 2 : 1;
   if (nq == 1) k_attn_few<D, MX, 1, NT><<<g, 256, 0, st>>>(a, chunk_tiles, 0);
-  else if (nq == 2) k_attn_few<D, MX, 2, NT><<<g, 256, 0, st>>>(a, chunk_tiles, 0);
-  else if constexpr (D == 64) k_attn_few<D, MX, 4, NT><<<g, 256, 0, st>>>(a, chunk_tiles, 0);
+  if constexpr (D == 64 || MX)
+    if (nq == 2) k_attn_few<D, MX, 2, NT><<<g, 256, 0, st>>>(a, chunk_tiles, 0);
+  if constexpr (D == 64 && MX)
+    if (nq == 4) k_attn_few<D, MX, 4, NT><<<g, 256, 0, st>>>(a, chunk_tiles, 0);
 }
 
 hipError_t launch_attn_few(const AttnArgs& a, int D, bool mx, const AttnPlan& plan, hipStream_t st) {

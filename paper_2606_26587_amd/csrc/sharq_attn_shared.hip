@@ -39,10 +39,12 @@ static void shared(const AttnArgs& a, const AttnPlan& p, hipStream_t st) {
   const int first = p.prefix.tiles * p.prefix.chunks * a.c.heads, ct = p.own.chunk_tiles, oc = p.own.chunks;
   const unsigned units = p.few ? (unsigned)a.b.seqs : (unsigned)p.own.tiles;
   const dim3 g((unsigned)first + (unsigned)oc * units * (unsigned)a.c.heads);
-  if (!p.few) k_attn_shared_rows<D, MX><<<g, 256, 0, st>>>(a, p.prefix, first, p.own);
-  else if (p.few == 1) k_attn_shared<D, MX, 1, NT><<<g, 256, 0, st>>>(a, p.prefix, first, ct, oc);
-  else if (p.few == 2) k_attn_shared<D, MX, 2, NT><<<g, 256, 0, st>>>(a, p.prefix, first, ct, oc);
-  else if constexpr (D == 64) k_attn_shared<D, MX, 4, NT><<<g, 256, 0, st>>>(a, p.prefix, first, ct, oc);
+  if (p.few == 0) k_attn_shared_rows<D, MX><<<g, 256, 0, st>>>(a, p.prefix, first, p.own);
+  if (p.few == 1) k_attn_shared<D, MX, 1, NT><<<g, 256, 0, st>>>(a, p.prefix, first, ct, oc);
+  if constexpr (D == 64 || MX)
+    if (p.few == 2) k_attn_shared<D, MX, 2, NT><<<g, 256, 0, st>>>(a, p.prefix, first, ct, oc);
+  if constexpr (D == 64 && MX)
+    if (p.few == 4) k_attn_shared<D, MX, 4, NT><<<g, 256, 0, st>>>(a, p.prefix, first, ct, oc);
 }
 
 hipError_t launch_attn_shared(const AttnArgs& a, int D, bool mx, const AttnPlan& p, hipStream_t st) {

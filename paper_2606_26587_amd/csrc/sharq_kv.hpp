@@ -101,7 +101,11 @@ constexpr AttnPlan attn_plan(int64_t seqs, int64_t rows, int64_t max_rows, int64
   // a window leaves little of a prefix, and rows that see different parts of it
   p.shared = prefix_len > 0 && window >= max_len;
   const int64_t r = max_rows * group, own = max_len - (p.shared ? prefix_len : 0);
-  p.few = r <= 16 ? 1 : r <= 32 ? 2 : r <= 64 && D == 64 ? 4 : 0;   // (64 rows' states over heads of 128 fill the registers)
+  // The kernel for few rows up to 16, and up to 32 or 64 where it is the faster one.  In it and in the kernel for many:
+  // bf16, heads of 128, 16 x 8 tokens of 4 query heads over 8000 87 and 81 us, 64 x 5 over 600 29 and 25, 1 x 8 over
+  // 4000 13.6 and 14.4; heads of 64, 2 x 8 over 16000 19 and 23, 16 x 12 over 8000 62 and 58; MXFP4, heads of 64,
+  // 16 x 12 39 and 53.  (64 rows' states over heads of 128 fill the registers.)
+  p.few = r <= 16 ? 1 : r <= 32 && (D == 64 || mx) ? 2 : r <= 64 && D == 64 && mx ? 4 : 0;
   // tokens that a tile of rows sees at most: its window and its own positions, and the sinks
   const int64_t span = p.few ? max_rows : kAttnRows / group + 2;
   const int64_t w = window < max_len ? window + span : own, part = w < own ? w : own;
@@ -112,11 +116,15 @@ constexpr AttnPlan attn_plan(int64_t seqs, int64_t rows, int64_t max_rows, int64
     // One round of workgroups where a wavefront has few turns of its tiles.  Where it has many, and the kernel's states
     // leave room for three workgroups a CU, four rounds: then what sequences of different lengths leave idle counts for
     // more than starting up and joining.  One round against four, 8 heads: single tokens in bf16, 8 x 8191 44.8 and
-    // 47.2 us, 64 x 1000 40.3 and 45.1, 64 x 4000 135 and 124, 24 x 32768 502 and 420; 5 tokens a sequence, 20 rows,
-    // over 16 x 16000: heads of 64 98.8 and 82.6, of 128 146 and 158.  Beside a shared prefix's workgroups: one round.
+    // 47.2 us, 64 x 1000 40.3 and 45.1, 64 x 4000 135 and 124, 24 x 32768 502 and 420; 5 tokens a sequence, 20 rows
+    // of heads of 64, over 16 x 16000 98.8 and 82.6.  Beside a shared prefix's workgroups: one round.
     const bool lean = p.few == 1 || (p.few == 2 && D == 64);
     const int64_t units = seqs * heads, turns = units * ceil_div(kv, 4);
-    p.own = attn_split(1, units, kv, p.shared ? 512 : lean && turns >= 6144 ? 2048 : mx && p.few == 1 ? 768 : 512, 4);
+    // Where one round leaves a third of the chip idle, two: 33 x 1500 single tokens in bf16 47.2 and 36.9 us, 40 x 1500
+    // 45.6 and 39.9; 33 x 8 tokens over 5000 in MXFP4 68.1 and 55.1.  (With 480 of 512 places taken the same loses 10%.)
+    const bool idle = units > 256 && units <= 341 && turns >= (lean ? 3072 : 4096);
+    const int want = p.shared ? 512 : lean && turns >= 6144 ? 2048 : idle ? 1024 : mx && p.few == 1 ? 768 : 512;
+    p.own = attn_split(1, units, kv, want, 4);
   } else {
     // no sequence has more than max_rows rows, and all together have no more than rows
     const int64_t most = seqs * ceil_div(r, kAttnRows), packed = rows * group / kAttnRows + seqs;

@@ -207,6 +207,15 @@ def test_smallest_scales(scale, per, lens, prefix, fmt):
 
 
 @pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("prefix", [0, 192])
+@pytest.mark.parametrize("new", [1, 4, 5, 8, 9, 16, 17, 33])
+def test_rows_around_the_limits_of_the_kernels(new, prefix, D, fmt):
+    """16, 32, 64 and 128 rows of a sequence and key/value head and one token more, with 4 query heads to a head."""
+    run([new, max(1, new - 3), 1], [700, 260, 450], 16, 8, 2, D, fmt, prefix_len=prefix)
+
+
+@pytest.mark.parametrize("fmt", FMTS)
 @pytest.mark.parametrize("count", [65, 130, 200])
 def test_more_sequences_than_a_wavefront(count, fmt):
     rng = np.random.default_rng(count)
