@@ -525,8 +525,7 @@ SHARQ_API size_t sharq_attention_workspace_bytes(const sharq_kv_cache *cache, co
  * K and V including the rows' own (appended before).  Query head h reads
  * key/value head h / (q_heads / kv_heads); q_heads is a multiple of kv_heads,
  * at most 128 times.  One call takes prompts, chunks of prompts and single
- * tokens, mixed; over an MXFP4 cache single tokens with long contexts run faster
- * in a call of their own than beside a prompt.
+ * tokens, mixed.
  *   Q, O: bf16 [rows][q_heads * head_dim], row strides ldq, ldo, 16-byte aligned
  *   with 16-byte row strides; O overlaps neither Q nor the cache (O == Q is refused).
  *   lse: fp32 [rows][q_heads] or NULL: the natural logarithm of the sum of

@@ -23,6 +23,7 @@ static hipError_t launch_attn_rows(const AttnArgs& a, int D, bool mx, const Attn
 }
 
 hipError_t launch_attn_few(const AttnArgs& a, int D, bool mx, const AttnPlan& plan, hipStream_t st);
+hipError_t launch_attn_mixed(const AttnArgs& a, int D, const AttnPlan& plan, hipStream_t st);
 hipError_t launch_attn_shared(const AttnArgs& a, int D, bool mx, const AttnPlan& plan, hipStream_t st);
 hipError_t launch_attn_merge(const AttnArgs& a, int D, hipStream_t st);
 
@@ -31,13 +32,14 @@ hipError_t launch_attention(const uint16_t* q, int64_t ldq, uint16_t* o, int64_t
                             const int32_t* prefix_table, int prefix_len, int q_heads, int D, bool mx, int window,
                             int sinks, float scale, void* ws, hipStream_t st) {
   const int64_t items = (int64_t)b.rows * q_heads;
-  AttnArgs a{q, ldq, o, ldo, lse, b, c, prefix_table, prefix_len, plan.shared ? prefix_len : 0, q_heads / c.heads,
-             q_heads, window, sinks, (float)((double)scale * 1.4426950408889634),
-             static_cast<float2*>(ws), nullptr, plan.slots};
+  AttnArgs a{q, ldq, o, ldo, lse, b, c, prefix_table, prefix_len, plan.shared ? prefix_len : 0,
+             plan.mixed ? 16 : 0, q_heads / c.heads, q_heads, window, sinks,
+             (float)((double)scale * 1.4426950408889634), static_cast<float2*>(ws), nullptr, plan.slots};
   if (plan.slots) a.po = reinterpret_cast<float*>(static_cast<char*>(ws) + attn_ml_bytes(items, plan.slots));
-  const hipError_t e = plan.shared ? launch_attn_shared(a, D, mx, plan, st)
-                       : plan.few  ? launch_attn_few(a, D, mx, plan, st)
-                                   : launch_attn_rows(a, D, mx, plan.own, st);
+  const hipError_t e = plan.shared  ? launch_attn_shared(a, D, mx, plan, st)
+                       : plan.mixed ? launch_attn_mixed(a, D, plan, st)
+                       : plan.few   ? launch_attn_few(a, D, mx, plan, st)
+                                    : launch_attn_rows(a, D, mx, plan.own, st);
   if (e != hipSuccess || plan.slots == 0) return e;
   return launch_attn_merge(a, D, st);
 }

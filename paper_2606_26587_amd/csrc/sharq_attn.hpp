@@ -20,6 +20,7 @@ struct AttnArgs {
   const int32_t* prefix_table;
   int prefix_len;
   int t0;            // a sequence's own part begins at this token: prefix_len, or 0 (the whole sequence)
+  int few_rows;      // sequences of up to this many rows to a key/value head are not the many-row kernel's
   int group, q_heads, window, sinks;
   float scale;       // of the scores, times log2 e
   // partial results, where the tokens of a row are split over workgroups: slot

@@ -53,8 +53,8 @@ __device__ __forceinline__ void attn_few(const AttnArgs& a, int block, int chunk
   const int head = block % a.c.heads;
   const int sc = block / a.c.heads, seq = sc % a.b.seqs, chunk = sc / a.b.seqs;
   const SeqRows sr = seq_rows(a.b, seq);
-  if (sr.n == 0) return;
-  const int base = sr.len - sr.n, rows = sr.n * a.group < 16 * NQ ? sr.n * a.group : 16 * NQ;
+  if (sr.n == 0 || sr.n * a.group > 16 * NQ) return;
+  const int base = sr.len - sr.n, rows = sr.n * a.group;
   const int p_hi = sr.len - 1;
   const KvSpan span = kv_span(a.t0, sr.len, base, p_hi, a.window, a.sinks, kTok);
   const int first = chunk * chunk_tiles, last = span.n < first + chunk_tiles ? span.n : first + chunk_tiles;

@@ -53,14 +53,14 @@ constexpr int kT = kAttnTile;        // tokens of a key/value tile
 constexpr int kRowsA = kAttnRows;    // rows of a workgroup: 32 a wavefront
 
 // Sequence (and its rows) and tile of work unit `unit` of tiles of kRowsA rows; false: none.
-__device__ __forceinline__ bool find_tile(const KvBatchArgs& b, int group, int unit, int& seq, SeqRows& sr, int& tile) {
+__device__ __forceinline__ bool find_tile(const KvBatchArgs& b, int group, int few_rows, int unit, int& seq, SeqRows& sr, int& tile) {
   const int lane = (int)(threadIdx.x & 63);
   int base = 0;
   for (int s0 = 0; s0 < b.seqs; s0 += 64) {
     const int s = s0 + lane;
     SeqRows r{0, 0, 0};
     if (s < b.seqs) r = seq_rows(b, s);
-    const int n = (r.n * group + kRowsA - 1) / kRowsA;
+    const int n = r.n * group > few_rows ? (r.n * group + kRowsA - 1) / kRowsA : 0;
     int sum = n;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
@@ -115,7 +115,7 @@ __device__ __forceinline__ void attn_rows(const AttnArgs& a, int block, int tile
   } else {
     int tile;
     SeqRows sr;
-    if (!find_tile(a.b, a.group, unit, seq, sr, tile)) return;
+    if (!find_tile(a.b, a.group, a.few_rows, unit, seq, sr, tile)) return;
     const int r0 = tile * kRowsA, total = sr.n * a.group;
     const int base = sr.len - sr.n;   // position of the sequence's first row
     rows = total - r0 < kRowsA ? total - r0 : kRowsA;

@@ -33,6 +33,27 @@ __global__ __launch_bounds__(256, 2) void k_attn_shared(AttnArgs a, AttnSplit pr
   else attn_few<D, MX, NQ, NT>(a, block - prefix_blocks, chunk_tiles, 0, lds.few);
 }
 
+// Prompts and single tokens over an MXFP4 cache in one call, none of them split: the tiles of 128 rows first, then a
+// workgroup for each sequence of few rows.
+template <int D>
+__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void k_attn_mixed(AttnArgs a, int rows_blocks, int tiles) {
+  __shared__ union {
+    RowsLds<D> rows;
+    FewLds<D> few;
+  } lds;
+  const int block = (int)blockIdx.x;
+  if (block < rows_blocks) attn_rows<D, true, false>(a, block, tiles, 1 << 30, 0, lds.rows);
+  else attn_few<D, true, 1, 2>(a, block - rows_blocks, 1 << 30, 0, lds.few);
+}
+
+hipError_t launch_attn_mixed(const AttnArgs& a, int D, const AttnPlan& p, hipStream_t st) {
+  const int first = p.own.tiles * a.c.heads;
+  const dim3 g((unsigned)first + (unsigned)a.b.seqs * (unsigned)a.c.heads);
+  if (D == 128) k_attn_mixed<128><<<g, 256, 0, st>>>(a, first, p.own.tiles);
+  else k_attn_mixed<64><<<g, 256, 0, st>>>(a, first, p.own.tiles);
+  return hipGetLastError();
+}
+
 template <int D, bool MX>
 static void shared(const AttnArgs& a, const AttnPlan& p, hipStream_t st) {
   constexpr int NT = MX ? 2 : 1;

@@ -80,6 +80,7 @@ struct AttnPlan {
   bool shared;      // the prefix is read for all sequences together
   AttnSplit own, prefix;
   int slots;        // partial results of a row; 0: none, results are final
+  bool mixed;       // sequences of few rows and of many, each by its kernel
 };
 
 // Splits kv_tiles of each of `units` workgroups so that about `want` workgroups
@@ -138,6 +139,11 @@ constexpr AttnPlan attn_plan(int64_t seqs, int64_t rows, int64_t max_rows, int64
     likely = likely < seqs ? seqs : likely;
     const int64_t units = (likely < tiles ? likely : tiles) * heads;
     p.own = attn_split(tiles, units, kv, D == 64 ? 1024 : 512, 4);
+    // The longest sequences far above the mean: most of the others may have a token each, on which the kernel for many
+    // rows spends a whole tile's dequantization.  A prompt of 2000 and 63 single tokens over 4000 in MXFP4 155 us
+    // without and 111 with both kernels in one launch; 20 prompts of 125 to 2000 245 and 247.  (bf16: 240 and 226, but
+    // a chunk of 512 and 31 single tokens over 8000 238 and 251.)
+    p.mixed = mx && !p.shared && p.own.chunks == 1 && 3 * rows < 2 * seqs * max_rows;
   }
   p.slots = p.own.chunks > 1 ? p.own.chunks : 0;
   if (p.shared) {

@@ -216,6 +216,19 @@ def test_rows_around_the_limits_of_the_kernels(new, prefix, D, fmt):
 
 
 @pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("D,hkv,group", [(128, 8, 4), (64, 16, 4), (128, 8, 1), (128, 4, 16), (64, 16, 17)])
+@pytest.mark.parametrize("window,sinks,prefix", [(0, 0, 0), (37, 3, 0), (50, 0, 48)])
+def test_prompts_and_single_tokens_in_one_call(window, sinks, prefix, D, hkv, group, fmt):
+    """Many sequences of one or a few rows beside some of many: on an MXFP4 cache each kind has its kernel, in one launch."""
+    new = [150, 1, 0, 4, 5, 1, 16, 17, 1, 64] + [1] * 60
+    lens = [150, 200, 80, 90, 5, 1, 130, 70, 64, 300] + [48 + 3 * i for i in range(60)]
+    if prefix:
+        lens = [max(n, prefix + 1) for n in lens]
+    table_of = dict(bad_pages=[(1, 2, -1), (12, 0, 0)]) if not prefix else {}
+    run(new, lens, 16, hkv * group, hkv, D, fmt, window=window, sinks=sinks, prefix_len=prefix, pad=11, **table_of)
+
+
+@pytest.mark.parametrize("fmt", FMTS)
 @pytest.mark.parametrize("count", [65, 130, 200])
 def test_more_sequences_than_a_wavefront(count, fmt):
     rng = np.random.default_rng(count)

@@ -36,6 +36,11 @@ int64_t plan(int64_t seqs, int64_t rows, int64_t max_rows, int64_t max_len, int 
   for (int i = 0; i < 9; ++i) out[i] = v[i];
   return attn_workspace(rows * heads * group, p.slots, D);
 }
+int mixed(int64_t seqs, int64_t rows, int64_t max_rows, int64_t max_len, int heads, int group, int D, int mx,
+          int64_t window, int64_t sinks, int64_t prefix) {
+  const AttnPlan p = attn_plan(seqs, rows, max_rows, max_len, heads, group, D, mx, window, sinks, prefix);
+  return p.mixed ? 1 + (p.few || p.shared || p.slots) : 0;   // 2: a plan that may not be
+}
 int tile_rows() { return kAttnRows; }
 int tile_tokens() { return kAttnTile; }
 }
@@ -169,6 +174,26 @@ def test_plans_cover_every_tile_of_every_row(kv):
             assert window >= max_len and pre_tiles * R >= int(n.sum()) * group
             assert -(-prefix // T) <= pre_chunks * pre_each
     assert {k[0] for k in kinds} == {0, 1, 2, 4} and {k[1:] for k in kinds} == {(0, False), (0, True), (1, True)}
+
+
+def test_mixed_plans(kv):
+    """Both kernels in one launch: unsplit batches of some long and many short sequences on an MXFP4 cache, no others."""
+    kv.mixed.argtypes = [ctypes.c_int64] * 4 + [ctypes.c_int] * 4 + [ctypes.c_int64] * 3
+    big = 2 ** 31 - 1
+    assert kv.mixed(64, 2063, 2000, 4000, 8, 4, 128, 1, big, 0, 0) == 1
+    assert kv.mixed(64, 2063, 2000, 4000, 8, 4, 128, 1, 100, 4, 1024) == 1      # a window: the prefix is like any page
+    assert kv.mixed(64, 2063, 2000, 4000, 8, 4, 128, 0, big, 0, 0) == 0         # bf16
+    assert kv.mixed(64, 2063, 2000, 4000, 8, 4, 128, 1, big, 0, 1024) == 0      # a shared prefix
+    assert kv.mixed(64, 100000, 2000, 4000, 8, 4, 128, 1, big, 0, 0) == 0       # of about the same lengths
+    assert kv.mixed(64, 64, 1, 4000, 8, 4, 128, 1, big, 0, 0) == 0              # few rows all
+    assert kv.mixed(2, 2001, 2000, 4000, 1, 4, 128, 1, big, 0, 0) == 0          # split
+    rng = np.random.default_rng(5)
+    for _ in range(3000):
+        seqs, most = int(rng.integers(1, 3000)), int(rng.integers(1, 5000))
+        got = kv.mixed(seqs, int(rng.integers(most, seqs * most + 1)), most, most + int(rng.integers(0, 9000)),
+                       int(rng.integers(1, 17)), int(rng.integers(1, 33)), int(rng.choice([64, 128])),
+                       int(rng.integers(2)), int(rng.choice([big, 50])), int(rng.integers(0, 9)), 0)
+        assert got in (0, 1)
 
 
 # ---------------------------------------------------------------------------
