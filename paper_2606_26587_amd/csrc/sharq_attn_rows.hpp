@@ -52,8 +52,10 @@ constexpr int kSchedMfma = 0x8, kSchedLdsRead = 0x100;   // kinds of instruction
 constexpr int kT = kAttnTile;        // tokens of a key/value tile
 constexpr int kRowsA = kAttnRows;    // rows of a workgroup: 32 a wavefront
 
-// Sequence (and its rows) and tile of work unit `unit` of tiles of kRowsA rows; false: none.
-__device__ __forceinline__ bool find_tile(const KvBatchArgs& b, int group, int few_rows, int unit, int& seq, SeqRows& sr, int& tile) {
+// Sequence (and its rows) and tile of work unit `unit` of tiles of kRowsA rows, over the sequences of more than
+// few_rows rows; false: none.
+__device__ __forceinline__ bool find_tile(const KvBatchArgs& b, int group, int few_rows, int unit, int& seq, SeqRows& sr,
+                                          int& tile) {
   const int lane = (int)(threadIdx.x & 63);
   int base = 0;
   for (int s0 = 0; s0 < b.seqs; s0 += 64) {
@@ -234,7 +236,8 @@ __device__ __forceinline__ void attn_rows(const AttnArgs& a, int block, int tile
       const int row = 16 * wave + mx_row, c0 = 4 * mx_block;
       const Codes& x = ahead[stage];
       const bool dead = !((live >> row) & 1);
-      const uint32_t ks = dead ? 0 : x.ks >> (8 * (mx_byte & 3)) & 0xFF, vs = dead ? 0 : x.vs >> (8 * (mx_byte & 3)) & 0xFF;
+      const int at = 8 * (mx_byte & 3);
+      const uint32_t ks = dead ? 0 : x.ks >> at & 0xFF, vs = dead ? 0 : x.vs >> at & 0xFF;
       const uint32_t kw[4] = {x.k.x, x.k.y, x.k.z, x.k.w}, vw[4] = {x.v.x, x.v.y, x.v.z, x.v.w};
 #pragma unroll
       for (int e = 0; e < 4; ++e) {   // zero codes times 2^-127

@@ -123,7 +123,7 @@ constexpr AttnPlan attn_plan(int64_t seqs, int64_t rows, int64_t max_rows, int64
     const int64_t units = seqs * heads, turns = units * ceil_div(kv, 4);
     // Where one round leaves a third of the chip idle, two: 33 x 1500 single tokens in bf16 47.2 and 36.9 us, 40 x 1500
     // 45.6 and 39.9; 33 x 8 tokens over 5000 in MXFP4 68.1 and 55.1.  (With 480 of 512 places taken the same loses 10%.)
-    const bool idle = units > 256 && units <= 341 && turns >= (lean ? 3072 : 4096);
+    const bool idle = units > 256 && units <= 341 && turns >= (lean ? 3000 : 4000);
     const int want = p.shared ? 512 : lean && turns >= 6144 ? 2048 : idle ? 1024 : mx && p.few == 1 ? 768 : 512;
     p.own = attn_split(1, units, kv, want, 4);
   } else {
