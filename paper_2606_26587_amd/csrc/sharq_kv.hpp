@@ -139,6 +139,14 @@ constexpr AttnPlan attn_plan(int64_t seqs, int64_t rows, int64_t max_rows, int64
     likely = likely < seqs ? seqs : likely;
     const int64_t units = (likely < tiles ? likely : tiles) * heads;
     p.own = attn_split(tiles, units, kv, D == 64 ? 1024 : 512, 4);
+    // Not where the partial results take longer than what the split saves of the longest walk: ns of a tile, alone on its
+    // CU or not, and of a row and head's partial result, written and read.  A prompt of 1024, 32 query heads of 128:
+    // 36.0 us split in two, 27.5 whole; 4 x 300, 16 query heads, 19.0 in five parts, 11.9 whole.
+    const int64_t alone = D == 64 ? 1250 : 1400, among = D == 64 ? 1900 : 2100;
+    const int64_t whole = kv * (units > 256 ? among : alone);
+    const int64_t split = p.own.chunk_tiles * (units * p.own.chunks > 256 ? among : alone) + 4000 +
+                          rows * heads * group * p.own.chunks * (D + 2) * 2 * 4 / 4500;
+    if (whole <= split) p.own = attn_split(tiles, units, kv, 1, 4);
     // The longest sequences far above the mean: most of the others may have a token each, on which the kernel for many
     // rows spends a whole tile's dequantization.  A prompt of 2000 and 63 single tokens over 4000 in MXFP4 155 us
     // without and 111 with both kernels in one launch; 20 prompts of 125 to 2000 245 and 247.  (bf16: 240 and 226, but
