@@ -158,7 +158,12 @@ constexpr AttnPlan attn_plan(int64_t seqs, int64_t rows, int64_t max_rows, int64
     const int64_t tiles = ceil_div(rows * group, kAttnRows);
     // 64 tokens behind 8192: 41.9 us with 256 workgroups, 46.4 with 384, 54.1 with 512; 40.4 with 192, but 16 behind
     // 32768 then 47.8 against 43.3
-    p.prefix = attn_split(tiles, tiles * heads, ceil_div(prefix_len, kAttnTile), 256, 2);
+    const int64_t kv = ceil_div(prefix_len, kAttnTile), units = tiles * heads;
+    p.prefix = attn_split(tiles, units, kv, 256, 2);
+    // Where that leaves long walks (then the partial results weigh less), twice as many: 32 x up to 32 tokens behind 4096,
+    // 32 and 8 heads of 128, 94.7 and 82.8 us, behind 16384 339 and 258; 4 single tokens behind 61440 in MXFP4 48.4 and
+    // 35.2; 256 behind 16384 118 and 122, in MXFP4 106 and 103.  (8 x 100 behind 2048, 32 tiles: 39.5 and 45.2.)
+    if (kv >= 48 && p.prefix.chunk_tiles >= 28) p.prefix = attn_split(tiles, units, kv, 512, 2);
     p.slots = p.own.chunks + p.prefix.chunks;
   }
   return p;
