@@ -256,7 +256,7 @@ class KVBatch:
     """The sequences of a call (sharq_kv_batch): row_offsets int32 [seqs + 1], lens
     int32 [seqs] (the call's rows among them), page_table int32 [seqs, n], on the
     GPU; the rows of the row tensors, and the host's bounds of a sequence's rows and
-    length."""
+    length (max_len at most n pages)."""
     row_offsets: torch.Tensor
     lens: torch.Tensor
     page_table: torch.Tensor
@@ -278,7 +278,11 @@ class KVBatch:
         ld = self.page_table.stride(0) if seqs > 1 else self.page_table.shape[1]
         struct = KVBatchStruct(seqs, self.rows, self.max_rows, self.max_len, ld, self.row_offsets.data_ptr(),
                                self.lens.data_ptr(), self.page_table.data_ptr())
-        self.__dict__.update(device_index=self.lens.get_device(), ref=ctypes.byref(struct))
+        # the library is told the stride alone: that the table is as wide as max_len takes is checked here, per call
+        # (the page size is the cache's); where nothing is looked up, any width will do
+        least = -1 if seqs == 0 or self.rows == 0 else self.max_len
+        self.__dict__.update(device_index=self.lens.get_device(), table_pages=self.page_table.shape[1],
+                             table_tokens=least, ref=ctypes.byref(struct))
 
 
 def alloc_kv_cache(pages: int, page_size: int, kv_heads: int, head_dim: int, fmt: str = "bf16", device="cuda",
@@ -471,6 +475,13 @@ def _here(cache: KVCache, batch: KVBatch, where: str):
         raise SharqError(EINVAL, where)
 
 
+def _table(cache: KVCache, batch: KVBatch, where: str):
+    """Every token that the call may look up has a column in the page table.  A table that is a slice of a wider one has
+    a stride above its width: behind a row's own entries come the parent's, and behind the last row's perhaps nothing."""
+    if batch.table_tokens > batch.table_pages * cache.page_size:
+        raise SharqError(EINVAL, where)
+
+
 def sharq_kv_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, cache: KVCache, batch: KVBatch,
                     cos: Optional[torch.Tensor] = None, sin: Optional[torch.Tensor] = None,
                     positions: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
@@ -480,6 +491,7 @@ def sharq_kv_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor,
     Returns the rotated queries (q_out; `q` itself for an in-place update), None without q."""
     where = "sharq_kv_append"
     _here(cache, batch, where)
+    _table(cache, batch, where)
     rows, dev = batch.rows, cache.device_index
     ldk, ldv = _rows(k, rows, cache.width, dev, where), _rows(v, rows, cache.width, dev, where)
     heads = ldq = ldo = angles = 0
@@ -516,6 +528,7 @@ def sharq_kv_read(cache: KVCache, batch: KVBatch, k_out: Optional[torch.Tensor] 
     """The rows' cached keys and values as bf16 [rows, kv_heads * head_dim] (padding rows are left as they are)."""
     where = "sharq_kv_read"
     _here(cache, batch, where)
+    _table(cache, batch, where)
     shape = (batch.rows, cache.width)
     if k_out is None:
         k_out = torch.empty(shape, dtype=_BF, device=cache.k.device)
@@ -550,6 +563,7 @@ def sharq_attention(q: torch.Tensor, cache: KVCache, batch: KVBatch, scale: Opti
     when given.  workspace: a buffer of attention_workspace_bytes, allocated here when needed and None."""
     where = "sharq_attention"
     _here(cache, batch, where)
+    _table(cache, batch, where)
     rows, dev, width = batch.rows, cache.device_index, q.shape[-1]
     heads, rest = divmod(width, cache.head_dim)
     ldq = _rows(q, rows, width, dev, where)
