@@ -2,12 +2,16 @@
 
 Argument marshalling only: buffers are torch tensors on the GPU (torch is used
 for device memory and streams), every computation runs in the library's
-kernels.  Importing this module raises if the library has not been built;
+kernels.  A call runs on `stream` (a torch.cuda.Stream; None: the current one),
+and the buffers that it is not given are allocated there: like any tensor of
+that stream, they are marked with record_stream before they are dropped while
+another stream still uses them.  Importing this module raises if the library has not been built;
 there is no fallback path.
 """
 
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import functools
 import os
@@ -154,6 +158,16 @@ _current = _stream_handle()
 
 def _stream(stream):
     return _current() if stream is None else stream.cuda_stream
+
+
+_CURRENT = contextlib.nullcontext()
+
+
+def _on(stream):
+    """The context in which a call allocates its buffers: its own stream, whose work in the order of the calls is what
+    the allocator relies on when it hands a block out again.  (From another stream's blocks one could come whose last
+    reader there is still to run.)"""
+    return _CURRENT if stream is None else torch.cuda.stream(stream)
 
 
 # ---------------------------------------------------------------------------
@@ -345,7 +359,8 @@ def sharq_quantize_weight(w: torch.Tensor, fmt="mx", out: Optional[QuantWeight] 
     (scale_rule: the MXFP4 E8M0 rule, ignored when `out` is given)."""
     N, K = w.shape
     if out is None:
-        out = alloc_weight(N, K, fmt, 1, w.device, scale_rule)
+        with _on(stream):
+            out = alloc_weight(N, K, fmt, 1, w.device, scale_rule)
     ws = out.struct()
     _check(lib.sharq_quantize_weight(_ptr(w), _DT.get(w.dtype, -1), N, K, w.stride(0), ctypes.byref(ws),
                                      _stream(stream)), "sharq_quantize_weight")
@@ -361,7 +376,8 @@ def sharq_prepare(x: torch.Tensor, gamma: Optional[torch.Tensor], eps: float = 1
     ignored when `out` is given, which carries them."""
     M, K = x.shape
     if out is None:
-        out = alloc_act(M, K, n, m, fmt, x.device, pairs, mode, scale_rule=scale_rule)
+        with _on(stream):
+            out = alloc_act(M, K, n, m, fmt, x.device, pairs, mode, scale_rule=scale_rule)
     f = _FMT[fmt] if isinstance(fmt, str) else fmt
     st = out.struct()
     _check(lib.sharq_prepare(_ptr(x), _DT.get(x.dtype, -1), M, K, x.stride(0), _ptr(gamma), eps,
@@ -379,9 +395,11 @@ def sharq_prepare_residual(x: torch.Tensor, residual: torch.Tensor, gamma: Optio
     update) and prepared.  Returns (prepared activation, h)."""
     M, K = x.shape
     if out is None:
-        out = alloc_act(M, K, n, m, fmt, x.device, pairs)
+        with _on(stream):
+            out = alloc_act(M, K, n, m, fmt, x.device, pairs)
     if h_out is None:
-        h_out = torch.empty_like(x)
+        with _on(stream):
+            h_out = torch.empty_like(x)
     f = _FMT[fmt] if isinstance(fmt, str) else fmt
     st = out.struct()
     _check(lib.sharq_prepare_residual(_ptr(x), _ptr(residual), _ptr(h_out), _DT.get(x.dtype, -1), M, K, x.stride(0),
@@ -398,7 +416,8 @@ def sharq_prepare_silu_mul(gate: torch.Tensor, up: torch.Tensor, n: int = 2, m: 
     h = bf16(SiLU(gate) * up) is prepared (and written to h_out when given)."""
     M, K = gate.shape
     if out is None:
-        out = alloc_act(M, K, n, m, fmt, gate.device, pairs)
+        with _on(stream):
+            out = alloc_act(M, K, n, m, fmt, gate.device, pairs)
     f = _FMT[fmt] if isinstance(fmt, str) else fmt
     st = out.struct()
     _check(lib.sharq_prepare_silu_mul(_ptr(gate), _ptr(up), _ptr(h_out), _DT.get(gate.dtype, -1), M, K,
@@ -412,7 +431,8 @@ def sharq_linear(a: PreparedAct, w: QuantWeight, out: Optional[torch.Tensor] = N
                  stream=None) -> torch.Tensor:
     """Y [rows, N] = backbone GEMM + residual GEMM over the shared weight."""
     if out is None:
-        out = torch.empty((a.rows, w.N), dtype=dtype, device=a.dn_codes.device)
+        with _on(stream):
+            out = torch.empty((a.rows, w.N), dtype=dtype, device=a.dn_codes.device)
     ast, wst = a.struct(), w.struct()
     _check(lib.sharq_linear(ctypes.byref(ast), ctypes.byref(wst), _ptr(out), _DT.get(out.dtype, -1),
                             out.stride(0) if out.dim() == 2 else w.N, _stream(stream)), "sharq_linear")
@@ -427,9 +447,11 @@ def sharq_prepare_linear(x: torch.Tensor, gamma: Optional[torch.Tensor], w: Quan
     (one kernel for a few rows).  Returns (prepared activation, Y)."""
     M, K = x.shape
     if act is None:
-        act = alloc_act(M, K, n, m, fmt, x.device, pairs, scale_rule=scale_rule)
+        with _on(stream):
+            act = alloc_act(M, K, n, m, fmt, x.device, pairs, scale_rule=scale_rule)
     if out is None:
-        out = torch.empty((M, w.N), dtype=dtype, device=x.device)
+        with _on(stream):
+            out = torch.empty((M, w.N), dtype=dtype, device=x.device)
     f = _FMT[fmt] if isinstance(fmt, str) else fmt
     ast, wst = act.struct(), w.struct()
     _check(lib.sharq_prepare_linear(_ptr(x), _DT.get(x.dtype, -1), M, K, x.stride(0), _ptr(gamma), eps,
@@ -444,7 +466,8 @@ def sharq_linear_grouped(a: PreparedAct, row_index: Optional[torch.Tensor], expe
                          stream=None) -> torch.Tensor:
     """Mixture-of-experts form: Y[i] = SharQ(A[row_index[i]], W_e) for i in expert e's slice."""
     if out is None:
-        out = torch.empty((total, w.N), dtype=dtype, device=a.dn_codes.device)
+        with _on(stream):
+            out = torch.empty((total, w.N), dtype=dtype, device=a.dn_codes.device)
     ast, wst = a.struct(), w.struct()
     _check(lib.sharq_linear_grouped(ctypes.byref(ast), _ptr(row_index), _ptr(expert_offsets), total,
                                     ctypes.byref(wst), _ptr(out), _DT.get(out.dtype, -1),
@@ -502,7 +525,8 @@ def sharq_kv_append(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor,
         if rest:
             raise SharqError(EINVAL, where)
         if q_out is None:
-            q_out = torch.empty((rows, width), dtype=q.dtype, device=q.device)
+            with _on(stream):
+                q_out = torch.empty((rows, width), dtype=q.dtype, device=q.device)
         ldo = _rows(q_out, rows, width, dev, where)
     if (cos is None) != (sin is None):
         raise SharqError(EINVAL, where)
@@ -531,9 +555,11 @@ def sharq_kv_read(cache: KVCache, batch: KVBatch, k_out: Optional[torch.Tensor] 
     _table(cache, batch, where)
     shape = (batch.rows, cache.width)
     if k_out is None:
-        k_out = torch.empty(shape, dtype=_BF, device=cache.k.device)
+        with _on(stream):
+            k_out = torch.empty(shape, dtype=_BF, device=cache.k.device)
     if v_out is None:
-        v_out = torch.empty(shape, dtype=_BF, device=cache.k.device)
+        with _on(stream):
+            v_out = torch.empty(shape, dtype=_BF, device=cache.k.device)
     ldk, ldv = (_rows(t, *shape, cache.device_index, where) for t in (k_out, v_out))
     _check(lib.sharq_kv_read(cache.ref, batch.ref, k_out.data_ptr(), ldk, v_out.data_ptr(), ldv, BF16,
                              _stream(stream)), where)
@@ -570,7 +596,8 @@ def sharq_attention(q: torch.Tensor, cache: KVCache, batch: KVBatch, scale: Opti
     if rest:
         raise SharqError(EINVAL, where)
     if out is None:
-        out = torch.empty((rows, width), dtype=q.dtype, device=q.device)
+        with _on(stream):
+            out = torch.empty((rows, width), dtype=q.dtype, device=q.device)
     ldo = _rows(out, rows, width, dev, where)
     if lse is not None and (lse.dtype is not torch.float32 or lse.shape != (rows, heads) or not lse.is_contiguous()
                             or lse.get_device() != dev):
@@ -588,8 +615,8 @@ def sharq_attention(q: torch.Tensor, cache: KVCache, batch: KVBatch, scale: Opti
     size = 0
     if workspace is None:
         size = lib.sharq_attention_workspace_bytes(cache.ref, batch.ref, ts, heads)
-        if size:   # on the stream that uses it: freed on return, and taken again only behind the call
-            with torch.cuda.stream(stream):
+        if size:   # freed on return, and taken again only behind the call
+            with _on(stream):
                 workspace = torch.empty(size, dtype=torch.uint8, device=q.device)
     elif workspace.get_device() != dev or not workspace.is_contiguous():
         raise SharqError(EINVAL, where)
