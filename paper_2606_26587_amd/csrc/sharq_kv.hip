@@ -44,8 +44,6 @@ __device__ __forceinline__ uint32_t kv_quantize8(const float* x, uint32_t rule_b
   return (uint32_t)(e + 127);
 }
 
-constexpr int kAppendThreads = 128;
-
 // A thread takes 8 values of a head's first half and the 8 that pair with them.
 // Workgroup b: row b / parts, threads of its part of the row's heads.
 template <int D, bool MX>
@@ -120,8 +118,6 @@ __global__ __launch_bounds__(kAppendThreads) void k_kv_append(KvAppendArgs a, Kv
                                                           bf16x2(hi[4], hi[5]), bf16x2(hi[6], hi[7]));
 }
 
-constexpr int kReadThreads = 128;
-
 // A thread reads 8 values; workgroup b: row b / parts, as above.
 template <int D, bool MX>
 __global__ __launch_bounds__(kReadThreads) void k_kv_read(uint16_t* ko, int64_t ldk, uint16_t* vo, int64_t ldv,
@@ -156,7 +152,7 @@ hipError_t launch_kv_append(const uint16_t* q, const uint16_t* k, const uint16_t
                             int angles, const int32_t* pos, uint32_t rule_bias, const KvBatchArgs& b,
                             const KvCacheArgs& c, int D, bool mx, hipStream_t st) {
   KvAppendArgs a{q, k, v, ldq, ldk, ldv, qo, ldqo, cos, sin, pos, angles, q_heads, 0, rule_bias};
-  a.parts = ((q_heads + 2 * c.heads) * (D / 16) + kAppendThreads - 1) / kAppendThreads;
+  a.parts = kv_append_parts(q_heads, c.heads, D);
   const dim3 g((unsigned)b.rows * (unsigned)a.parts), t(kAppendThreads);
   if (D == 128)
     mx ? k_kv_append<128, true><<<g, t, 0, st>>>(a, b, c) : k_kv_append<128, false><<<g, t, 0, st>>>(a, b, c);
@@ -167,7 +163,7 @@ hipError_t launch_kv_append(const uint16_t* q, const uint16_t* k, const uint16_t
 
 hipError_t launch_kv_read(uint16_t* ko, int64_t ldk, uint16_t* vo, int64_t ldv, const KvBatchArgs& b,
                           const KvCacheArgs& c, int D, bool mx, hipStream_t st) {
-  const int parts = (2 * c.heads * (D / 8) + kReadThreads - 1) / kReadThreads;
+  const int parts = kv_read_parts(c.heads, D);
   const dim3 g((unsigned)b.rows * (unsigned)parts), t(kReadThreads);
   if (D == 128)
     mx ? k_kv_read<128, true><<<g, t, 0, st>>>(ko, ldk, vo, ldv, parts, b, c)

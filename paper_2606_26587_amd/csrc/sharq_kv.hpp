@@ -61,6 +61,21 @@ constexpr int kv_tile_start(const KvSpan& s, int t0, int i, int T) {
 }
 
 // ---------------------------------------------------------------------------
+// Launches of the append and the read-back
+// ---------------------------------------------------------------------------
+
+constexpr int kAppendThreads = 128, kReadThreads = 128;
+
+// Workgroups of a row: a thread takes 16 values in the append, 8 in the read-back.
+constexpr int kv_append_parts(int q_heads, int heads, int D) {
+  return ((q_heads + 2 * heads) * (D / 16) + kAppendThreads - 1) / kAppendThreads;
+}
+constexpr int kv_read_parts(int heads, int D) { return (2 * heads * (D / 8) + kReadThreads - 1) / kReadThreads; }
+
+// A launch has fewer than 2^32 threads.
+constexpr bool kv_launches(int64_t blocks, int threads) { return blocks <= 0xFFFFFFFFll / threads; }
+
+// ---------------------------------------------------------------------------
 // Work split of the attention
 // ---------------------------------------------------------------------------
 

@@ -28,7 +28,7 @@ constexpr int64_t kMaxSeqs = (int64_t)1 << 16;
 constexpr int64_t kMaxHeads = 1024;
 constexpr int64_t kMaxGroup = 128;
 constexpr float kMinScale = 0x1p-100f, kMaxScale = 0x1p100f;   // scale times log2 e and times a maximum's start stay normal
-constexpr int64_t kMaxHeadRows = (int64_t)1 << 26;   // rows times heads of a call: launches stay below 2^31 threads
+constexpr int64_t kMaxHeadRows = (int64_t)1 << 26;   // rows times heads of a call: row and head numbers fit 27 bits
 
 bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 bool row_aligned(const void* p, int64_t ld) { return aligned(p, 16) && (ld * 2) % 16 == 0; }
@@ -142,6 +142,9 @@ sharq_status sharq_kv_append(const void* Q, const void* K, const void* V, sharq_
       !aligned(positions, 4) || (q_heads > 0 && (!row_aligned(Q, ldq) || !row_aligned(Q_out, ldqo))))
     return SHARQ_EALIGN;
   if (batch->max_len == 0) return SHARQ_OK;   // no row has a position
+  if (!sharq::kv_launches(batch->rows * sharq::kv_append_parts((int)q_heads, cache->kv_heads, (int)D),
+                          sharq::kAppendThreads))
+    return SHARQ_EUNSUPPORTED;
   return hip_status(sharq::launch_kv_append(
       static_cast<const uint16_t*>(Q), static_cast<const uint16_t*>(K), static_cast<const uint16_t*>(V), ldq, ldk, ldv,
       (int)q_heads, static_cast<uint16_t*>(Q_out), ldqo, cos, sin, (int)angles, positions,
@@ -161,6 +164,8 @@ sharq_status sharq_kv_read(const sharq_kv_cache* cache, const sharq_kv_batch* ba
   if (batch->rows == 0 || batch->seqs == 0) return SHARQ_OK;
   if (!K || !V) return SHARQ_EINVAL;
   if (!row_aligned(K, ldk) || !row_aligned(V, ldv)) return SHARQ_EALIGN;
+  if (!sharq::kv_launches(batch->rows * sharq::kv_read_parts(cache->kv_heads, cache->head_dim), sharq::kReadThreads))
+    return SHARQ_EUNSUPPORTED;
   return hip_status(sharq::launch_kv_read(static_cast<uint16_t*>(K), ldk, static_cast<uint16_t*>(V), ldv,
                                           batch_args(batch, batch->rows), cache_args(cache), cache->head_dim,
                                           cache->fmt == SHARQ_KV_MXFP4, reinterpret_cast<hipStream_t>(stream)));
