@@ -535,8 +535,10 @@ SHARQ_API size_t sharq_attention_workspace_bytes(const sharq_kv_cache *cache, co
  *   run at the same time need workspaces of their own.
  * A row that sees no token gets O = 0 and lse = -inf.  Cache slots that no row
  * of the call sees may hold anything; the keys, values and queries that are
- * seen must be finite, their scores too.  Products are summed in fp32; the
- * weights are rounded to bf16 for the product with V, their sum is not.
+ * seen must be finite, their scores too.  (A NaN that a row sees makes that row's
+ * results NaN, a value's in its column; earlier rows of sequences that hold the
+ * token may be NaN as well.)  Products are summed in fp32; the weights are rounded
+ * to bf16 for the product with V, their sum is not.
  */
 SHARQ_API sharq_status sharq_attention(const void *Q, sharq_dtype xdt, int64_t q_heads, int64_t ldq,
                                        const sharq_kv_cache *cache, const sharq_kv_batch *batch,

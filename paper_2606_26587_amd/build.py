@@ -37,15 +37,9 @@ HIP_FLAGS = [
 ]
 
 
-# The attention's running maxima: no canonicalisation of NaNs (none is an
-# operand that counts) in front of every v_max.
-SOURCE_FLAGS = {name: ["-fno-honor-nans"] for name in ("sharq_attn.hip", "sharq_attn_few.hip", "sharq_attn_shared.hip")}
-
-
 def _compile(src: str) -> str:
-    name = os.path.basename(src)
-    obj = os.path.join(BUILD, name + ".o")
-    cmd = [HIPCC, *HIP_FLAGS, *SOURCE_FLAGS.get(name, []), "-c", src, "-o", obj]
+    obj = os.path.join(BUILD, os.path.basename(src) + ".o")
+    cmd = [HIPCC, *HIP_FLAGS, "-c", src, "-o", obj]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"hipcc failed for {src}:\n{r.stdout}\n{r.stderr}")

@@ -84,6 +84,12 @@ __device__ __forceinline__ int64_t shfl64(int64_t v, int lane) {
   return (int64_t)((uint64_t)(uint32_t)__shfl((int)v, lane) | (uint64_t)(uint32_t)__shfl((int)(v >> 32), lane) << 32);
 }
 
+// The larger of two, NaN if either is (v_maximum3_f32): a NaN that a row sees
+// stays in its maximum and its sum, so that its results are NaN however the tokens
+// are split.  (v_max_f32 drops it and, where NaNs count, costs two instructions
+// more to quiet its operands.)
+__device__ __forceinline__ float attn_max(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+
 // A row that saw nothing has sum 0 and the running maximum's start, a finite
 // number, so that no difference of maxima is a NaN.
 constexpr float kNoMax = -__FLT_MAX__;
@@ -114,7 +120,7 @@ __device__ __forceinline__ unsigned long long row_sees(unsigned long long live, 
 }
 
 __device__ __forceinline__ float attn_lse(float m, float l, float scale) {
-  return l > 0.0f ? (m * scale + __log2f(l)) * 0.69314718055994531f : -__builtin_inff();
+  return l != 0.0f ? (m * scale + __log2f(l)) * 0.69314718055994531f : -__builtin_inff();
 }
 
 }  // namespace sharq

@@ -46,13 +46,13 @@ __global__ __launch_bounds__(256) void k_attn_merge(AttnArgs a) {
         }
         float now = top;
 #pragma unroll
-        for (int i = 0; i < kTrip; ++i) now = t[i].y > 0.0f ? fmaxf(now, t[i].x) : now;
+        for (int i = 0; i < kTrip; ++i) now = t[i].y != 0.0f ? attn_max(now, t[i].x) : now;
         const float f = __builtin_amdgcn_exp2f((top - now) * a.scale);
         sum *= f, o.x *= f, o.y *= f, o.z *= f, o.w *= f;
         top = now;
 #pragma unroll
         for (int i = 0; i < kTrip; ++i) {
-          if (!(t[i].y > 0.0f)) continue;
+          if (t[i].y == 0.0f) continue;   // it saw nothing (a sum that is NaN did)
           const float e = __builtin_amdgcn_exp2f((t[i].x - now) * a.scale);
           sum += e * t[i].y;
           o.x += e * x[i].x, o.y += e * x[i].y, o.z += e * x[i].z, o.w += e * x[i].w;
@@ -66,7 +66,7 @@ __global__ __launch_bounds__(256) void k_attn_merge(AttnArgs a) {
       if (grp != 0) continue;
       top = kNoMax, sum = 0.0f, o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
-      for (int i = 0; i < kG; ++i) top = fmaxf(top, lds_s[i].x);
+      for (int i = 0; i < kG; ++i) top = attn_max(top, lds_s[i].x);
 #pragma unroll
       for (int i = 0; i < kG; ++i) {
         const float e = __builtin_amdgcn_exp2f((lds_s[i].x - top) * a.scale);
@@ -77,7 +77,7 @@ __global__ __launch_bounds__(256) void k_attn_merge(AttnArgs a) {
     } else if (item >= items) {
       continue;
     }
-    const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+    const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
     const int64_t row = item / a.q_heads, h = item % a.q_heads;
     *reinterpret_cast<uint2*>(a.o + row * a.ldo + h * D + 4 * ch) =
         make_uint2(bf16x2(o.x * inv, o.y * inv), bf16x2(o.z * inv, o.w * inv));

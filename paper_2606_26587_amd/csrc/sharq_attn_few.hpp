@@ -181,16 +181,16 @@ __device__ __forceinline__ void attn_few(const AttnArgs& a, int block, int chunk
 #pragma unroll
             for (int i = 0; i < 4; ++i) s[n][mt][i] = see & (1u << (16 * mt + i)) ? s[n][mt][i] : -__builtin_inff();
         }
-        top[n] = fmaxf(fmaxf(fmaxf(s[n][0][0], s[n][0][1]), fmaxf(s[n][0][2], s[n][0][3])),
-                       fmaxf(fmaxf(s[n][1][0], s[n][1][1]), fmaxf(s[n][1][2], s[n][1][3])));
-        top[n] = fmaxf(top[n], __shfl_xor(top[n], 16));
-        top[n] = fmaxf(top[n], __shfl_xor(top[n], 32));
+        top[n] = attn_max(attn_max(attn_max(s[n][0][0], s[n][0][1]), attn_max(s[n][0][2], s[n][0][3])),
+                       attn_max(attn_max(s[n][1][0], s[n][1][1]), attn_max(s[n][1][2], s[n][1][3])));
+        top[n] = attn_max(top[n], __shfl_xor(top[n], 16));
+        top[n] = attn_max(top[n], __shfl_xor(top[n], 32));
         moved |= (top[n] - m[n]) * a.scale > kMaxStep;
       }
       if (__any(moved)) {
 #pragma unroll
         for (int n = 0; n < NQ; ++n) {
-          top[n] = fmaxf(top[n], m[n]);
+          top[n] = attn_max(top[n], m[n]);
           const float alpha = __builtin_amdgcn_exp2f((m[n] - top[n]) * a.scale);
           m[n] = top[n];
           l[n] *= alpha;
@@ -240,7 +240,7 @@ __device__ __forceinline__ void attn_few(const AttnArgs& a, int block, int chunk
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
         s[w] = lds_ml[w][r];
-        top = fmaxf(top, s[w].x);
+        top = attn_max(top, s[w].x);
       }
       float sum = 0.0f, x0 = 0.0f, x1 = 0.0f, x2 = 0.0f, x3 = 0.0f;
 #pragma unroll
@@ -254,9 +254,9 @@ __device__ __forceinline__ void attn_few(const AttnArgs& a, int block, int chunk
       if (a.slots) {
         const int64_t at = ((int64_t)(first_slot + chunk) * a.b.rows + row_g) * a.q_heads + h;
         if (ch == 0) a.ml[at] = make_float2(top, sum);
-        if (sum > 0.0f) *reinterpret_cast<float4*>(a.po + at * D + 4 * ch) = make_float4(x0, x1, x2, x3);
+        if (sum != 0.0f) *reinterpret_cast<float4*>(a.po + at * D + 4 * ch) = make_float4(x0, x1, x2, x3);
       } else {
-        const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+        const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
         *reinterpret_cast<uint2*>(a.o + row_g * a.ldo + (int64_t)h * D + 4 * ch) =
             make_uint2(bf16x2(x0 * inv, x1 * inv), bf16x2(x2 * inv, x3 * inv));
         if (a.lse && ch == 0) a.lse[row_g * a.q_heads + h] = attn_lse(top, sum, a.scale);

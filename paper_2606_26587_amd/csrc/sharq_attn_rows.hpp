@@ -329,15 +329,15 @@ __device__ __forceinline__ void attn_rows(const AttnArgs& a, int block, int tile
 #pragma unroll
       for (int i = 2; i < 16; i += 4)
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {   // v_max3
+        for (int k = 0; k < 4; ++k) {   // v_maximum3
           const v16f& x = s[k >> 1];
           const int at0 = i + 2 * (k & 1);
-          if (at0 < 16) tops[k] = fmaxf(fmaxf(tops[k], x[at0]), x[at0 + 1]);
+          if (at0 < 16) tops[k] = attn_max(attn_max(tops[k], x[at0]), x[at0 + 1]);
         }
-      float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-      top = fmaxf(top, __shfl_xor(top, 32));
+      float top = attn_max(attn_max(tops[0], tops[1]), attn_max(tops[2], tops[3]));
+      top = attn_max(top, __shfl_xor(top, 32));
       if (__any((top - m) * a.scale > kMaxStep)) {
-        top = fmaxf(top, m);
+        top = attn_max(top, m);
         const float alpha = __builtin_amdgcn_exp2f((m - top) * a.scale);
         m = top;
         l *= alpha;
@@ -403,7 +403,7 @@ __device__ __forceinline__ void attn_rows(const AttnArgs& a, int block, int tile
     }
     return;
   }
-  const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+  const float inv = l != 0.0f ? 1.0f / l : 0.0f;
   const int64_t out = (int64_t)row_g * a.ldo + (int64_t)qh * D;
 #pragma unroll
   for (int d = 0; d < kDT; ++d)
