@@ -14,6 +14,7 @@ from __future__ import annotations
 import contextlib
 import ctypes
 import functools
+import operator
 import os
 from dataclasses import dataclass
 from typing import Optional, Sequence
@@ -568,7 +569,8 @@ def sharq_kv_read(cache: KVCache, batch: KVBatch, k_out: Optional[torch.Tensor] 
 
 @functools.lru_cache(maxsize=64)
 def _attn_ref(scale: float, window: int, sinks: int):
-    """A reference to the C structure of a call without a shared prefix: a layer's are always the same."""
+    """A reference to the C structure of a call without a shared prefix: a layer's are always the same.  Plain numbers
+    only: anything else would be kept by its identity, whatever it holds later."""
     return ctypes.byref(AttnStruct(scale, window, sinks, None, 0))
 
 
@@ -611,7 +613,7 @@ def sharq_attention(q: torch.Tensor, cache: KVCache, batch: KVBatch, scale: Opti
     if prefix_len or prefix_table is not None:
         ts = ctypes.byref(AttnStruct(scale, window, sinks, _ptr(prefix_table), prefix_len))
     else:
-        ts = _attn_ref(scale, window, sinks)
+        ts = _attn_ref(float(scale), operator.index(window), operator.index(sinks))
     size = 0
     if workspace is None:
         size = lib.sharq_attention_workspace_bytes(cache.ref, batch.ref, ts, heads)

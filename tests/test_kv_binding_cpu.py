@@ -130,3 +130,26 @@ def test_buffers_of_a_call_are_allocated_on_its_stream(lib, on_stream, monkeypat
     on_stream.clear()
     f(*args, stream=None)
     assert on_stream and all(s is None for s in on_stream)
+
+
+def test_a_scale_in_a_tensor_is_read_at_every_call(lib):
+    """A 0-d tensor's value may change between calls; the structure of a call is kept by its values, not by the object
+    that held them."""
+    cache = S.alloc_kv_cache(8, 16, 2, 64, "bf16", "cpu")
+    batch = S.KVBatch(i32(0, 1, 2), i32(1, 1), torch.zeros(2, 4, dtype=torch.int32), 2, 1, 64)
+    scale, window, sinks = torch.tensor(0.5), torch.tensor(7), torch.tensor(1)
+
+    def passed():
+        lib.calls.clear()
+        S.sharq_attention(rows(2, 256), cache, batch, scale=scale, window=window, sinks=sinks)
+        t = lib.calls[-1][1][6]._obj
+        return t.scale, t.window, t.sinks
+
+    assert passed() == (0.5, 7, 1)
+    scale.fill_(0.25)
+    window.fill_(100)
+    sinks.fill_(4)
+    assert passed() == (0.25, 100, 4)
+    assert passed() == (0.25, 100, 4)
+    with pytest.raises(TypeError):
+        S.sharq_attention(rows(2, 256), cache, batch, window=1.5)
