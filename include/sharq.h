@@ -439,7 +439,9 @@ typedef struct {
  *   seqs, rows    sequences; rows of the row tensors, at least row_offsets[seqs].
  *                 Rows behind the last sequence are padding: neither looked at
  *                 nor written.
- *   max_rows      no sequence has more rows in this call.
+ *   max_rows      no sequence has more rows in this call.  (The attention's work is
+ *                 split over the chip by max_rows and max_len: bounds far above the
+ *                 sequences' own rows and lengths cost time, and workspace.)
  *   max_len       no sequence has more tokens; max_len <= ld_table * page_size
  *                 and at most 2^30.
  *   row_offsets   device int32 [seqs + 1], non-decreasing, first 0.

@@ -30,15 +30,15 @@
 // with 4 query heads a key/value head a tile is 32 tokens, so little of a causal
 // or windowed tile is masked, and masks are formed only in tiles that need one.
 //
-// Measured (8192 tokens, 32 query and 8 key/value heads of 128, causal): 537 us,
-// 1.02 PFLOP/s, 0.84 of what a library bf16 product of 8192^3 reaches on the same
+// Measured (8192 tokens, 32 query and 8 key/value heads of 128, causal): 532 to 546
+// us across boxes, 1.02 PFLOP/s, 0.84 of what a library bf16 product of 8192^3 reaches on the same
 // card.  The matrix cores are busy half of the cycles and so is the VALU; what
 // bounds it is power: on zeros the same launch takes 424 us.  Tiles of 32 tokens
 // with three wavefronts a SIMD (586 us), the first half's exponentials beside the
 // second half's products (544, and with the maximum left out 546 against 540),
 // halves of masked tiles skipped (571) and raised priority around the products
 // (550) were measured and not kept.  Heads of 64: 830 TFLOP/s, the exponentials
-// weigh twice as much.  An MXFP4 cache costs 1% here.
+// weigh twice as much.  An MXFP4 cache costs 2.5% here (538 and 552).
 
 #pragma once
 

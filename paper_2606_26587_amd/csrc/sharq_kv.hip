@@ -1,7 +1,10 @@
 // Paged key/value cache: appending rotated keys and values, and reading them
 // back.  Both move every byte once and are bound by HBM bandwidth where rows are
-// many: 9000 rows of 32 + 8 + 8 heads of 128 (bf16, 187 MB) 36 us, 5.2 TB/s; 22000
-// into an MXFP4 cache 86 us (5.1 TB/s) and back 29 us (4.1 TB/s).  One row takes
+// many: 7445 rows of 32 + 8 + 8 heads of 128 (bf16, 187 MB) 36 us, 5.2 TB/s; 20144
+// into an MXFP4 cache 86 us (5.1 TB/s).  Read back: 22000 rows of 8 heads of 128 from
+// a bf16 cache 38.5 us (4.7 TB/s); 20144 from an MXFP4 one 28.5 us, where a row's
+// workgroup takes part of the cache lines that its neighbours take too, over
+// several XCDs: 47 MB are fetched of 22 held.  One row takes
 // 2.7 us, the chain of offsets, length, page table and store; the row's values are
 // loaded beside it.
 //

@@ -99,7 +99,11 @@ struct AttnPlan {
 };
 
 // Splits kv_tiles of each of `units` workgroups so that about `want` workgroups
-// run, each over a multiple of `least` tiles.
+// run, each over a multiple of `least` tiles.  kv_tiles follows from the host's
+// bounds: sequences far shorter than max_len fall into the first parts, and the
+// workgroups of the others end at once.  4 single tokens over 4000, 32 and 8 heads
+// of 128 in bf16: 17.4 us with max_len 4000, 23.4 with 16384, 38.6 with 131072; a
+// prompt of 512 15.5 us, 27.7 (and 34 MB of workspace) with max_len 8192.
 constexpr AttnSplit attn_split(int64_t tiles, int64_t units, int64_t kv_tiles, int64_t want, int least) {
   int64_t chunks = units > 0 ? want / units : 1;
   if (chunks > ceil_div(kv_tiles, least)) chunks = ceil_div(kv_tiles, least);
@@ -162,17 +166,20 @@ constexpr AttnPlan attn_plan(int64_t seqs, int64_t rows, int64_t max_rows, int64
     const int64_t split = p.own.chunk_tiles * (units * p.own.chunks > 256 ? among : alone) + 4000 +
                           rows * heads * group * p.own.chunks * (D + 2) * 2 * 4 / 4500;
     if (whole <= split) p.own = attn_split(tiles, units, kv, 1, 4);
-    // The longest sequences far above the mean: most of the others may have a token each, on which the kernel for many
-    // rows spends a whole tile's dequantization.  A prompt of 2000 and 63 single tokens over 4000 in MXFP4 155 us
-    // without and 111 with both kernels in one launch; 20 prompts of 125 to 2000 245 and 247.  (bf16: 240 and 226, but
-    // a chunk of 512 and 31 single tokens over 8000 238 and 251.)
+    // The mean below two thirds of the longest: some sequences may have a token each, on which the kernel for many rows
+    // spends a whole tile's dequantization.  How many do, the host does not know, and need not: the kernel for many rows
+    // alone and both in one launch, in MXFP4, 32 and 8 heads of 128: a prompt of 2000 and 63 single tokens over 4000 152
+    // and 99 us, 6 prompts of 1000 and 4 single tokens over 8000 (mean 0.6) 171 and 119, 16 of 1000 and 16 over 4000 216
+    // and 209, but 2 of 2000 and 6 over 4000 95 and 104; prompts alone, whose lengths differ, 20 of 125 to 2000 302 and
+    // 300, 1000, 400 and 300 29.2 and 28.9, heads of 64 185 and 186.  (bf16: 240 and 226, but a chunk of 512 and 31
+    // single tokens over 8000 238 and 251.)
     p.mixed = mx && !p.shared && p.own.chunks == 1 && 3 * rows < 2 * seqs * max_rows;
   }
   p.slots = p.own.chunks > 1 ? p.own.chunks : 0;
   if (p.shared) {
     const int64_t tiles = ceil_div(rows * group, kAttnRows);
-    // 64 tokens behind 8192: 41.9 us with 256 workgroups, 46.4 with 384, 54.1 with 512; 40.4 with 192, but 16 behind
-    // 32768 then 47.8 against 43.3
+    // 64 tokens behind 8192, 400 of their own each: 49.6 us with 256 workgroups, 49.8 with 384, 56.2 with 512; 44.5 with
+    // 192, but 16 behind 32768 then 45.2 against 41.4 (384: 42.4), and 40 x 4 behind 4096 in MXFP4 33.3 against 29.8
     const int64_t kv = ceil_div(prefix_len, kAttnTile), units = tiles * heads;
     p.prefix = attn_split(tiles, units, kv, 256, 2);
     // Where that leaves long walks (then the partial results weigh less), twice as many: 32 x up to 32 tokens behind 4096,

@@ -271,7 +271,8 @@ class KVBatch:
     """The sequences of a call (sharq_kv_batch): row_offsets int32 [seqs + 1], lens
     int32 [seqs] (the call's rows among them), page_table int32 [seqs, n], on the
     GPU; the rows of the row tensors, and the host's bounds of a sequence's rows and
-    length (max_len at most n pages)."""
+    length (max_len at most n pages; the attention's work is split by these bounds,
+    so far above the sequences' own they cost time)."""
     row_offsets: torch.Tensor
     lens: torch.Tensor
     page_table: torch.Tensor
