@@ -8,7 +8,7 @@
  * GEMMs that read one shared FP4 weight payload (Sec. 3.3 eqs.
  * "sharq-sparse-backbone", "sharq-quantized-backbone", "sharq-residual",
  * "sharq-output"; Sec. 3.4).  Between a decoder layer's qkv linear and its o
- * linear stand a paged key/value cache, in bf16 or in the library's MXFP4, and
+ * linear stand a paged key/value cache, in bf16, E4M3 or the library's MXFP4, and
  * the attention that reads it (sharq_kv_append, sharq_kv_read, sharq_attention).
  *
  * Conventions for every entry point
@@ -415,10 +415,18 @@ SHARQ_API sharq_status sharq_linear_grouped(const sharq_act *a, const int32_t *r
  *                      index in the low nibble) [pages][kv_heads][page_size][head_dim/2]
  *                      and k_scale, v_scale E8M0 [pages][kv_heads][page_size][head_dim/32],
  *                      one per 32 consecutive values of a token's head.
- *   scale_rule         MXFP4: the sharq_scale_rule that sharq_kv_append applies.
- *   k, v 16-byte aligned, the scales 4-byte aligned.
+ *                      SHARQ_KV_FP8: k, v E4M3 codes (OCP: bias 7, largest value 448,
+ *                      0x7F and 0xFF NaN) [pages][kv_heads][page_size][head_dim] and
+ *                      k_scale, v_scale E8M0 [pages][kv_heads][page_size/16], one for
+ *                      16 consecutive tokens of a page and head: a block.  A value is
+ *                      code * 2^(scale - 127), which is a bf16.
+ *   scale_rule         MXFP4, FP8: the sharq_scale_rule that sharq_kv_append applies.
+ *                      FP8: floor(log2 amax) - 8 (a peak above 448 * 2^e saturates), or
+ *                      ceil(log2(amax / 448)), under which nothing does; both at
+ *                      least -117.
+ *   k, v 16-byte aligned, MXFP4's scales 4-byte aligned.
  */
-typedef enum { SHARQ_KV_BF16 = 0, SHARQ_KV_MXFP4 = 1 } sharq_kv_format;
+typedef enum { SHARQ_KV_BF16 = 0, SHARQ_KV_MXFP4 = 1, SHARQ_KV_FP8 = 2 } sharq_kv_format;
 
 typedef struct {
   int64_t pages;
@@ -479,6 +487,12 @@ SHARQ_API size_t sharq_kv_buffer_bytes(const sharq_kv_cache *c, int32_t which);
  * itself with ldqo == ldq) or to the cache's format.  Values are not rotated.
  * A row at a negative position, or whose angle is not in the tables, is left
  * out: neither its query nor its key and value are written.
+ * SHARQ_KV_FP8: a block's scale is the largest that its tokens have needed.  The
+ * tokens before a sequence's first row of this call keep the scale that is there;
+ * where the new ones need a larger one, their codes are rounded again to it (which
+ * changes only values that become subnormal codes).  Bytes of the block's other
+ * slots stay.  A value that is not finite is stored as NaN and does not count for
+ * the scale.
  */
 SHARQ_API sharq_status sharq_kv_append(const void *Q, const void *K, const void *V, sharq_dtype xdt, int64_t q_heads,
                                        int64_t ldq, int64_t ldk, int64_t ldv, const float *cos, const float *sin,
@@ -489,7 +503,7 @@ SHARQ_API sharq_status sharq_kv_append(const void *Q, const void *K, const void 
  * Reads the rows' keys and values back from the cache (keys as they were
  * stored, rotated): K, V [rows][kv_heads * head_dim] bf16, row strides ldk, ldv,
  * 16-byte aligned with 16-byte row strides.  An MXFP4 value E2M1 * 2^e is a
- * bf16, so nothing is rounded.  row_offsets that cover lens read whole sequences.
+ * bf16, and so is an E4M3 code's, so nothing is rounded.  row_offsets that cover lens read whole sequences.
  */
 SHARQ_API sharq_status sharq_kv_read(const sharq_kv_cache *cache, const sharq_kv_batch *batch, void *K, int64_t ldk,
                                      void *V, int64_t ldv, sharq_dtype ydt, void *stream);

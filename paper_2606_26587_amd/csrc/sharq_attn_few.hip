@@ -5,10 +5,10 @@
 
 namespace sharq {
 
-template <int D, bool MX, int NQ, int NT>
+template <int D, int F, int NQ, int NT>
 __global__ __launch_bounds__(256, 2) void k_attn_few(AttnArgs a, int chunk_tiles, int first_slot) {
   __shared__ FewLds<D> lds;
-  attn_few<D, MX, NQ, NT>(a, (int)blockIdx.x, chunk_tiles, first_slot, lds);
+  attn_few<D, F, NQ, NT>(a, (int)blockIdx.x, chunk_tiles, first_slot, lds);
 }
 
 // Joins the partial results of a row and head.  D / 4 threads form a group; WIDE
@@ -85,21 +85,28 @@ __global__ __launch_bounds__(256) void k_attn_merge(AttnArgs a) {
   }
 }
 
-template <int D, bool MX>
+template <int D, int F>
 static void few(int nq, dim3 g, const AttnArgs& a, int chunk_tiles, hipStream_t st) {
-  constexpr int NT = MX ? 2 : 1;
-  if (nq == 1) k_attn_few<D, MX, 1, NT><<<g, 256, 0, st>>>(a, chunk_tiles, 0);
-  if constexpr (D == 64 || MX)
-    if (nq == 2) k_attn_few<D, MX, 2, NT><<<g, 256, 0, st>>>(a, chunk_tiles, 0);
-  if constexpr (D == 64 && MX)
-    if (nq == 4) k_attn_few<D, MX, 4, NT><<<g, 256, 0, st>>>(a, chunk_tiles, 0);
+  constexpr int NT = F == kKvBf16 ? 1 : 2;
+  if (nq == 1) k_attn_few<D, F, 1, NT><<<g, 256, 0, st>>>(a, chunk_tiles, 0);
+  if constexpr (D == 64 || F != kKvBf16)
+    if (nq == 2) k_attn_few<D, F, 2, NT><<<g, 256, 0, st>>>(a, chunk_tiles, 0);
+  if constexpr (D == 64 && F != kKvBf16)
+    if (nq == 4) k_attn_few<D, F, 4, NT><<<g, 256, 0, st>>>(a, chunk_tiles, 0);
 }
 
-hipError_t launch_attn_few(const AttnArgs& a, int D, bool mx, const AttnPlan& plan, hipStream_t st) {
+template <int D>
+static void few(int fmt, int nq, dim3 g, const AttnArgs& a, int chunk_tiles, hipStream_t st) {
+  if (fmt == kKvBf16) few<D, kKvBf16>(nq, g, a, chunk_tiles, st);
+  else if (fmt == kKvMx) few<D, kKvMx>(nq, g, a, chunk_tiles, st);
+  else few<D, kKvF8>(nq, g, a, chunk_tiles, st);
+}
+
+hipError_t launch_attn_few(const AttnArgs& a, int D, int fmt, const AttnPlan& plan, hipStream_t st) {
   const dim3 g((unsigned)plan.own.chunks * (unsigned)a.b.seqs * (unsigned)a.c.heads);
   const int nq = plan.few, ct = plan.own.chunk_tiles;
-  if (D == 128) mx ? few<128, true>(nq, g, a, ct, st) : few<128, false>(nq, g, a, ct, st);
-  else mx ? few<64, true>(nq, g, a, ct, st) : few<64, false>(nq, g, a, ct, st);
+  if (D == 128) few<128>(fmt, nq, g, a, ct, st);
+  else few<64>(fmt, nq, g, a, ct, st);
   return hipGetLastError();
 }
 

@@ -41,9 +41,10 @@ struct FewLds {
   float2 ml[4][16];
 };
 
-template <int D, bool MX, int NQ, int NT>
+template <int D, int F, int NQ, int NT>
 __device__ __forceinline__ void attn_few(const AttnArgs& a, int block, int chunk_tiles, int first_slot,
                                          FewLds<D>& shared) {
+  constexpr bool MX = F == kKvMx, F8 = F == kKvF8;
   constexpr int kC = D / 8, kJ = D / 32, kDT = D / 16;
   constexpr int kTok = kSub * NT;            // tokens of a wavefront's turn
   constexpr int kG16 = 2 * NT;               // 16-token groups of a turn: each lies in one page
@@ -68,7 +69,10 @@ __device__ __forceinline__ void attn_few(const AttnArgs& a, int block, int chunk
     grow[n] = sr.first + r / a.group, qh[n] = head * a.group + r % a.group, p[n] = base + r / a.group;
     const uint16_t* qp = a.q + (int64_t)grow[n] * a.ldq + (int64_t)qh[n] * D;
 #pragma unroll
-    for (int j = 0; j < kJ; ++j) qf[n][j] = *reinterpret_cast<const v8bf*>(qp + (MX ? g * (D / 4) + 8 * j : 32 * j + 8 * g));
+    for (int j = 0; j < kJ; ++j)
+      qf[n][j] = *reinterpret_cast<const v8bf*>(qp + (MX   ? g * (D / 4) + 8 * j
+                                                      : F8 ? 64 * (j >> 1) + 16 * g + 8 * (j & 1)
+                                                           : 32 * j + 8 * g));
   }
   v4f o[NQ][kDT] = {};
   float m[NQ], l[NQ];
@@ -98,9 +102,15 @@ __device__ __forceinline__ void attn_few(const AttnArgs& a, int block, int chunk
     if (live == 0) continue;
     // Every load is made: a token that no row sees takes its place in its page, and a group without a page takes
     // another's.  Keys there are masked, values set to zero.
-    uint4 kb[kG16][MX ? 1 : kJ], vb[kG16][MX ? 1 : kC / 4];
+    constexpr int kKeys = MX ? 1 : F8 ? D / 64 : kJ, kVals = MX ? 1 : F8 ? D / 64 : kC / 4;
+    uint4 kb[kG16][kKeys], vb[kG16][kVals];
     uint32_t ke[kG16], ve[kG16];
     const int l1 = __builtin_ctzll(live), any = __builtin_amdgcn_readlane(at, l1) - (l1 & 15);
+    uint32_t kse = 0, vse = 0;   // E4M3: lane i holds the scales of token i's block
+    if (F8) {
+      const uint32_t block = (uint32_t)(at >= 0 ? at : any) / kF8Block;
+      kse = a.c.ks[block], vse = a.c.vs[block];
+    }
 #pragma unroll
     for (int i = 0; i < kG16; ++i) {
       const unsigned mine = (unsigned)(live >> (16 * i)) & 0xFFFFu;
@@ -108,7 +118,7 @@ __device__ __forceinline__ void attn_few(const AttnArgs& a, int block, int chunk
       const int64_t row = mine ? __builtin_amdgcn_readlane(at, l0) - (l0 & 15) : any;
       if (MX) {
         const uint8_t *kp = a.c.k + row * (D / 2), *vp = a.c.v + row * (D / 2);
-        const uint8_t *kse = a.c.ks + row * (D / 32), *vse = a.c.vs + row * (D / 32);
+        const uint8_t *ksp = a.c.ks + row * (D / 32), *vsp = a.c.vs + row * (D / 32);
         // a quarter g of a token: the operand's for the keys, for the values one that suits the LDS
         const uint32_t ko = (uint32_t)(col * (D / 2) + g * (D / 8)), vo = (uint32_t)(v_tok * (D / 2) + g * (D / 8));
         if (D == 128) {
@@ -118,8 +128,17 @@ __device__ __forceinline__ void attn_few(const AttnArgs& a, int block, int chunk
           const uint2 x = *reinterpret_cast<const uint2*>(kp + ko), y = *reinterpret_cast<const uint2*>(vp + vo);
           kb[i][0] = make_uint4(x.x, x.y, 0, 0), vb[i][0] = make_uint4(y.x, y.y, 0, 0);
         }
-        ke[i] = kse[(uint32_t)(col * (D / 32) + g * (D / 32) / 4)];
-        ve[i] = vse[(uint32_t)(v_tok * (D / 32) + g * (D / 32) / 4)];
+        ke[i] = ksp[(uint32_t)(col * (D / 32) + g * (D / 32) / 4)];
+        ve[i] = vsp[(uint32_t)(v_tok * (D / 32) + g * (D / 32) / 4)];
+      } else if (F8) {   // 16 tokens lie in a row: their values come as they lie
+        const uint8_t *kp = a.c.k + row * D, *vp = a.c.v + row * D;
+#pragma unroll
+        for (int j = 0; j < kKeys; ++j) {
+          kb[i][j] = *reinterpret_cast<const uint4*>(kp + (uint32_t)(col * D + 16 * g) + 64 * j);
+          vb[i][j] = *reinterpret_cast<const uint4*>(vp + (uint32_t)(lane * 16) + 1024 * j);
+        }
+        ke[i] = (uint32_t)__builtin_amdgcn_readlane((int)kse, l0);
+        ve[i] = (uint32_t)__builtin_amdgcn_readlane((int)vse, l0);
       } else {
         const uint8_t *kp = a.c.k + row * (D * 2), *vp = a.c.v + row * (D * 2);
 #pragma unroll
@@ -139,6 +158,9 @@ __device__ __forceinline__ void attn_few(const AttnArgs& a, int block, int chunk
           if (MX) {
             const uint4& w = kb[2 * u + mt][0];
             kx = mx_bf16x8(j == 0 ? w.x : j == 1 ? w.y : j == 2 ? w.z : w.w, ke[2 * u + mt]);
+          } else if (F8) {
+            const uint4& w = kb[2 * u + mt][j >> 1];
+            kx = f8_bf16x8(j & 1 ? make_uint2(w.z, w.w) : make_uint2(w.x, w.y), ke[2 * u + mt]);
           } else {
             kx = kb[2 * u + mt][j];
           }
@@ -158,6 +180,16 @@ __device__ __forceinline__ void attn_few(const AttnArgs& a, int block, int chunk
 #pragma unroll
           for (int e = 0; e < D / 32; ++e)   // zero codes times 2^-127
             v_lds[16 * mt * kC + kv_chunk<D>(t, c0 + e)] = mx_bf16x8(dead ? 0 : w[e], dead ? 0 : ve[i]);
+        } else if (F8) {
+#pragma unroll
+          for (int j = 0; j < kVals; ++j) {
+            const int t = j * (1024 / D) + lane / (D / 16), c0 = 2 * (lane % (D / 16));
+            const bool dead = !((mine >> t) & 1);
+            const uint4 x = vb[i][j];
+            const uint32_t e = dead ? 127 : ve[i];
+            v_lds[16 * mt * kC + kv_chunk<D>(t, c0)] = f8_bf16x8(dead ? make_uint2(0, 0) : make_uint2(x.x, x.y), e);
+            v_lds[16 * mt * kC + kv_chunk<D>(t, c0 + 1)] = f8_bf16x8(dead ? make_uint2(0, 0) : make_uint2(x.z, x.w), e);
+          }
         } else {
 #pragma unroll
           for (int j = 0; j < kC / 4; ++j) {

@@ -90,9 +90,10 @@ struct RowsLds {
   uint4 kv[2][2][kT * D / 8];   // two stages of keys and values
 };
 
-template <int D, bool MX, bool ALL>
+template <int D, int F, bool ALL>
 __device__ __forceinline__ void attn_rows(const AttnArgs& a, int block, int tiles, int chunk_tiles, int first_slot,
                                           RowsLds<D>& shared) {
+  constexpr bool MX = F == kKvMx, F8 = F == kKvF8, CODES = MX || F8;
   constexpr int kC = D / 8, kDT = D / 32;   // 16-byte chunks of a row, 32-wide tiles of D
   auto& lds = shared.kv;
   int* const lds_p = reinterpret_cast<int*>(&lds[0][0][0]);
@@ -200,10 +201,12 @@ __device__ __forceinline__ void attn_rows(const AttnArgs& a, int block, int tile
   // they go to LDS over all banks.  A step of few rows is shorter than the way from HBM: with one tile on its way
   // 16 x 9 tokens, 4 query heads a key/value head, over 8000 took 80 us, with two 69; a prompt of 5759, heads of 64,
   // 210 and 191.
+  // E4M3: the same with 16 values a load as they lie; the 16 tokens have one scale.
+  constexpr int kW = F8 ? D / 64 : 1;
   struct Codes {
-    uint4 k, v;
+    uint4 k[kW], v[kW];
     uint32_t ks, vs;
-  } ahead[MX ? 2 : 1];
+  } ahead[CODES ? 2 : 1];
   const int mx_row = mx_token<D>(lane), mx_block = (lane >> 4) % (D / 32);
   const int mx_byte = mx_row * (D / 32) + mx_block;   // of the 16 tokens' scales; loaded as the dword that holds it
   auto load = [&](int at, int to) {
@@ -213,10 +216,20 @@ __device__ __forceinline__ void attn_rows(const AttnArgs& a, int block, int tile
       const int64_t row0 = mine ? __builtin_amdgcn_readlane(at, l0) - (l0 & 15) : 0;
       const uint32_t block = (uint32_t)mx_byte;
       Codes& x = ahead[to];
-      x.k = *reinterpret_cast<const uint4*>(a.c.k + row0 * (D / 2) + block * 16);
-      x.v = *reinterpret_cast<const uint4*>(a.c.v + row0 * (D / 2) + block * 16);
+      x.k[0] = *reinterpret_cast<const uint4*>(a.c.k + row0 * (D / 2) + block * 16);
+      x.v[0] = *reinterpret_cast<const uint4*>(a.c.v + row0 * (D / 2) + block * 16);
       x.ks = reinterpret_cast<const uint32_t*>(a.c.ks + row0 * (D / 32))[block / 4];
       x.vs = reinterpret_cast<const uint32_t*>(a.c.vs + row0 * (D / 32))[block / 4];
+    } else if (F8) {   // likewise
+      const int64_t row0 = mine ? __builtin_amdgcn_readlane(at, l0) - (l0 & 15) : 0;
+      const uint8_t *kp = a.c.k + row0 * D, *vp = a.c.v + row0 * D;
+      Codes& x = ahead[to];
+#pragma unroll
+      for (int i = 0; i < kW; ++i) {
+        x.k[i] = *reinterpret_cast<const uint4*>(kp + (uint32_t)lane * 16 + 1024 * i);
+        x.v[i] = *reinterpret_cast<const uint4*>(vp + (uint32_t)lane * 16 + 1024 * i);
+      }
+      x.ks = a.c.ks[row0 / kF8Block], x.vs = a.c.vs[row0 / kF8Block];
     } else if (mine) {
       const int64_t row0 = __builtin_amdgcn_readlane(at, l0) - (l0 & 15);
       const uint8_t *kp = a.c.k + row0 * (D * 2), *vp = a.c.v + row0 * (D * 2);
@@ -238,15 +251,29 @@ __device__ __forceinline__ void attn_rows(const AttnArgs& a, int block, int tile
       const bool dead = !((live >> row) & 1);
       const int at = 8 * (mx_byte & 3);
       const uint32_t ks = dead ? 0 : x.ks >> at & 0xFF, vs = dead ? 0 : x.vs >> at & 0xFF;
-      const uint32_t kw[4] = {x.k.x, x.k.y, x.k.z, x.k.w}, vw[4] = {x.v.x, x.v.y, x.v.z, x.v.w};
+      const uint32_t kw[4] = {x.k[0].x, x.k[0].y, x.k[0].z, x.k[0].w}, vw[4] = {x.v[0].x, x.v[0].y, x.v[0].z, x.v[0].w};
 #pragma unroll
       for (int e = 0; e < 4; ++e) {   // zero codes times 2^-127
         lds[stage][0][kv_chunk<D>(row, c0 + e)] = mx_bf16x8(dead ? 0 : kw[e], ks);
         lds[stage][1][kv_chunk<D>(row, c0 + e)] = mx_bf16x8(dead ? 0 : vw[e], vs);
       }
     }
+    if (F8) {
+      const Codes& x = ahead[stage];
+#pragma unroll
+      for (int i = 0; i < kW; ++i) {
+        const int row = 16 * wave + i * (1024 / D) + lane / (D / 16), c0 = 2 * (lane % (D / 16));
+        const bool dead = !((live >> row) & 1);
+        const uint32_t ks = dead ? 127 : x.ks, vs = dead ? 127 : x.vs;
+        const uint4 k = dead ? make_uint4(0, 0, 0, 0) : x.k[i], v = dead ? make_uint4(0, 0, 0, 0) : x.v[i];
+        lds[stage][0][kv_chunk<D>(row, c0)] = f8_bf16x8(make_uint2(k.x, k.y), ks);
+        lds[stage][0][kv_chunk<D>(row, c0 + 1)] = f8_bf16x8(make_uint2(k.z, k.w), ks);
+        lds[stage][1][kv_chunk<D>(row, c0)] = f8_bf16x8(make_uint2(v.x, v.y), vs);
+        lds[stage][1][kv_chunk<D>(row, c0 + 1)] = f8_bf16x8(make_uint2(v.z, v.w), vs);
+      }
+    }
   };
-  if (!MX) {
+  if (!CODES) {
     for (int i = tid; i < kT * kC; i += 256) lds[0][1][i] = lds[1][1][i] = make_uint4(0, 0, 0, 0);
     __syncthreads();
   }
@@ -262,9 +289,9 @@ __device__ __forceinline__ void attn_rows(const AttnArgs& a, int block, int tile
       v_at[d][u] = 16 * kv_chunk<D>(8 * u + 4 * half + ((lane & 15) >> 2), 4 * d + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) +
                    8 * (lane & 1);
 
-  // Tiles and pages of a tile on their way while one is worked on.  MXFP4: tile ti is in ahead[] and in LDS at the
+  // Tiles and pages of a tile on their way while one is worked on.  Codes: tile ti is in ahead[] and in LDS at the
   // parity of ti - first.
-  constexpr int kAhead = MX ? 2 : 1;
+  constexpr int kAhead = CODES ? 2 : 1;
   unsigned long long live[kAhead + 1] = {};   // of this tile and the next ones, token by token: whether it is there
   int next = 0;
   const bool any = first < end && a.c.pages > 0;
@@ -284,7 +311,7 @@ __device__ __forceinline__ void attn_rows(const AttnArgs& a, int block, int tile
   // the queries, here and once: the loop's own waits would count the tiles' loads among theirs
 #pragma unroll
   for (int i = 0; i < D / 16; ++i) asm volatile("" : "+v"(qf[i]));
-  if (!MX) lds_load_wait();
+  if (!CODES) lds_load_wait();
   __syncthreads();
   auto step = [&](int ti, auto stage_c) {
     constexpr int stage = decltype(stage_c)::value;
@@ -292,7 +319,7 @@ __device__ __forceinline__ void attn_rows(const AttnArgs& a, int block, int tile
     const int at = row_of(next, ti + kAhead);
     live[kAhead] = __ballot(at >= 0);
     next = page_of(ti + kAhead + 1);
-    load(at, MX ? stage : stage ^ 1);
+    load(at, CODES ? stage : stage ^ 1);
     if (ts <= w_hi && live[0] != 0) {
       const char *sk = reinterpret_cast<const char*>(lds[stage][0]), *sv = reinterpret_cast<const char*>(lds[stage][1]);
       v16f s[2] = {};
@@ -368,13 +395,13 @@ __device__ __forceinline__ void attn_rows(const AttnArgs& a, int block, int tile
     store(stage ^ 1, live[1]);
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) live[i] = live[i + 1];
-    if (!MX) lds_load_wait();
+    if (!CODES) lds_load_wait();
     __syncthreads();
   };
   if (any)
-    for (int ti = first; ti < end; ti += 2) {   // (MXFP4: in pairs, so that waits stay counted; past the end are no tokens)
+    for (int ti = first; ti < end; ti += 2) {   // (codes: in pairs, so that waits stay counted; past the end are no tokens)
       step(ti, std::integral_constant<int, 0>{});
-      if (MX || ti + 1 < end) step(ti + 1, std::integral_constant<int, 1>{});
+      if (CODES || ti + 1 < end) step(ti + 1, std::integral_constant<int, 1>{});
     }
   l += __shfl_xor(l, 32);
   const int mine = rows - wave * 32 < 32 ? rows - wave * 32 : 32;   // rows of this wavefront

@@ -121,8 +121,173 @@ __global__ __launch_bounds__(kAppendThreads) void k_kv_append(KvAppendArgs a, Kv
                                                           bf16x2(hi[4], hi[5]), bf16x2(hi[6], hi[7]));
 }
 
+// Values of dims j..j+N-1 and j+D/2..j+D/2+N-1 of a head, from bf16, N a multiple of 8.
+template <int D, int N>
+__device__ __forceinline__ void load_halves(const uint16_t* src, float* lo, float* hi) {
+#pragma unroll
+  for (int i = 0; i < N; i += 8) {
+    const uint4 x0 = *reinterpret_cast<const uint4*>(src + i), x1 = *reinterpret_cast<const uint4*>(src + i + D / 2);
+    const uint32_t w0[4] = {x0.x, x0.y, x0.z, x0.w}, w1[4] = {x1.x, x1.y, x1.z, x1.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      lo[i + 2 * k] = bf16_lo(w0[k]), lo[i + 2 * k + 1] = bf16_hi(w0[k]);
+      hi[i + 2 * k] = bf16_lo(w1[k]), hi[i + 2 * k + 1] = bf16_hi(w1[k]);
+    }
+  }
+}
+
+template <int N>
+__device__ __forceinline__ void rotate_halves(const float* cp, const float* sp, float* lo, float* hi) {
+#pragma unroll
+  for (int i = 0; i < N; i += 4) {
+    const float4 c = *reinterpret_cast<const float4*>(cp + i), s = *reinterpret_cast<const float4*>(sp + i);
+    const float cs[4] = {c.x, c.y, c.z, c.w}, sn[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float u = lo[i + k], w = hi[i + k];
+      lo[i + k] = u * cs[k] - w * sn[k];
+      hi[i + k] = w * cs[k] + u * sn[k];
+    }
+  }
+}
+
+// One wavefront: the keys or values of a head of one block of 16 tokens, of which tokens [from, from + n) are rows of
+// the call from `row` on and, where `olds`, those before are in the cache.  Lane: token lane / 4, a quarter of both
+// halves of the head.  The block's new scale is the larger of the one that its old tokens have and the one that the new
+// ones need; where it grows, old codes are rounded again (exactly, but for those that become subnormal).
+template <int D>
+__device__ __forceinline__ void append8_block(const KvAppendArgs& a, const KvCacheArgs& c, bool is_v, int h, int at,
+                                              int row, int pos, int from, int n, bool olds) {
+  constexpr int N = D / 8;   // values of a half: 16 or 8
+  const int lane = (int)threadIdx.x & 63, t = lane >> 2, j = (lane & 3) * N;
+  uint8_t* const codes = (is_v ? c.v : c.k) + ((int64_t)at + t) * D + j;
+  uint8_t* const scale = (is_v ? c.vs : c.ks) + at / kF8Block;
+  bool mine = t >= from && t < from + n;
+  const int r = row + (mine ? t - from : 0);
+  float lo[N], hi[N];
+  load_halves<D, N>((is_v ? a.v + r * a.ldv : a.k + r * a.ldk) + h * D + j, lo, hi);
+  uint32_t old[2][N / 4] = {};
+  const bool was = olds && t < from;
+  int before = kF8Least;
+  if (olds) {   // on its way with the row's values, whether the scale grows or not
+    before = (int)*scale - 127;
+    if (was)
+#pragma unroll
+      for (int i = 0; i < N / 4; ++i) {
+        old[0][i] = reinterpret_cast<const uint32_t*>(codes)[i];
+        old[1][i] = reinterpret_cast<const uint32_t*>(codes + D / 2)[i];
+      }
+  }
+  if (a.cos) {
+    const int angle = a.pos ? a.pos[r] : pos + (r - row);
+    if (angle < 0 || angle >= a.angles) mine = false;   // left out
+    if (!is_v && mine)
+      rotate_halves<N>(a.cos + (int64_t)angle * (D / 2) + j, a.sin + (int64_t)angle * (D / 2) + j, lo, hi);
+  }
+  if (!__any(mine)) return;
+  uint32_t peak = 0;   // of the finite values: one that is not does not take its neighbours with it
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const uint32_t x = __float_as_uint(lo[i]) & 0x7FFFFFFFu, y = __float_as_uint(hi[i]) & 0x7FFFFFFFu;
+    if (x < 0x7F800000u && x > peak) peak = x;
+    if (y < 0x7F800000u && y > peak) peak = y;
+  }
+  if (!mine) peak = 0;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const uint32_t o = (uint32_t)__shfl_xor((int)peak, d);
+    peak = o > peak ? o : peak;
+  }
+  const int need = f8_exponent(peak, a.rule_bias), e = need > before ? need : before;
+  if (was && e > before) {
+    // a step of 20 takes the largest code to zero
+    const float f = exp2_int(before - e < -30 ? -30 : before - e);
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) {
+      reinterpret_cast<uint32_t*>(codes)[i] = f8_rescale4(old[0][i], f);
+      reinterpret_cast<uint32_t*>(codes + D / 2)[i] = f8_rescale4(old[1][i], f);
+    }
+  }
+  if (mine) {
+    const float inv = exp2_int(-e);
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) {
+      reinterpret_cast<uint32_t*>(codes)[i] = f8_encode4(lo + 4 * i, inv);
+      reinterpret_cast<uint32_t*>(codes + D / 2)[i] = f8_encode4(hi + 4 * i, inv);
+    }
+  }
+  if (lane == 0) *scale = (uint8_t)(e + 127);
+}
+
+// Appends to an E4M3 cache.  A scale is shared by 16 tokens of a page and head, so a block is one wavefront's, which
+// the row that begins it finds: the first of a sequence's rows, or one at a multiple of 16.
+template <int D>
+__global__ __launch_bounds__(kAppend8Threads) void k_kv_append8(KvAppendArgs a, KvBatchArgs b, KvCacheArgs c,
+                                                                unsigned queries, int group) {
+  const int tid = (int)threadIdx.x;
+  if (blockIdx.x < queries) {   // a thread: 8 values of a head's first half and the 8 that pair with them
+    constexpr int kPer = D / 16;
+    const unsigned item = blockIdx.x * kAppend8Threads + tid, per_row = (unsigned)a.q_heads * kPer;
+    const int row = (int)(item / per_row), rest = (int)(item % per_row), h = rest / kPer, j = rest % kPer * 8;
+    const int first = (int)((blockIdx.x * kAppend8Threads + (tid & ~63)) / per_row);   // of the wavefront
+    if (first >= b.rows) return;
+    float lo[8], hi[8];
+    const bool has = row < b.rows;
+    if (has) load_halves<D, 8>(a.q + row * a.ldq + h * D + j, lo, hi);
+    int s = find_seq(b, first), past = b.seqs;   // few of a wavefront's threads are at a later row than the first
+    if (!has) return;
+    if (row == first) past = s;
+    while (s < past) {
+      const int mid = s + (past - s) / 2;
+      if (b.offs[mid + 1] <= row) s = mid + 1;
+      else past = mid;
+    }
+    if (s >= b.seqs) return;
+    const SeqRows r = seq_rows(b, s);
+    const int i = row - r.first, p = r.len - r.n + i;
+    if (i < 0 || i >= r.n || p < 0) return;
+    if (a.cos) {
+      const int angle = a.pos ? a.pos[row] : p;
+      if (angle < 0 || angle >= a.angles) return;
+      rotate_halves<8>(a.cos + (int64_t)angle * (D / 2) + j, a.sin + (int64_t)angle * (D / 2) + j, lo, hi);
+    }
+    uint16_t* const dst = a.qo + row * a.ldqo + h * D + j;
+    *reinterpret_cast<uint4*>(dst) = make_uint4(bf16x2(lo[0], lo[1]), bf16x2(lo[2], lo[3]), bf16x2(lo[4], lo[5]),
+                                                bf16x2(lo[6], lo[7]));
+    *reinterpret_cast<uint4*>(dst + D / 2) = make_uint4(bf16x2(hi[0], hi[1]), bf16x2(hi[2], hi[3]),
+                                                        bf16x2(hi[4], hi[5]), bf16x2(hi[6], hi[7]));
+    return;
+  }
+  const unsigned block = blockIdx.x - queries, parts = (unsigned)kv_append8_parts(c.heads);
+  const int item = (int)(block % parts) * 4 + (tid >> 6), unit = (int)(block / parts);
+  if (item >= 2 * c.heads) return;
+  const bool is_v = item & 1;
+  const int h = item >> 1;
+  const int64_t end64 = ((int64_t)unit + 1) * group;
+  const int end = end64 < b.rows ? (int)end64 : b.rows;
+  int row = unit * group;
+  while (row < end) {
+    const int s = find_seq(b, row);
+    if (s >= b.seqs) return;
+    const SeqRows r = seq_rows(b, s);
+    if (row < r.first || row >= r.first + r.n) return;   // offsets that decrease
+    const int base = r.len - r.n, last = r.first + r.n;
+    if (base + (row - r.first) < 0) row = -base < r.n ? r.first - base : last;   // rows at negative positions
+    while (row < last && row < end) {
+      const int p = base + (row - r.first), from = p & (kF8Block - 1);
+      const int n = kF8Block - from < last - row ? kF8Block - from : last - row;
+      if (row == r.first || from == 0) {
+        const int page = b.table[s * b.ldt + (p >> c.page_shift)];
+        const int at = kv_row(page, p & ~(kF8Block - 1), c.pages, c.heads, h, c.page_shift);
+        if (at >= 0) append8_block<D>(a, c, is_v, h, at, row, p, from, n, from > 0);
+      }
+      row += n;
+    }
+  }
+}
+
 // A thread reads 8 values; workgroup b: row b / parts, as above.
-template <int D, bool MX>
+template <int D, int F>
 __global__ __launch_bounds__(kReadThreads) void k_kv_read(uint16_t* ko, int64_t ldk, uint16_t* vo, int64_t ldv,
                                                           int parts, KvBatchArgs b, KvCacheArgs c) {
   constexpr int kPer = D / 8;
@@ -140,9 +305,12 @@ __global__ __launch_bounds__(kReadThreads) void k_kv_read(uint16_t* ko, int64_t 
                        : kv_row(b.table[s * b.ldt + (p >> c.page_shift)], p, c.pages, c.heads, h, c.page_shift);
   uint4 y{};
   if (at >= 0) {
-    if (MX) {
+    if (F == kKvMx) {
       const uint32_t codes = *reinterpret_cast<const uint32_t*>((is_v ? c.v : c.k) + (int64_t)at * (D / 2) + j / 2);
       y = mx_bf16x8(codes, (is_v ? c.vs : c.ks)[(int64_t)at * (D / 32) + j / 32]);
+    } else if (F == kKvF8) {
+      const uint2 codes = *reinterpret_cast<const uint2*>((is_v ? c.v : c.k) + (int64_t)at * D + j);
+      y = f8_bf16x8(codes, (is_v ? c.vs : c.ks)[at / kF8Block]);
     } else {
       y = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(is_v ? c.v : c.k) + (int64_t)at * D + j);
     }
@@ -153,8 +321,17 @@ __global__ __launch_bounds__(kReadThreads) void k_kv_read(uint16_t* ko, int64_t 
 hipError_t launch_kv_append(const uint16_t* q, const uint16_t* k, const uint16_t* v, int64_t ldq, int64_t ldk,
                             int64_t ldv, int q_heads, uint16_t* qo, int64_t ldqo, const float* cos, const float* sin,
                             int angles, const int32_t* pos, uint32_t rule_bias, const KvBatchArgs& b,
-                            const KvCacheArgs& c, int D, bool mx, hipStream_t st) {
+                            const KvCacheArgs& c, int D, int fmt, int64_t max_rows, hipStream_t st) {
+  const bool mx = fmt == kKvMx;
   KvAppendArgs a{q, k, v, ldq, ldk, ldv, qo, ldqo, cos, sin, pos, angles, q_heads, 0, rule_bias};
+  if (fmt == kKvF8) {
+    const int group = kv_append8_group(max_rows);
+    const unsigned first = (unsigned)kv_append8_queries(b.rows, q_heads, D);
+    const dim3 g8((unsigned)kv_append8_blocks(b.rows, max_rows, q_heads, c.heads, D)), t8(kAppend8Threads);
+    if (D == 128) k_kv_append8<128><<<g8, t8, 0, st>>>(a, b, c, first, group);
+    else k_kv_append8<64><<<g8, t8, 0, st>>>(a, b, c, first, group);
+    return hipGetLastError();
+  }
   a.parts = kv_append_parts(q_heads, c.heads, D);
   const dim3 g((unsigned)b.rows * (unsigned)a.parts), t(kAppendThreads);
   if (D == 128)
@@ -164,16 +341,21 @@ hipError_t launch_kv_append(const uint16_t* q, const uint16_t* k, const uint16_t
   return hipGetLastError();
 }
 
+template <int D>
+static void kv_read(int fmt, dim3 g, uint16_t* ko, int64_t ldk, uint16_t* vo, int64_t ldv, int parts,
+                    const KvBatchArgs& b, const KvCacheArgs& c, hipStream_t st) {
+  const dim3 t(kReadThreads);
+  if (fmt == kKvBf16) k_kv_read<D, kKvBf16><<<g, t, 0, st>>>(ko, ldk, vo, ldv, parts, b, c);
+  else if (fmt == kKvMx) k_kv_read<D, kKvMx><<<g, t, 0, st>>>(ko, ldk, vo, ldv, parts, b, c);
+  else k_kv_read<D, kKvF8><<<g, t, 0, st>>>(ko, ldk, vo, ldv, parts, b, c);
+}
+
 hipError_t launch_kv_read(uint16_t* ko, int64_t ldk, uint16_t* vo, int64_t ldv, const KvBatchArgs& b,
-                          const KvCacheArgs& c, int D, bool mx, hipStream_t st) {
+                          const KvCacheArgs& c, int D, int fmt, hipStream_t st) {
   const int parts = kv_read_parts(c.heads, D);
-  const dim3 g((unsigned)b.rows * (unsigned)parts), t(kReadThreads);
-  if (D == 128)
-    mx ? k_kv_read<128, true><<<g, t, 0, st>>>(ko, ldk, vo, ldv, parts, b, c)
-       : k_kv_read<128, false><<<g, t, 0, st>>>(ko, ldk, vo, ldv, parts, b, c);
-  else
-    mx ? k_kv_read<64, true><<<g, t, 0, st>>>(ko, ldk, vo, ldv, parts, b, c)
-       : k_kv_read<64, false><<<g, t, 0, st>>>(ko, ldk, vo, ldv, parts, b, c);
+  const dim3 g((unsigned)b.rows * (unsigned)parts);
+  if (D == 128) kv_read<128>(fmt, g, ko, ldk, vo, ldv, parts, b, c, st);
+  else kv_read<64>(fmt, g, ko, ldk, vo, ldv, parts, b, c, st);
   return hipGetLastError();
 }
 

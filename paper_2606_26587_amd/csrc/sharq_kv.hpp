@@ -7,12 +7,19 @@
 
 namespace sharq {
 
+// Formats of a cache, numbered as in the C ABI.
+constexpr int kKvBf16 = 0, kKvMx = 1, kKvF8 = 2;
+
+// Tokens that share a scale in an E4M3 cache: the smallest page, and the tokens
+// that the attention's kernels bring at a time, so that these have one scale.
+constexpr int kF8Block = 16;
+
 // Buffers and sizes of a cache, as the kernels take them.  A cache row is one
 // token of one key/value head; row (page * heads + head) * page_size + slot.
 // Row numbers fit 32 bits (checked at the call), byte offsets need 64.
 struct KvCacheArgs {
   uint8_t *k, *v;
-  uint8_t *ks, *vs;   // E8M0 scales (MXFP4)
+  uint8_t *ks, *vs;   // E8M0 scales (MXFP4: per row and 32 values; E4M3: per 16 rows)
   int pages, heads, page_shift;
 };
 
@@ -72,6 +79,22 @@ constexpr int kv_append_parts(int q_heads, int heads, int D) {
 }
 constexpr int kv_read_parts(int heads, int D) { return (2 * heads * (D / 8) + kReadThreads - 1) / kReadThreads; }
 
+// E4M3: the append's workgroups of four wavefronts.  The first of them take the
+// queries, 16 values a thread; the others the blocks of 16 tokens that `group`
+// consecutive rows begin, a wavefront for the keys or the values of a head.  One
+// row a unit where sequences bring few, so that as many wavefronts run as there
+// are blocks; 16 where they bring many, of which about one begins a block.
+constexpr int kAppend8Threads = 256;
+constexpr int kv_append8_group(int64_t max_rows) { return max_rows < 2 * kF8Block ? 1 : kF8Block; }
+constexpr int64_t kv_append8_queries(int64_t rows, int q_heads, int D) {
+  return (rows * q_heads * (D / 16) + kAppend8Threads - 1) / kAppend8Threads;
+}
+constexpr int kv_append8_parts(int heads) { return (2 * heads + 3) / 4; }
+constexpr int64_t kv_append8_blocks(int64_t rows, int64_t max_rows, int q_heads, int heads, int D) {
+  const int group = kv_append8_group(max_rows);
+  return kv_append8_queries(rows, q_heads, D) + (rows + group - 1) / group * kv_append8_parts(heads);
+}
+
 // A launch has fewer than 2^32 threads.
 constexpr bool kv_launches(int64_t blocks, int threads) { return blocks <= 0xFFFFFFFFll / threads; }
 
@@ -115,8 +138,9 @@ constexpr AttnSplit attn_split(int64_t tiles, int64_t units, int64_t kv_tiles, i
 }
 
 constexpr AttnPlan attn_plan(int64_t seqs, int64_t rows, int64_t max_rows, int64_t max_len, int heads, int group, int D,
-                             bool mx, int64_t window, int64_t sinks, int64_t prefix_len) {
+                             int fmt, int64_t window, int64_t sinks, int64_t prefix_len) {
   AttnPlan p{};
+  const bool mx = fmt != kKvBf16;   // codes that become bf16 on the way
   if (max_rows > rows) max_rows = rows;
   // a window leaves little of a prefix, and rows that see different parts of it
   p.shared = prefix_len > 0 && window >= max_len;

@@ -5,19 +5,18 @@
 #include <limits.h>
 
 #include "../../include/sharq.h"
-#include "sharq_device.hpp"
-#include "sharq_kv.hpp"
+#include "sharq_kv_device.hpp"
 
 namespace sharq {
 hipError_t launch_kv_append(const uint16_t* q, const uint16_t* k, const uint16_t* v, int64_t ldq, int64_t ldk,
                             int64_t ldv, int q_heads, uint16_t* qo, int64_t ldqo, const float* cos, const float* sin,
                             int angles, const int32_t* pos, uint32_t rule_bias, const KvBatchArgs& b,
-                            const KvCacheArgs& c, int D, bool mx, hipStream_t st);
+                            const KvCacheArgs& c, int D, int fmt, int64_t max_rows, hipStream_t st);
 hipError_t launch_kv_read(uint16_t* ko, int64_t ldk, uint16_t* vo, int64_t ldv, const KvBatchArgs& b,
-                          const KvCacheArgs& c, int D, bool mx, hipStream_t st);
+                          const KvCacheArgs& c, int D, int fmt, hipStream_t st);
 hipError_t launch_attention(const uint16_t* q, int64_t ldq, uint16_t* o, int64_t ldo, float* lse,
                             const KvBatchArgs& b, const KvCacheArgs& c, const AttnPlan& plan,
-                            const int32_t* prefix_table, int prefix_len, int q_heads, int D, bool mx, int window,
+                            const int32_t* prefix_table, int prefix_len, int q_heads, int D, int fmt, int window,
                             int sinks, float scale, void* ws, hipStream_t st);
 }  // namespace sharq
 
@@ -37,7 +36,7 @@ sharq_status hip_status(hipError_t e) { return e == hipSuccess ? SHARQ_OK : SHAR
 // Sizes and format of a cache.
 sharq_status check_sizes(const sharq_kv_cache* c) {
   if (!c) return SHARQ_EINVAL;
-  if (c->fmt != SHARQ_KV_BF16 && c->fmt != SHARQ_KV_MXFP4) return SHARQ_EINVAL;
+  if (c->fmt != SHARQ_KV_BF16 && c->fmt != SHARQ_KV_MXFP4 && c->fmt != SHARQ_KV_FP8) return SHARQ_EINVAL;
   if (c->pages < 0 || c->kv_heads < 1 || c->page_size < 1 || (c->page_size & (c->page_size - 1)) != 0 ||
       c->head_dim < 1)
     return SHARQ_EINVAL;
@@ -53,8 +52,9 @@ sharq_status check_cache(const sharq_kv_cache* c) {
   if (s != SHARQ_OK || c->pages == 0) return s;   // an empty pool is never dereferenced
   if (!c->k || !c->v) return SHARQ_EINVAL;
   if (!aligned(c->k, 16) || !aligned(c->v, 16)) return SHARQ_EALIGN;
-  if (c->fmt == SHARQ_KV_MXFP4) {
+  if (c->fmt != SHARQ_KV_BF16) {
     if (!c->k_scale || !c->v_scale) return SHARQ_EINVAL;
+    if (c->fmt == SHARQ_KV_FP8) return SHARQ_OK;   // scales are read one by one
     if (!aligned(c->k_scale, 4) || !aligned(c->v_scale, 4)) return SHARQ_EALIGN;
   }
   return SHARQ_OK;
@@ -107,7 +107,7 @@ int attn_sinks(const sharq_attn* t) { return t->sinks > INT_MAX ? INT_MAX : (int
 
 sharq::AttnPlan plan_of(const sharq_kv_cache* c, const sharq_kv_batch* b, const sharq_attn* t, int64_t q_heads) {
   return sharq::attn_plan(b->seqs, owned_rows(b), b->max_rows, b->max_len, c->kv_heads, (int)(q_heads / c->kv_heads),
-                          c->head_dim, c->fmt == SHARQ_KV_MXFP4, attn_window(t), attn_sinks(t), t->prefix_len);
+                          c->head_dim, c->fmt, attn_window(t), attn_sinks(t), t->prefix_len);
 }
 
 }  // namespace
@@ -117,8 +117,10 @@ extern "C" {
 size_t sharq_kv_buffer_bytes(const sharq_kv_cache* c, int32_t which) {
   if (check_sizes(c) != SHARQ_OK || which < 0 || which > 3) return 0;
   const size_t values = (size_t)c->pages * (size_t)c->kv_heads * (size_t)c->page_size * (size_t)c->head_dim;
-  if (which < 2) return c->fmt == SHARQ_KV_BF16 ? values * 2 : values / 2;
-  return c->fmt == SHARQ_KV_BF16 ? 0 : values / 32;
+  if (which < 2) return c->fmt == SHARQ_KV_BF16 ? values * 2 : c->fmt == SHARQ_KV_FP8 ? values : values / 2;
+  return c->fmt == SHARQ_KV_BF16  ? 0
+         : c->fmt == SHARQ_KV_FP8 ? values / c->head_dim / sharq::kF8Block
+                                  : values / 32;
 }
 
 sharq_status sharq_kv_append(const void* Q, const void* K, const void* V, sharq_dtype xdt, int64_t q_heads,
@@ -142,14 +144,18 @@ sharq_status sharq_kv_append(const void* Q, const void* K, const void* V, sharq_
       !aligned(positions, 4) || (q_heads > 0 && (!row_aligned(Q, ldq) || !row_aligned(Q_out, ldqo))))
     return SHARQ_EALIGN;
   if (batch->max_len == 0) return SHARQ_OK;   // no row has a position
-  if (!sharq::kv_launches(batch->rows * sharq::kv_append_parts((int)q_heads, cache->kv_heads, (int)D),
-                          sharq::kAppendThreads))
+  const bool f8 = cache->fmt == SHARQ_KV_FP8, ceil = cache->scale_rule == SHARQ_SCALE_CEIL;
+  if (f8 ? !sharq::kv_launches(sharq::kv_append8_blocks(batch->rows, batch->max_rows, (int)q_heads, cache->kv_heads, (int)D),
+                               sharq::kAppend8Threads)
+         : !sharq::kv_launches(batch->rows * sharq::kv_append_parts((int)q_heads, cache->kv_heads, (int)D),
+                               sharq::kAppendThreads))
     return SHARQ_EUNSUPPORTED;
   return hip_status(sharq::launch_kv_append(
       static_cast<const uint16_t*>(Q), static_cast<const uint16_t*>(K), static_cast<const uint16_t*>(V), ldq, ldk, ldv,
       (int)q_heads, static_cast<uint16_t*>(Q_out), ldqo, cos, sin, (int)angles, positions,
-      cache->scale_rule == SHARQ_SCALE_CEIL ? sharq::kE8Ceil : sharq::kE8Floor, batch_args(batch, batch->rows),
-      cache_args(cache), (int)D, cache->fmt == SHARQ_KV_MXFP4, reinterpret_cast<hipStream_t>(stream)));
+      f8 ? (ceil ? sharq::kF8Ceil : sharq::kF8Floor) : (ceil ? sharq::kE8Ceil : sharq::kE8Floor),
+      batch_args(batch, batch->rows), cache_args(cache), (int)D, cache->fmt, batch->max_rows,
+      reinterpret_cast<hipStream_t>(stream)));
 }
 
 sharq_status sharq_kv_read(const sharq_kv_cache* cache, const sharq_kv_batch* batch, void* K, int64_t ldk, void* V,
@@ -168,7 +174,7 @@ sharq_status sharq_kv_read(const sharq_kv_cache* cache, const sharq_kv_batch* ba
     return SHARQ_EUNSUPPORTED;
   return hip_status(sharq::launch_kv_read(static_cast<uint16_t*>(K), ldk, static_cast<uint16_t*>(V), ldv,
                                           batch_args(batch, batch->rows), cache_args(cache), cache->head_dim,
-                                          cache->fmt == SHARQ_KV_MXFP4, reinterpret_cast<hipStream_t>(stream)));
+                                          cache->fmt, reinterpret_cast<hipStream_t>(stream)));
 }
 
 size_t sharq_attention_workspace_bytes(const sharq_kv_cache* cache, const sharq_kv_batch* batch,
@@ -203,7 +209,7 @@ sharq_status sharq_attention(const void* Q, sharq_dtype xdt, int64_t q_heads, in
   return hip_status(sharq::launch_attention(
       static_cast<const uint16_t*>(Q), ldq, static_cast<uint16_t*>(O), ldo, lse, batch_args(batch, owned_rows(batch)),
       cache_args(cache), plan, attn->prefix_table, (int)attn->prefix_len, (int)q_heads, (int)D,
-      cache->fmt == SHARQ_KV_MXFP4, attn_window(attn), attn_sinks(attn), attn->scale, workspace, reinterpret_cast<hipStream_t>(stream)));
+      cache->fmt, attn_window(attn), attn_sinks(attn), attn->scale, workspace, reinterpret_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

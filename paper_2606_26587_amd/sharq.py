@@ -225,7 +225,10 @@ class QuantWeight:
                             None if self.tensor_scale is None else self.tensor_scale.data_ptr(), self.scale_rule)
 
 
-KV_FORMATS = {"bf16": 0, "mx": 1, "mxfp4": 1}
+KV_FORMATS = {"bf16": 0, "mx": 1, "mxfp4": 1, "fp8": 2}
+_KV_DTYPES = (torch.bfloat16, torch.uint8, torch.float8_e4m3fn)
+#: tokens of a block of an "fp8" cache, which share a scale
+KV_BLOCK = 16
 
 
 # The two descriptors below are used by every layer of a decode step: they are
@@ -236,30 +239,32 @@ KV_FORMATS = {"bf16": 0, "mx": 1, "mxfp4": 1}
 class KVCache:
     """A paged key/value cache (device buffers; sharq_kv_cache in include/sharq.h).
     fmt "bf16": k, v [pages, kv_heads, page_size, head_dim]; "mx": k, v uint8
-    codes [..., head_dim / 2] and their E8M0 scales uint8 [..., head_dim / 32]."""
+    codes [..., head_dim / 2] and their E8M0 scales uint8 [..., head_dim / 32]; "fp8": k, v
+    float8_e4m3fn [..., head_dim] and E8M0 scales uint8 [pages, kv_heads, page_size / 16]."""
     fmt: str
     k: torch.Tensor
     v: torch.Tensor
     k_scale: Optional[torch.Tensor] = None
     v_scale: Optional[torch.Tensor] = None
-    scale_rule: str = "floor"                 # "mx": E8M0 rule of sharq_kv_append (SCALE_RULES)
+    scale_rule: str = "floor"                 # "mx", "fp8": E8M0 rule of sharq_kv_append (SCALE_RULES)
 
     def __post_init__(self):
-        mx = KV_FORMATS[self.fmt] == 1
+        fmt = KV_FORMATS[self.fmt]
         shape = tuple(self.k.shape)
         ok = len(shape) == 4 and tuple(self.v.shape) == shape
         for t in (self.k, self.v):
-            ok = ok and t.dtype == (torch.uint8 if mx else torch.bfloat16)
-        if mx and ok:
+            ok = ok and t.dtype == _KV_DTYPES[fmt]
+        if fmt and ok:
+            scales = shape[:3] + (shape[3] // 16,) if fmt == 1 else shape[:2] + (shape[2] // KV_BLOCK,)
             ok = self.k_scale is not None and self.v_scale is not None
             for t in (self.k_scale, self.v_scale):
-                ok = ok and t.dtype == torch.uint8 and tuple(t.shape) == shape[:3] + (shape[3] // 16,)
+                ok = ok and t.dtype == torch.uint8 and tuple(t.shape) == scales
         given = [t for t in (self.k, self.v, self.k_scale, self.v_scale) if t is not None]
         if not ok or any(not t.is_contiguous() or t.device != self.k.device for t in given):
             raise SharqError(EINVAL, "KVCache")
         pages, kv_heads, page_size = shape[:3]
-        head_dim = shape[3] * 2 if mx else shape[3]
-        struct = KVCacheStruct(pages, page_size, kv_heads, head_dim, KV_FORMATS[self.fmt], self.k.data_ptr(),
+        head_dim = shape[3] * 2 if fmt == 1 else shape[3]
+        struct = KVCacheStruct(pages, page_size, kv_heads, head_dim, fmt, self.k.data_ptr(),
                                self.v.data_ptr(), _ptr(self.k_scale), _ptr(self.v_scale),
                                SCALE_RULES[self.scale_rule])
         self.__dict__.update(pages=pages, kv_heads=kv_heads, page_size=page_size, head_dim=head_dim,
@@ -305,9 +310,11 @@ def alloc_kv_cache(pages: int, page_size: int, kv_heads: int, head_dim: int, fmt
                    scale_rule: str = "floor") -> KVCache:
     """An empty paged cache; its pages are read only where something was appended."""
     shape = (pages, kv_heads, page_size)
-    if KV_FORMATS[fmt] == 0:
-        return KVCache(fmt, *(torch.empty(shape + (head_dim,), dtype=torch.bfloat16, device=device) for _ in "kv"),
-                       scale_rule=scale_rule)
+    if KV_FORMATS[fmt] != 1:
+        dtype = _KV_DTYPES[KV_FORMATS[fmt]]
+        codes = [torch.empty(shape + (head_dim,), dtype=dtype, device=device) for _ in "kv"]
+        scales = [torch.empty(shape[:2] + (page_size // KV_BLOCK,), dtype=torch.uint8, device=device) for _ in "kv"]
+        return KVCache(fmt, *codes, *(scales if KV_FORMATS[fmt] == 2 else ()), scale_rule=scale_rule)
     return KVCache(fmt, *(torch.empty(shape + (head_dim // n,), dtype=torch.uint8, device=device)
                           for n in (2, 2, 32, 32)), scale_rule=scale_rule)
 
