@@ -10,11 +10,16 @@
  * "sharq-output"; Sec. 3.4).  Between a decoder layer's qkv linear and its o
  * linear stand a paged key/value cache, in bf16, E4M3 or the library's MXFP4, and
  * the attention that reads it (sharq_kv_append, sharq_kv_read, sharq_attention).
+ * Around them stand what a server does between two steps: the tables that these
+ * calls take, from the requests' lengths (sharq_kv_assign), and beam search's choice
+ * of the next tokens with the reordering of the cached states behind it
+ * (sharq_beam_select, sharq_beam_reorder, sharq_kv_copy).
  *
  * Conventions for every entry point
  *   - Tensor pointers are DEVICE pointers owned by the caller; the library
- *     allocates nothing, keeps no global state and never synchronizes.  The one
- *     call that needs scratch memory, sharq_attention, takes it as an argument.
+ *     allocates nothing, keeps no global state and never synchronizes.  Calls that
+ *     need scratch memory (sharq_attention, sharq_kv_assign, sharq_beam_select) take
+ *     it as an argument.
  *   - `stream` is a hipStream_t passed as void* (NULL = the default stream);
  *     all work is enqueued asynchronously on it.
  *   - Errors are returned, never thrown.  Arguments are validated before any
@@ -560,6 +565,138 @@ SHARQ_API sharq_status sharq_attention(const void *Q, sharq_dtype xdt, int64_t q
                                        const sharq_kv_cache *cache, const sharq_kv_batch *batch,
                                        const sharq_attn *attn, void *O, int64_t ldo, float *lse, void *workspace,
                                        size_t workspace_bytes, void *stream);
+
+/*
+ * Pages that no sequence holds, as a stack.
+ *   pages        pages of the pool.
+ *   free_pages   device int32 [pages]: the first *count entries are free pages; the
+ *                last of them is given out first.
+ *   count, count_out
+ *                device int32 [1]: entries before and after a call (they may be
+ *                the same word).
+ */
+typedef struct {
+  int64_t pages;
+  int32_t *free_pages;
+  const int32_t *count;
+  int32_t *count_out;
+} sharq_kv_pool;
+
+/*
+ * The requests of a step, one for each sequence of the call that follows.
+ *   seqs, rows, max_len, ld_table
+ *                as in sharq_kv_batch; rows: entries of the row arrays.
+ *   page_size    a power of two in [16, 1024].  seqs * ceil(max_len / page_size) is
+ *                at most 2^30.
+ *   keep         device int32 [seqs]: cached tokens that stay (0: the sequence is
+ *                new, or has ended; fewer than there are: the last ones are dropped).
+ *   add          device int32 [seqs]: tokens that this step brings.
+ *   held         device int32 [seqs]: columns of its page table that are filled.
+ *   held_out     device int32 [seqs]: the same after the call (it may be `held`).
+ *   row_offsets  device int32 [seqs + 1], written.
+ *   lens         device int32 [seqs], written (it may be `keep`).
+ *   page_table   device int32 [seqs][ld_table]: new columns are written.
+ *   own_table    device int32 [seqs][ld_table] or NULL: new columns are written
+ *                there as well, and pages that go back are taken from it.  For
+ *                sequences whose page_table names pages of others (beams that share
+ *                a prompt: -1 in own_table where the page is another's).
+ *   row_seq, positions, slots
+ *                device int32 [rows] or NULL: of every row its sequence, its
+ *                position and its slot in the pool, page * page_size + position %
+ *                page_size, -1 without a page.
+ *   missing      device int32 [1] or NULL: columns for which there was no page.
+ */
+typedef struct {
+  int64_t seqs, rows, max_len, ld_table;
+  int32_t page_size;
+  const int32_t *keep, *add, *held;
+  int32_t *held_out, *row_offsets, *lens, *page_table, *own_table;
+  int32_t *row_seq, *positions, *slots, *missing;
+} sharq_kv_requests;
+
+/* Bytes of workspace that sharq_kv_assign needs; 0 for invalid sizes. */
+SHARQ_API size_t sharq_kv_assign_workspace_bytes(const sharq_kv_requests *r);
+
+/*
+ * Builds a step's tables on the device: for sequence s, in order,
+ *   n_s = add_s, cut where the call's rows end; row_offsets = exclusive sums of n;
+ *   lens_s = keep_s + n_s; need_s = ceil(lens_s / page_size) columns.
+ * Columns need_s .. held_s - 1 go back onto the stack, in the order of sequences
+ * and columns (entries that are no page of the pool are passed over; the table
+ * keeps them).  Then columns held_s .. need_s - 1 are given pages from the top of
+ * the stack, in the same order; where it is empty they get -1, an absent page, and
+ * `missing` counts them.  held_out_s = need_s.  row_offsets, lens and page_table are
+ * those of a sharq_kv_batch.  Rows behind the last sequence are left as they were.
+ * Values of the device arrays outside their range (negative, above max_len or the
+ * table's columns) count as the nearest inside.  The result does not depend on the
+ * order in which the device runs.  workspace: 4-byte aligned.
+ */
+SHARQ_API sharq_status sharq_kv_assign(const sharq_kv_pool *pool, const sharq_kv_requests *r, void *workspace,
+                                       size_t workspace_bytes, void *stream);
+
+/* Bytes of workspace that sharq_beam_select needs; 0 for invalid sizes. */
+SHARQ_API size_t sharq_beam_workspace_bytes(int64_t groups, int64_t beams, int64_t vocab);
+
+/*
+ * Beam search's choice.  A group has `beams` (1 to 32) hypotheses with scores (sums of
+ * log-probabilities), fp32 [groups][beams].  logits [groups * beams][vocab] (dtype
+ * BF16, F16 or F32, row stride ld elements, element-aligned).  Candidate (b, v) has
+ *   score_b + x_bv - lse_b,  lse_b = ln sum_v e^(x_bv);
+ * a beam that is done has one, (b, eos), with score_b.  Of each group the `beams` best,
+ * best first, equal ones by the lower b * vocab + v:
+ *   scores_out  fp32 [groups][beams] (it may be `scores`)
+ *   parents     int32 [groups][beams]: b
+ *   tokens      int32 [groups][beams]: v
+ *   done        uint8 [groups * beams] (0 or not) or NULL, with eos in [0, vocab)
+ *   done_out    uint8 [groups * beams] (it may be `done`), NULL exactly if done is:
+ *               done[b], or v == eos.
+ *   eos         -1 where there is none (then done is NULL).
+ * A logit of -inf is no candidate, nor is any of a beam whose score is -inf or whose
+ * score or logits hold a NaN or whose logits hold +inf.  Where a group has fewer than `beams`
+ * candidates, the places behind have score -inf, token -1 and themselves as parent.
+ * Scores are compared in 64 bits, whatever their rounding to scores_out.
+ * groups * beams is at most 2^20, beams * vocab below 2^31.  workspace: 8-byte aligned.
+ */
+SHARQ_API sharq_status sharq_beam_select(const void *logits, sharq_dtype dtype, int64_t ld, int64_t groups,
+                                         int64_t beams, int64_t vocab, const float *scores, const uint8_t *done,
+                                         int32_t eos, float *scores_out, int32_t *parents, int32_t *tokens,
+                                         uint8_t *done_out, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The states of groups of beams behind a choice.  Beam i of a group goes on from
+ * parents[i], int32 [groups][beams].  The beams of a group have the same number of
+ * cached tokens, lens (device int32 [groups * beams], the first of each group counts).
+ *   table, table_out    device int32 [groups * beams][cols], row strides ldt, ldto (it
+ *                       may be `table` with the same stride), or both NULL.
+ *                       Whole pages are shared: table_out[i] names its parent's.  The
+ *                       page that is partly filled goes to a parent's first child; each
+ *                       further child takes over the page of a parent without children
+ *                       (in order; there are as many).  Columns behind stay a beam's own.
+ *   copies              device int32 [groups * beams][3], with table: (source page, destination
+ *                       page, tokens) of what has to be copied into the pages taken over,
+ *                       for sharq_kv_copy on the caches of all layers; -1s for
+ *                       the others.
+ *   tokens, ids, ids_out
+ *                       or all NULL: chosen tokens int32 [groups][beams], and the sequences' tokens, device int32
+ *                       [groups * beams][id_cols], row strides ldi, ldio (ids_out may
+ *                       be `ids`): ids_out[i][t] = ids[parents[i]][t] for t < len,
+ *                       ids_out[i][len] = tokens[i]; columns behind are left as they were.
+ * Parents outside [0, beams) count as the nearest inside.  groups * beams is at most 2^20.
+ */
+SHARQ_API sharq_status sharq_beam_reorder(int64_t groups, int64_t beams, const int32_t *parents, const int32_t *lens,
+                                          int32_t page_size, const int32_t *table, int64_t ldt, int32_t *table_out,
+                                          int64_t ldto, int64_t cols, int32_t *copies, const int32_t *tokens,
+                                          const int32_t *ids, int64_t ldi, int32_t *ids_out, int64_t ldio,
+                                          int64_t id_cols, void *stream);
+
+/*
+ * Copies the first tokens of pages, keys and values of all heads, with their scales:
+ * copies, device int32 [n][3]: (source page, destination page, tokens).  An entry whose
+ * pages are the same or outside the pool is passed over; tokens above page_size
+ * count as page_size.  No page is the destination of two entries, or the destination of
+ * one and the source of another.
+ */
+SHARQ_API sharq_status sharq_kv_copy(const sharq_kv_cache *cache, const int32_t *copies, int64_t n, void *stream);
 
 SHARQ_API const char *sharq_status_str(sharq_status s);
 

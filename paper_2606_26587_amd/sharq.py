@@ -76,6 +76,18 @@ class AttnStruct(ctypes.Structure):
                 ("prefix_table", ctypes.c_void_p), ("prefix_len", ctypes.c_int64)]
 
 
+class KVPoolStruct(ctypes.Structure):
+    _fields_ = [("pages", ctypes.c_int64), ("free_pages", ctypes.c_void_p), ("count", ctypes.c_void_p),
+                ("count_out", ctypes.c_void_p)]
+
+
+class KVRequestsStruct(ctypes.Structure):
+    _fields_ = [("seqs", ctypes.c_int64), ("rows", ctypes.c_int64), ("max_len", ctypes.c_int64),
+                ("ld_table", ctypes.c_int64), ("page_size", ctypes.c_int32)] + [
+        (name, ctypes.c_void_p) for name in ("keep", "add", "held", "held_out", "row_offsets", "lens", "page_table",
+                                             "own_table", "row_seq", "positions", "slots", "missing")]
+
+
 def _load():
     if not os.path.exists(_LIB_PATH):
         raise ImportError(f"{_LIB_PATH} is not built; run `python -m paper_2606_26587_amd.build`")
@@ -125,6 +137,21 @@ def _load():
     L.sharq_attention.restype = ctypes.c_int
     L.sharq_attention.argtypes = [c_vp, ctypes.c_int, c_i64, c_i64, cache_p, batch_p, attn_p, c_vp, c_i64, c_vp, c_vp,
                                   ctypes.c_size_t, c_vp]
+    pool_p, requests_p = ctypes.POINTER(KVPoolStruct), ctypes.POINTER(KVRequestsStruct)
+    L.sharq_kv_assign_workspace_bytes.restype = ctypes.c_size_t
+    L.sharq_kv_assign_workspace_bytes.argtypes = [requests_p]
+    L.sharq_kv_assign.restype = ctypes.c_int
+    L.sharq_kv_assign.argtypes = [pool_p, requests_p, c_vp, ctypes.c_size_t, c_vp]
+    L.sharq_beam_workspace_bytes.restype = ctypes.c_size_t
+    L.sharq_beam_workspace_bytes.argtypes = [c_i64, c_i64, c_i64]
+    L.sharq_beam_select.restype = ctypes.c_int
+    L.sharq_beam_select.argtypes = [c_vp, ctypes.c_int, c_i64, c_i64, c_i64, c_i64, c_vp, c_vp, ctypes.c_int32, c_vp,
+                                    c_vp, c_vp, c_vp, c_vp, ctypes.c_size_t, c_vp]
+    L.sharq_beam_reorder.restype = ctypes.c_int
+    L.sharq_beam_reorder.argtypes = [c_i64, c_i64, c_vp, c_vp, ctypes.c_int32, c_vp, c_i64, c_vp, c_i64, c_i64, c_vp,
+                                     c_vp, c_vp, c_i64, c_vp, c_i64, c_i64, c_vp]
+    L.sharq_kv_copy.restype = ctypes.c_int
+    L.sharq_kv_copy.argtypes = [cache_p, c_vp, c_i64, c_vp]
     return L
 
 
@@ -304,6 +331,98 @@ class KVBatch:
         least = -1 if seqs == 0 or self.rows == 0 else self.max_len
         self.__dict__.update(device_index=self.lens.get_device(), table_pages=self.page_table.shape[1],
                              table_tokens=least, ref=ctypes.byref(struct))
+
+
+def _ints(t: Optional[torch.Tensor], shape, device, where: str) -> Optional[int]:
+    """Address of a contiguous int32 tensor of this shape on this device (None: NULL)."""
+    if t is None:
+        return None
+    if t.dtype is not torch.int32 or tuple(t.shape) != shape or not t.is_contiguous() or t.device != device:
+        raise SharqError(EINVAL, where)
+    return t.data_ptr()
+
+
+def _int_rows(t: torch.Tensor, rows: int, device, where: str) -> int:
+    """Row stride of an int32 matrix [rows, width] on this device, its rows contiguous."""
+    if t.dtype is not torch.int32 or t.dim() != 2 or t.shape[0] != rows or t.device != device:
+        raise SharqError(EINVAL, where)
+    width = t.shape[1]
+    if rows <= 1:
+        ld = width          # the stride of a single row means nothing
+    else:
+        ld = t.stride(0)
+    if (width > 1 and t.stride(1) != 1) or ld < width:
+        raise SharqError(EINVAL, where)
+    return ld
+
+
+@dataclass(frozen=True)
+class KVPool:
+    """Pages that no sequence holds, as a stack on the GPU (sharq_kv_pool): free_pages int32 [pages], of which the first
+    `count` (int32 [1]) are free and the last of these is given out first; count_out: the count after a call (None: the
+    same word)."""
+    free_pages: torch.Tensor
+    count: torch.Tensor
+    count_out: Optional[torch.Tensor] = None
+
+    def __post_init__(self):
+        dev, out = self.free_pages.device, self.count if self.count_out is None else self.count_out
+        pages = self.free_pages.numel()
+        struct = KVPoolStruct(pages, _ints(self.free_pages, (pages,), dev, "KVPool"),
+                              *(_ints(t, (1,), dev, "KVPool") for t in (self.count, out)))
+        self.__dict__.update(pages=pages, device_index=self.free_pages.get_device(), ref=ctypes.byref(struct))
+
+
+def alloc_kv_pool(pages: int, device="cuda") -> KVPool:
+    """A pool of `pages` free pages; page 0 is given out first."""
+    return KVPool(torch.arange(pages - 1, -1, -1, dtype=torch.int32, device=device),
+                  torch.full((1,), pages, dtype=torch.int32, device=device))
+
+
+@dataclass(frozen=True)
+class KVRequests:
+    """The requests of a step (sharq_kv_requests), int32 tensors on the GPU: keep, add, held [seqs] (cached tokens that
+    stay, tokens that come, columns of the page table that are filled); row_offsets [seqs + 1], lens [seqs] (it may be
+    `keep`) and page_table [seqs, n], written by sharq_kv_assign and then those of a KVBatch; rows: entries of the row
+    arrays; max_len: no sequence gets longer.  Optional: held_out [seqs] (None: `held` itself), own_table like
+    page_table, row_seq, positions, slots [rows], missing [1]."""
+    keep: torch.Tensor
+    add: torch.Tensor
+    held: torch.Tensor
+    row_offsets: torch.Tensor
+    lens: torch.Tensor
+    page_table: torch.Tensor
+    rows: int
+    max_len: int
+    page_size: int
+    held_out: Optional[torch.Tensor] = None
+    own_table: Optional[torch.Tensor] = None
+    row_seq: Optional[torch.Tensor] = None
+    positions: Optional[torch.Tensor] = None
+    slots: Optional[torch.Tensor] = None
+    missing: Optional[torch.Tensor] = None
+
+    def __post_init__(self):
+        where, dev, seqs = "KVRequests", self.keep.device, self.keep.numel()
+        table, own = self.page_table, self.own_table
+        ld = _int_rows(table, seqs, dev, where)
+        if own is not None and (own.shape != table.shape or _int_rows(own, seqs, dev, where) != ld):
+            raise SharqError(EINVAL, where)
+        if self.rows < 0 or self.max_len < 0 or self.page_size < 1 or (
+                seqs > 0 and -(-self.max_len // self.page_size) > table.shape[1]):
+            raise SharqError(EINVAL, where)
+        out = self.held if self.held_out is None else self.held_out
+        per_seq = [_ints(t, (seqs,), dev, where) for t in (self.keep, self.add, self.held, out)]
+        struct = KVRequestsStruct(seqs, self.rows, self.max_len, ld, self.page_size, *per_seq,
+                                  _ints(self.row_offsets, (seqs + 1,), dev, where), _ints(self.lens, (seqs,), dev, where),
+                                  table.data_ptr(), _ptr(own),
+                                  *(_ints(t, (self.rows,), dev, where) for t in (self.row_seq, self.positions, self.slots)),
+                                  _ints(self.missing, (1,), dev, where))
+        self.__dict__.update(device_index=self.keep.get_device(), device=dev, ref=ctypes.byref(struct))
+
+    def batch(self, max_rows: int) -> KVBatch:
+        """The KVBatch that the tables describe once sharq_kv_assign has written them."""
+        return KVBatch(self.row_offsets, self.lens, self.page_table, self.rows, max_rows, self.max_len)
 
 
 def alloc_kv_cache(pages: int, page_size: int, kv_heads: int, head_dim: int, fmt: str = "bf16", device="cuda",
@@ -637,6 +756,134 @@ def sharq_attention(q: torch.Tensor, cache: KVCache, batch: KVBatch, scale: Opti
     if status:
         raise SharqError(status, where)
     return out
+
+
+def kv_assign_workspace_bytes(requests: KVRequests) -> int:
+    """Bytes of workspace of sharq_kv_assign for these sizes."""
+    return lib.sharq_kv_assign_workspace_bytes(requests.ref)
+
+
+def _workspace(workspace: Optional[torch.Tensor], size: int, dev: int, stream, where: str):
+    """(buffer, bytes): the caller's, or one of the call's own stream, freed on return and taken again only behind it."""
+    if workspace is None:
+        with _on(stream):
+            workspace = torch.empty(max(size, 1), dtype=torch.uint8, device=torch.device("cuda", dev))
+    elif workspace.get_device() != dev or not workspace.is_contiguous():
+        raise SharqError(EINVAL, where)
+    return workspace, workspace.nbytes
+
+
+def sharq_kv_assign(pool: KVPool, requests: KVRequests, workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Row offsets, lengths, page tables and slot maps of a step from the requests' lengths, on the GPU: pages of tokens
+    that are dropped go back to the pool, new columns are given pages (-1 where there are none)."""
+    where = "sharq_kv_assign"
+    dev = requests.device_index
+    if dev < 0 or dev != pool.device_index or dev != _device():
+        raise SharqError(EINVAL, where)
+    workspace, size = _workspace(workspace, 0 if workspace is not None else kv_assign_workspace_bytes(requests), dev,
+                                 stream, where)
+    _check(lib.sharq_kv_assign(pool.ref, requests.ref, workspace.data_ptr(), size, _stream(stream)), where)
+
+
+def beam_workspace_bytes(groups: int, beams: int, vocab: int) -> int:
+    """Bytes of workspace of sharq_beam_select for these sizes."""
+    return lib.sharq_beam_workspace_bytes(groups, beams, vocab)
+
+
+def _flat(t: Optional[torch.Tensor], dtype, shape, dev: int, where: str) -> Optional[int]:
+    """Address of a contiguous tensor of this type and shape on device `dev` (None: NULL)."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or t.get_device() != dev:
+        raise SharqError(EINVAL, where)
+    return t.data_ptr()
+
+
+def sharq_beam_select(logits: torch.Tensor, scores: torch.Tensor, done: Optional[torch.Tensor] = None, eos: int = -1,
+                      scores_out: Optional[torch.Tensor] = None, parents: Optional[torch.Tensor] = None,
+                      tokens: Optional[torch.Tensor] = None, done_out: Optional[torch.Tensor] = None,
+                      workspace: Optional[torch.Tensor] = None, stream=None):
+    """Beam search's choice of the next tokens.  logits [groups * beams, vocab] (bf16, fp16 or fp32; rows may be
+    strided), scores fp32 [groups, beams]; done: uint8 [groups, beams], beams that have ended with token eos.  Returns
+    (scores, parents, tokens, done) [groups, beams], the best first; scores_out and done_out may be `scores` and
+    `done`.  done is None without it."""
+    where = "sharq_beam_select"
+    dev = logits.get_device()
+    if dev < 0 or dev != _device() or logits.dim() != 2 or scores.dim() != 2:
+        raise SharqError(EINVAL, where)
+    (groups, beams), (rows, vocab) = scores.shape, logits.shape
+    if rows != groups * beams or (vocab > 1 and logits.stride(1) != 1):
+        raise SharqError(EINVAL, where)
+    ld = logits.stride(0) if rows > 1 else vocab
+    shape = (groups, beams)
+    with _on(stream):
+        if scores_out is None:
+            scores_out = torch.empty(shape, dtype=torch.float32, device=logits.device)
+        if parents is None:
+            parents = torch.empty(shape, dtype=torch.int32, device=logits.device)
+        if tokens is None:
+            tokens = torch.empty(shape, dtype=torch.int32, device=logits.device)
+        if done_out is None and done is not None:
+            done_out = torch.empty(shape, dtype=torch.uint8, device=logits.device)
+    pointers = [_flat(t, dtype, shape, dev, where) for t, dtype in (
+        (scores, torch.float32), (done, torch.uint8), (scores_out, torch.float32), (parents, torch.int32),
+        (tokens, torch.int32), (done_out, torch.uint8))]
+    workspace, size = _workspace(workspace, 0 if workspace is not None else beam_workspace_bytes(groups, beams, vocab),
+                                 dev, stream, where)
+    _check(lib.sharq_beam_select(logits.data_ptr(), _DT.get(logits.dtype, -1), ld, groups, beams, vocab, *pointers[:2],
+                                 eos, *pointers[2:], workspace.data_ptr(), size, _stream(stream)), where)
+    return scores_out, parents, tokens, done_out
+
+
+def sharq_beam_reorder(parents: torch.Tensor, lens: torch.Tensor, page_table: Optional[torch.Tensor], page_size: int,
+                       tokens: Optional[torch.Tensor] = None, ids: Optional[torch.Tensor] = None,
+                       table_out: Optional[torch.Tensor] = None, ids_out: Optional[torch.Tensor] = None,
+                       copies: Optional[torch.Tensor] = None, stream=None) -> Optional[torch.Tensor]:
+    """The beams' page tables and token ids behind a choice: parents int32 [groups, beams], lens int32 [groups * beams]
+    (a group's beams have the same), page_table int32 [groups * beams, n] or None, ids int32 [groups * beams, n] with the
+    chosen tokens, or None.  table_out, ids_out: None, in place.  Returns copies int32 [groups * beams, 3], what
+    sharq_kv_copy has to do in every layer's cache (None without a table)."""
+    where = "sharq_beam_reorder"
+    dev = parents.get_device()
+    if dev < 0 or dev != _device() or parents.dim() != 2:
+        raise SharqError(EINVAL, where)
+    device, (groups, beams) = parents.device, parents.shape
+    rows = groups * beams
+    p = _ints(parents, (groups, beams), device, where)
+    n = _ints(lens, (rows,), device, where)
+    tk = _ints(tokens, (groups, beams), device, where)
+    ldt = ldto = cols = ldi = ldio = id_cols = 0
+    if page_table is not None:
+        table_out = page_table if table_out is None else table_out
+        ldt, ldto, cols = _int_rows(page_table, rows, device, where), _int_rows(table_out, rows, device, where), page_table.shape[1]
+        if copies is None:
+            with _on(stream):
+                copies = torch.empty((rows, 3), dtype=torch.int32, device=device)
+        if table_out.shape != page_table.shape:
+            raise SharqError(EINVAL, where)
+    elif table_out is not None or copies is not None:
+        raise SharqError(EINVAL, where)
+    if ids is not None:
+        ids_out = ids if ids_out is None else ids_out
+        ldi, ldio, id_cols = _int_rows(ids, rows, device, where), _int_rows(ids_out, rows, device, where), ids.shape[1]
+        if ids_out.shape != ids.shape:
+            raise SharqError(EINVAL, where)
+    elif ids_out is not None:
+        raise SharqError(EINVAL, where)
+    _check(lib.sharq_beam_reorder(groups, beams, p, n, page_size, _ptr(page_table), ldt, _ptr(table_out), ldto, cols,
+                                  _ints(copies, (rows, 3), device, where), tk, _ptr(ids), ldi, _ptr(ids_out), ldio,
+                                  id_cols, _stream(stream)), where)
+    return copies
+
+
+def sharq_kv_copy(cache: KVCache, copies: torch.Tensor, stream=None) -> None:
+    """Copies the first tokens of pages into other pages: copies int32 [n, 3], (source, destination, tokens)."""
+    where = "sharq_kv_copy"
+    dev = cache.device_index
+    if dev < 0 or dev != _device() or copies.dim() != 2:
+        raise SharqError(EINVAL, where)
+    at = _flat(copies, torch.int32, (copies.shape[0], 3), dev, where)
+    _check(lib.sharq_kv_copy(cache.ref, at, copies.shape[0], _stream(stream)), where)
 
 
 def stack_weights(ws: Sequence[QuantWeight]) -> QuantWeight:
