@@ -70,9 +70,9 @@ __device__ __forceinline__ uint64_t wave_max64(uint64_t x) {
 
 // A part of a row: workgroup (row, chunk), whose wavefronts work apart, each on its 2048 of a turn's 8192 logits.  An
 // entry of a list: the value's order above, the complement of its column below, so that of equal values the lower
-// column is the better.
+// column is the better.  A list takes whatever may still be chosen, unsorted; it is cut to the best when it grows.
 template <typename T>
-__global__ __launch_bounds__(256) void k_beam_scan(BeamArgs a) {
+__global__ __launch_bounds__(256, 4) void k_beam_scan(BeamArgs a) {
   constexpr int kVec = 16 / (int)sizeof(T), kLoads = kBeamPer / kVec;
   __shared__ uint64_t lds_list[4][kListCap], lds_best[4][kMaxBeams];
   const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -80,27 +80,40 @@ __global__ __launch_bounds__(256) void k_beam_scan(BeamArgs a) {
   if (a.done && a.done[row]) return;   // its one candidate needs no logits
   const T* const x = static_cast<const T*>(a.logits) + (int64_t)row * a.ld;
   uint64_t *const list = lds_list[wave], *const best = lds_best[wave];
-  int have = 0;                      // entries of best[]
-  float least = -__builtin_inff();   // what a value has to pass: that of the last of `beams` entries
+  int n = 0;                         // entries of list[], at most half of it between turns
+  float least = -__builtin_inff();   // what a value has to pass: `beams` that are listed reach it
   float ref = -__builtin_inff();
   double sum = 0.0;
-  for (int tile = chunk * a.tiles; tile < (chunk + 1) * a.tiles; ++tile) {
-    const int base = tile * kBeamTile + wave * (64 * kBeamPer);
-    if (base >= a.vocab) break;
-    float v[kBeamPer];
-    if (base + 64 * kBeamPer <= a.vocab) {   // all loads on their way together
-      Vec<T, kVec> w[kLoads];
+  Vec<T, kVec> w[kLoads] = {};       // a turn's logits, on their way during the turn before
+  auto load = [&](int base) {
+    if (base + 64 * kBeamPer <= a.vocab)
 #pragma unroll
       for (int k = 0; k < kLoads; ++k) w[k] = *reinterpret_cast<const Vec<T, kVec>*>(x + base + (k * 64 + lane) * kVec);
+  };
+  auto cut = [&] {   // to the best, and what the last of them says
+    wave_sync();
+    best_of(list, n, a.beams, best);
+    wave_sync();
+    n = n < a.beams ? n : a.beams;
+    if (lane < n) list[lane] = best[lane];
+    if (n == a.beams) least = value32((uint32_t)(best[n - 1] >> 32));
+  };
+  const int end = (chunk + 1) * a.tiles * kBeamTile < a.vocab ? (chunk + 1) * a.tiles * kBeamTile : a.vocab;
+  int base = chunk * a.tiles * kBeamTile + wave * (64 * kBeamPer);
+  if (base < end) load(base);
+  for (; base < end; base += kBeamTile) {
+    float v[kBeamPer];
 #pragma unroll
-      for (int i = 0; i < kBeamPer; ++i) v[i] = as_float(w[i / kVec].v[i % kVec]);
-    } else {
+    for (int i = 0; i < kBeamPer; ++i) v[i] = as_float(w[i / kVec].v[i % kVec]);
+    if (base + 64 * kBeamPer > a.vocab) {   // the row ends in this turn
+      const int from = base + lane * kVec;
 #pragma unroll
       for (int i = 0; i < kBeamPer; ++i) {
-        const int at = base + (i / kVec * 64 + lane) * kVec + i % kVec;
+        const int at = from + i / kVec * 64 * kVec + i % kVec;
         v[i] = at < a.vocab ? as_float(x[at]) : -__builtin_inff();
       }
     }
+    if (base + kBeamTile < end) load(base + kBeamTile);
     float top = v[0];
 #pragma unroll
     for (int i = 1; i < kBeamPer; ++i) top = __builtin_fmaxf(top, v[i]);
@@ -123,9 +136,9 @@ __global__ __launch_bounds__(256) void k_beam_scan(BeamArgs a) {
     }
     const unsigned long long above = __ballot(top > least);
     if (above == 0) continue;
+    float bound = value32(order32(least) + 1);   // the next number above
     // Where many lanes have something, the `beams`-th of their best is a bound as well: so many values reach it.
-    uint32_t bound = order32(least) + 1;
-    if (__popcll(above) > a.beams) {
+    if (__popcll(above) > 2 * a.beams || (n == 0 && __popcll(above) > a.beams)) {
       const uint32_t mine = order32(top);
       int rank = 0;
 #pragma unroll 8
@@ -134,48 +147,47 @@ __global__ __launch_bounds__(256) void k_beam_scan(BeamArgs a) {
         rank += o > mine || (o == mine && j < lane);
       }
       const int l = __builtin_ctzll(__ballot(rank == a.beams - 1));
-      const uint32_t at = (uint32_t)__builtin_amdgcn_readlane((int)mine, l);
-      bound = at > bound ? at : bound;
+      const float at = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(top), l));
+      if (at > least) bound = least = at;
     }
-    wave_sync();
-    for (int i = lane; i < have; i += 64) list[i] = best[i];
-    int n = have;
+    const int before = n;
+    int first = base + lane * kVec;   // columns are made from it where they are needed: 32 of them would be kept
+    asm volatile("" : "+v"(first));
 #pragma unroll
     for (int i = 0; i < kBeamPer; ++i) {
-      const uint32_t o = order32(v[i]);
-      const bool in = o >= bound && v[i] == v[i];
+      const bool in = v[i] >= bound;
       const unsigned long long who = __ballot(in);
       if (who) {
         const int to = n + __popcll(who & ((1ull << lane) - 1));
-        const int col = base + (i / kVec * 64 + lane) * kVec + i % kVec;
-        if (in && to < kListCap) list[to] = (uint64_t)o << 32 | (uint32_t)~col;
+        const int col = first + i / kVec * 64 * kVec + i % kVec;
+        if (in && to < kListCap) list[to] = (uint64_t)order32(v[i]) << 32 | (uint32_t)~col;
         n += __popcll(who);
       }
     }
-    wave_sync();
-    if (n <= kListCap) {
-      best_of(list, n, a.beams, best);
-      have = n < a.beams ? n : a.beams;
-    } else {   // more values at the bound than the list holds: one after the other
-      uint64_t last = ~0ull;
-      const uint64_t old = lane < have ? best[lane] : 0;
+    if (n > kListCap) {   // more values at the bound than the list holds (they are equal, or sorted): one after the other
       wave_sync();
-      for (have = 0; have < a.beams; ++have) {
-        uint64_t mine = old < last ? old : 0;
-#pragma unroll
-        for (int i = 0; i < kBeamPer; ++i) {
+      const uint64_t old0 = lane < before ? list[lane] : 0, old1 = lane + 64 < before ? list[lane + 64] : 0;
+      uint64_t last = ~0ull;
+      wave_sync();
+      for (n = 0; n < a.beams; ++n) {
+        uint64_t mine = old0 < last ? old0 : 0;
+        if (old1 < last && old1 > mine) mine = old1;
+#pragma unroll 1
+        for (int i = 0; i < kBeamPer; ++i) {   // read anew: an entry of each, kept, would take 64 registers
           const int col = base + (i / kVec * 64 + lane) * kVec + i % kVec;
-          const uint64_t e = (uint64_t)order32(v[i]) << 32 | (uint32_t)~col;
-          if (v[i] > -__builtin_inff() && e < last && e > mine) mine = e;
+          const float y = col < a.vocab ? as_float(x[col]) : -__builtin_inff();
+          const uint64_t e = (uint64_t)order32(y) << 32 | (uint32_t)~col;
+          if (y > -__builtin_inff() && e < last && e > mine) mine = e;
         }
         mine = wave_max64(mine);
         if (mine == 0) break;
-        if (lane == 0) best[have] = mine;
+        if (lane == 0) list[n] = mine;
         last = mine;
       }
+      if (n == a.beams) least = value32((uint32_t)(last >> 32));
+    } else if (n > kListCap / 2) {
+      cut();
     }
-    wave_sync();
-    if (have == a.beams) least = value32((uint32_t)(best[have - 1] >> 32));
   }
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
@@ -185,11 +197,12 @@ __global__ __launch_bounds__(256) void k_beam_scan(BeamArgs a) {
   }
   const int64_t part = (int64_t)row * a.chunks + chunk;
   if (lane == 0) a.parts[part * 4 + wave] = BeamPart{sum, ref, 0};
-  for (int i = have + lane; i < a.beams; i += 64) best[i] = 0;
+  cut();
+  if (lane >= n && lane < a.beams) best[lane] = 0;
   __syncthreads();
   if (wave != 0) return;
   // the four lists' best; entries of 0 are none
-  int n = 0;
+  n = 0;
   for (int i = 0; i < 4 * a.beams; i += 64) {
     const int at = i + lane;
     const uint64_t e = at < 4 * a.beams ? lds_best[at / a.beams][at % a.beams] : 0;
@@ -217,6 +230,8 @@ __global__ __launch_bounds__(256) void k_beam_pick(BeamArgs a) {
   extern __shared__ uint64_t lds[];
   __shared__ double base_of[kMaxBeams], lse_of[kMaxBeams];
   __shared__ uint8_t done_of[kMaxBeams];
+  __shared__ BeamPart part_of[kBeamLists];
+  __shared__ double term_of[kBeamLists];
   __shared__ BeamKey bound_of[4];
   __shared__ int count;
   const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6, beams = a.beams;
@@ -228,29 +243,37 @@ __global__ __launch_bounds__(256) void k_beam_pick(BeamArgs a) {
   const uint64_t* const from = a.lists + row0 * a.chunks * beams;
   for (int i = tid; i < entries; i += 256) entry[i] = from[i];   // a beam that is done left its own unwritten
   if (tid == 0) count = 0;
-  for (int b = wave; b < beams; b += 4) {
-    const bool done = a.done && a.done[row0 + b];
-    float top = -__builtin_inff();
-    double sum = 0.0;
-    const BeamPart* const parts = a.parts + (row0 + b) * a.chunks * 4;
-    if (!done) {
-      for (int i = lane; i < a.chunks * 4; i += 64) top = __builtin_fmaxf(top, parts[i].top);
+  if (tid < 4) bound_of[tid] = BeamKey{0, 0};
+  if (tid < beams) {
+    done_of[tid] = a.done && a.done[row0 + tid];
+    base_of[tid] = (double)a.scores[row0 + tid];
+  }
+  const int b = tid < lists ? tid / a.chunks : 0;
+  // the sums: a thread has its list's four, then a thread a beam
+  float top = -__builtin_inff();
+  double sum = 0.0;
+  if (tid < lists) {
+    const BeamPart* const p = a.parts + (row0 * a.chunks + tid) * 4;
+    const BeamPart q[4] = {p[0], p[1], p[2], p[3]};
+    top = __builtin_fmaxf(__builtin_fmaxf(q[0].top, q[1].top), __builtin_fmaxf(q[2].top, q[3].top));
 #pragma unroll
-      for (int d = 1; d < 64; d <<= 1) top = __builtin_fmaxf(top, __shfl_xor(top, d));
-      for (int i = lane; i < a.chunks * 4; i += 64)
-        if (parts[i].sum != 0.0) sum += parts[i].sum * exp((double)parts[i].top - (double)top);
-#pragma unroll
-      for (int d = 1; d < 64; d <<= 1) {
-        const uint64_t u = __builtin_bit_cast(uint64_t, sum);
-        sum += __builtin_bit_cast(double, (uint64_t)(uint32_t)__shfl_xor((int)(uint32_t)u, d) |
-                                              (uint64_t)(uint32_t)__shfl_xor((int)(uint32_t)(u >> 32), d) << 32);
-      }
-    }
-    if (lane == 0) {
-      done_of[b] = done;
-      base_of[b] = (double)a.scores[row0 + b];
-      lse_of[b] = (double)top + log(sum);   // no logit: -inf - inf, and no candidate
-    }
+    for (int i = 0; i < 4; ++i)
+      if (q[i].sum != 0.0) sum += q[i].top == top ? q[i].sum : q[i].sum * exp((double)q[i].top - (double)top);
+    part_of[tid].sum = sum, part_of[tid].top = top;
+  }
+  __syncthreads();
+  if (tid < lists) {
+    float all = top;
+    for (int i = 0; i < a.chunks; ++i) all = __builtin_fmaxf(all, part_of[b * a.chunks + i].top);
+    if (sum != 0.0 && top != all) sum *= exp((double)top - (double)all);
+    term_of[tid] = sum;
+    if (tid % a.chunks == 0) lse_of[b] = (double)all;
+  }
+  __syncthreads();
+  if (tid < beams && !done_of[tid]) {
+    double s = 0.0;
+    for (int i = 0; i < a.chunks; ++i) s += term_of[tid * a.chunks + i];
+    lse_of[tid] += log(s);   // no logit: -inf - inf, and no candidate
   }
   __syncthreads();
   auto key_of = [&](int b, uint64_t e) {
@@ -266,20 +289,21 @@ __global__ __launch_bounds__(256) void k_beam_pick(BeamArgs a) {
     if (total > -__builtin_inf()) k.order = order64(total);
     return k;
   };
-  const int b = tid < lists ? tid / a.chunks : 0;
   const bool mine = tid < lists && (!done_of[b] || tid % a.chunks == 0);
   BeamKey head{0, 0};
   if (mine) head = key_of(b, entry[tid * beams]);
+  // equal orders: lists go by beam and column, as places do
   int rank = 0;
-  for (int j = 0; j < 64; ++j) {
-    const BeamKey o{(uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)head.order, j) |
-                        (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(head.order >> 32), j) << 32,
-                    (uint32_t)__builtin_amdgcn_readlane((int)head.at, j)};
-    rank += better(o, head) || (o.order == head.order && o.at == head.at && j < lane);
+  const int here = lists - wave * 64 < 64 ? lists - wave * 64 : 64;
+  for (int j = 0; j < here; ++j) {
+    const uint64_t o = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)head.order, j) |
+                       (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(head.order >> 32), j) << 32;
+    rank += o > head.order || (o == head.order && j < lane);
   }
-  if (rank == beams - 1) bound_of[wave] = head;
+  if (lane < here && rank == beams - 1) bound_of[wave] = head;
   __syncthreads();
   BeamKey bound = bound_of[0];
+#pragma unroll
   for (int w = 1; w < 4; ++w)
     if (better(bound_of[w], bound)) bound = bound_of[w];
   if (mine) {
