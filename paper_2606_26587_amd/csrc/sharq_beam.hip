@@ -58,6 +58,50 @@ __device__ __forceinline__ void best_of(const uint64_t* list, int n, int most, u
   }
 }
 
+// The largest of a wavefront's values (NaN does not count), the same in every lane: by data-parallel moves, which take a
+// tenth of the time of six exchanges through LDS.
+template <int CTRL>
+__device__ __forceinline__ float max_moved(float x) {
+  const int o = __builtin_amdgcn_update_dpp(__float_as_int(x), __float_as_int(x), CTRL, 0xF, 0xF, false);
+  return __builtin_fmaxf(x, __int_as_float(o));
+}
+__device__ __forceinline__ float wave_max(float x) {
+  x = max_moved<0x111>(x);   // rows of 16: shifted by 1, 2, 4, 8
+  x = max_moved<0x112>(x);
+  x = max_moved<0x114>(x);
+  x = max_moved<0x118>(x);
+  x = max_moved<0x142>(x);   // the last of a row to the next, of the first half to the second
+  x = max_moved<0x143>(x);
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
+}
+
+// Their sum in the last lane.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double sum_moved(double x) {
+  const uint64_t b = __builtin_bit_cast(uint64_t, x);
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)b, CTRL, ROWS, 0xF, false);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(b >> 32), CTRL, ROWS, 0xF, false);
+  return x + __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ double wave_sum(double x) {
+  x = sum_moved<0x111, 0xF>(x);
+  x = sum_moved<0x112, 0xF>(x);
+  x = sum_moved<0x114, 0xF>(x);
+  x = sum_moved<0x118, 0xF>(x);
+  x = sum_moved<0x142, 0xA>(x);   // into rows 1 and 3
+  return sum_moved<0x143, 0xC>(x);   // into rows 2 and 3
+}
+
+// x times 2^e, e a whole number of any size (not above 0).
+__device__ __forceinline__ double times_exp2(double x, double e) { return __builtin_amdgcn_ldexp(x, e > -4000.0 ? (int)e : -4000); }
+
+// The whole exponent of a reference, and what is left of it (a reference past 2^53 has nothing left).
+__device__ __forceinline__ double exponent_of(float ref, float& rest) {
+  const double y = (double)ref * 1.44269504088896341, e = __builtin_rint(y);
+  rest = (float)(y - e);
+  return e;
+}
+
 __device__ __forceinline__ uint64_t wave_max64(uint64_t x) {
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
@@ -77,13 +121,13 @@ __global__ __launch_bounds__(256, 4) void k_beam_scan(BeamArgs a) {
   __shared__ uint64_t lds_list[4][kListCap], lds_best[4][kMaxBeams];
   const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int row = (int)(blockIdx.x / (unsigned)a.chunks), chunk = (int)(blockIdx.x % (unsigned)a.chunks);
-  if (a.done && a.done[row]) return;   // its one candidate needs no logits
   const T* const x = static_cast<const T*>(a.logits) + (int64_t)row * a.ld;
   uint64_t *const list = lds_list[wave], *const best = lds_best[wave];
   int n = 0;                         // entries of list[], at most half of it between turns
   float least = -__builtin_inff();   // what a value has to pass: `beams` that are listed reach it
   float ref = -__builtin_inff();
-  double sum = 0.0;
+  float rest = 0.0f;
+  double sum = 0.0, exponent = -__builtin_inf();
   Vec<T, kVec> w[kLoads] = {};       // a turn's logits, on their way during the turn before
   auto load = [&](int base) {
     if (base + 64 * kBeamPer <= a.vocab)
@@ -101,6 +145,7 @@ __global__ __launch_bounds__(256, 4) void k_beam_scan(BeamArgs a) {
   const int end = (chunk + 1) * a.tiles * kBeamTile < a.vocab ? (chunk + 1) * a.tiles * kBeamTile : a.vocab;
   int base = chunk * a.tiles * kBeamTile + wave * (64 * kBeamPer);
   if (base < end) load(base);
+  if (a.done && a.done[row]) return;   // its one candidate needs no logits
   for (; base < end; base += kBeamTile) {
     float v[kBeamPer];
 #pragma unroll
@@ -117,17 +162,17 @@ __global__ __launch_bounds__(256, 4) void k_beam_scan(BeamArgs a) {
     float top = v[0];
 #pragma unroll
     for (int i = 1; i < kBeamPer; ++i) top = __builtin_fmaxf(top, v[i]);
-    float all = top;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) all = __builtin_fmaxf(all, __shfl_xor(all, d));
+    const float all = wave_max(top);
+    // Terms are 2^((x - ref) log2 e + rest) = e^x 2^-exponent, with a whole exponent: sums move from one to another exactly.
     if (all > ref + kRefStep || (ref == -__builtin_inff() && all > ref)) {
-      sum *= exp2((double)(ref - all) * 1.44269504088896341);   // 0 of the first reference's
-      ref = all;
+      const double e = exponent_of(all, rest);
+      sum = times_exp2(sum, exponent - e);   // 0 of the first reference's
+      ref = all, exponent = e;
     }
     if (ref != -__builtin_inff()) {
       float s[8] = {};
 #pragma unroll
-      for (int i = 0; i < kBeamPer; ++i) s[i & 7] += __builtin_amdgcn_exp2f((v[i] - ref) * kLog2e);
+      for (int i = 0; i < kBeamPer; ++i) s[i & 7] += __builtin_amdgcn_exp2f(__builtin_fmaf(v[i] - ref, kLog2e, rest));
       sum += (double)(((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7])));
     } else {   // nothing yet, unless it is a NaN
 #pragma unroll
@@ -189,14 +234,9 @@ __global__ __launch_bounds__(256, 4) void k_beam_scan(BeamArgs a) {
       cut();
     }
   }
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const uint64_t b = __builtin_bit_cast(uint64_t, sum);
-    sum += __builtin_bit_cast(double, (uint64_t)(uint32_t)__shfl_xor((int)(uint32_t)b, d) |
-                                          (uint64_t)(uint32_t)__shfl_xor((int)(uint32_t)(b >> 32), d) << 32);
-  }
+  sum = wave_sum(sum);
   const int64_t part = (int64_t)row * a.chunks + chunk;
-  if (lane == 0) a.parts[part * 4 + wave] = BeamPart{sum, ref, 0};
+  if (lane == 63) a.parts[part * 4 + wave] = BeamPart{sum, ref, 0};
   cut();
   if (lane >= n && lane < a.beams) best[lane] = 0;
   __syncthreads();
@@ -216,68 +256,78 @@ __global__ __launch_bounds__(256, 4) void k_beam_scan(BeamArgs a) {
   for (int i = n + lane; i < a.beams; i += 64) out[i] = 0;
 }
 
-struct BeamKey {
+struct __attribute__((aligned(16))) BeamKey {
   uint64_t order;   // of the score, 0: none
-  uint32_t at;      // beam * vocab + token
+  uint32_t at, pad;   // beam * vocab + token
 };
 __device__ __forceinline__ bool better(const BeamKey& x, const BeamKey& y) {
   return x.order > y.order || (x.order == y.order && x.at < y.at);
 }
 
-// Joins a group's lists.  A thread has one list, whose entries come best first: the `beams`-th best of a wavefront's
-// first entries bounds what can be chosen, and what reaches the bound is ranked.
+// Joins a group's lists.  A thread has one list, whose entries come best first.  As `beams` lists reach the `beams`-th of
+// a wavefront's first entries, nothing below can be chosen; what is not below it is ranked.
 __global__ __launch_bounds__(256) void k_beam_pick(BeamArgs a) {
   extern __shared__ uint64_t lds[];
   __shared__ double base_of[kMaxBeams], lse_of[kMaxBeams];
   __shared__ uint8_t done_of[kMaxBeams];
   __shared__ BeamPart part_of[kBeamLists];
-  __shared__ double term_of[kBeamLists];
-  __shared__ BeamKey bound_of[4];
+  __shared__ uint32_t bound_of[4];
   __shared__ int count;
-  const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6, beams = a.beams;
+  const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), beams = a.beams;
   const int lists = beams * a.chunks, entries = lists * beams;
-  uint64_t* const entry = lds;                       // [lists][beams]
-  uint64_t* const order = lds + entries;             // of those that reach the bound: their orders, and
-  uint32_t* const place = reinterpret_cast<uint32_t*>(order + (lists + 63) / 64 * beams * beams);   // their places
+  BeamKey* const found = reinterpret_cast<BeamKey*>(lds);         // up to as many as there are entries
+  uint64_t* const entry = lds + 2 * entries;                      // [lists][beams]
   const int64_t row0 = (int64_t)blockIdx.x * beams;
   const uint64_t* const from = a.lists + row0 * a.chunks * beams;
-  for (int i = tid; i < entries; i += 256) entry[i] = from[i];   // a beam that is done left its own unwritten
-  if (tid == 0) count = 0;
-  if (tid < 4) bound_of[tid] = BeamKey{0, 0};
-  if (tid < beams) {
-    done_of[tid] = a.done && a.done[row0 + tid];
-    base_of[tid] = (double)a.scores[row0 + tid];
-  }
   const int b = tid < lists ? tid / a.chunks : 0;
-  // the sums: a thread has its list's four, then a thread a beam
-  float top = -__builtin_inff();
-  double sum = 0.0;
-  if (tid < lists) {
+  BeamPart q[4] = {};
+  if (tid < lists) {   // all loads on their way together (a beam that is done left its own unwritten)
     const BeamPart* const p = a.parts + (row0 * a.chunks + tid) * 4;
-    const BeamPart q[4] = {p[0], p[1], p[2], p[3]};
-    top = __builtin_fmaxf(__builtin_fmaxf(q[0].top, q[1].top), __builtin_fmaxf(q[2].top, q[3].top));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) q[i] = p[i];
+  }
+  uint8_t done = 0;
+  float score = 0.0f;
+  if (tid < beams) {
+    if (a.done) done = a.done[row0 + tid];
+    score = a.scores[row0 + tid];
+  }
+  for (int i = tid; i < entries; i += 256) entry[i] = from[i];
+  if (tid == 0) count = 0;
+  if (tid < beams) done_of[tid] = done != 0, base_of[tid] = (double)score;
+  // a thread's four parts of a sum, then a wavefront a beam
+  {
+    const float top = __builtin_fmaxf(__builtin_fmaxf(q[0].ref, q[1].ref), __builtin_fmaxf(q[2].ref, q[3].ref));
+    float rest;
+    const double exponent = exponent_of(top, rest);
+    double sum = 0.0;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      if (q[i].sum != 0.0) sum += q[i].top == top ? q[i].sum : q[i].sum * exp((double)q[i].top - (double)top);
-    part_of[tid].sum = sum, part_of[tid].top = top;
+      if (q[i].sum != 0.0) sum += times_exp2(q[i].sum, exponent_of(q[i].ref, rest) - exponent);
+    if (tid < lists) part_of[tid] = BeamPart{sum, top, 0};
   }
   __syncthreads();
-  if (tid < lists) {
-    float all = top;
-    for (int i = 0; i < a.chunks; ++i) all = __builtin_fmaxf(all, part_of[b * a.chunks + i].top);
-    if (sum != 0.0 && top != all) sum *= exp((double)top - (double)all);
-    term_of[tid] = sum;
-    if (tid % a.chunks == 0) lse_of[b] = (double)all;
-  }
-  __syncthreads();
-  if (tid < beams && !done_of[tid]) {
-    double s = 0.0;
-    for (int i = 0; i < a.chunks; ++i) s += term_of[tid * a.chunks + i];
-    lse_of[tid] += log(s);   // no logit: -inf - inf, and no candidate
+  for (int i = wave; i < beams; i += 4) {
+    BeamPart p{0.0, -__builtin_inff(), 0};
+    for (int c = lane; c < a.chunks; c += 64) {   // more than 64 where the beams are few
+      const BeamPart o = part_of[i * a.chunks + c];
+      float rest;
+      const float top = __builtin_fmaxf(p.ref, o.ref);
+      const double e = exponent_of(top, rest);
+      double sum = o.sum != 0.0 ? times_exp2(o.sum, exponent_of(o.ref, rest) - e) : 0.0;
+      if (p.sum != 0.0) sum += times_exp2(p.sum, exponent_of(p.ref, rest) - e);
+      p = BeamPart{sum, top, 0};
+    }
+    float rest, left;
+    const float top = wave_max(p.ref);
+    const double e = exponent_of(top, left);
+    const double sum = wave_sum(p.sum != 0.0 ? times_exp2(p.sum, exponent_of(p.ref, rest) - e) : 0.0);
+    // no logit: -inf, and no candidate
+    if (lane == 63) lse_of[i] = (double)top + (log2(sum) - (double)left) * 0.69314718055994530942;
   }
   __syncthreads();
   auto key_of = [&](int b, uint64_t e) {
-    BeamKey k{0, 0};
+    BeamKey k{0, 0, 0};
     double total;
     if (done_of[b]) {
       total = base_of[b], k.at = (uint32_t)(b * a.vocab + a.eos);
@@ -290,27 +340,27 @@ __global__ __launch_bounds__(256) void k_beam_pick(BeamArgs a) {
     return k;
   };
   const bool mine = tid < lists && (!done_of[b] || tid % a.chunks == 0);
-  BeamKey head{0, 0};
+  BeamKey head{0, 0, 0};
   if (mine) head = key_of(b, entry[tid * beams]);
-  // equal orders: lists go by beam and column, as places do
-  int rank = 0;
-  const int here = lists - wave * 64 < 64 ? lists - wave * 64 : 64;
-  for (int j = 0; j < here; ++j) {
-    const uint64_t o = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)head.order, j) |
-                       (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(head.order >> 32), j) << 32;
-    rank += o > head.order || (o == head.order && j < lane);
-  }
-  if (lane < here && rank == beams - 1) bound_of[wave] = head;
-  __syncthreads();
-  BeamKey bound = bound_of[0];
+  // The upper halves of the orders will do: the largest one that `beams` first entries reach.
+  const uint32_t upper = (uint32_t)(head.order >> 32);
+  int reach = 0;
+#pragma unroll 8
+  for (int j = 0; j < 64; ++j) reach += (uint32_t)__builtin_amdgcn_readlane((int)upper, j) >= upper;
+  uint32_t bound = reach >= beams ? upper : 0;
 #pragma unroll
-  for (int w = 1; w < 4; ++w)
-    if (better(bound_of[w], bound)) bound = bound_of[w];
+  for (int d = 1; d < 64; d <<= 1) {
+    const uint32_t o = (uint32_t)__shfl_xor((int)bound, d);
+    bound = o > bound ? o : bound;
+  }
+  if (lane == 0) bound_of[wave] = bound;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < 4; ++w) bound = bound_of[w] > bound ? bound_of[w] : bound;
   if (mine) {
     BeamKey k = head;
-    for (int i = 0; k.order != 0 && !better(bound, k);) {
-      const int to = atomicAdd(&count, 1);   // in any order: the places are ranked below
-      order[to] = k.order, place[to] = k.at;
+    for (int i = 0; k.order != 0 && (uint32_t)(k.order >> 32) >= bound;) {
+      found[atomicAdd(&count, 1)] = k;   // in any order: they are ranked below
       if (++i == beams || done_of[b]) break;
       k = key_of(b, entry[tid * beams + i]);
     }
@@ -318,9 +368,10 @@ __global__ __launch_bounds__(256) void k_beam_pick(BeamArgs a) {
   __syncthreads();
   const int n = count;
   for (int i = tid; i < n; i += 256) {
-    const BeamKey k{order[i], place[i]};
+    const BeamKey k = found[i];
     int r = 0;
-    for (int j = 0; j < n; ++j) r += better(BeamKey{order[j], place[j]}, k);
+#pragma unroll 4
+    for (int j = 0; j < n; ++j) r += better(found[j], k);
     if (r >= beams) continue;
     const int parent = (int)(k.at / (uint32_t)a.vocab), token = (int)(k.at % (uint32_t)a.vocab);
     a.scores_out[row0 + r] = (float)value64(k.order);

@@ -44,11 +44,8 @@ constexpr int kBeamTile = 256 * kBeamPer;           // of a workgroup
 constexpr int kBeamLists = 256;                     // candidate lists of a group: a thread each in the second kernel
 constexpr int64_t kBeamLds = 60 << 10;              // what that kernel keeps in LDS at most
 
-// Bytes of LDS that joins the lists of `chunks` parts of a row: the lists, and the candidates that reach the bound, of
-// each wavefront's lists at most `beams`, whole.
-constexpr int64_t beam_lds(int64_t beams, int64_t chunks) {
-  return beams * beams * (8 * chunks + 12 * ceil_div(beams * chunks, 64));
-}
+// Bytes of LDS that joins the lists of `chunks` parts of a row: their entries, and as many candidates.
+constexpr int64_t beam_lds(int64_t beams, int64_t chunks) { return beams * beams * chunks * (8 + 16); }
 
 struct BeamSplit {
   int chunks, tiles;   // workgroups of a row of logits; their turns
@@ -64,10 +61,11 @@ constexpr BeamSplit beam_split(int64_t rows, int64_t beams, int64_t vocab) {
   return {(int)ceil_div(tiles, each), (int)each};
 }
 
-// A wavefront's part of a row's sum of exponentials: sum of e^(x - top).
+// A wavefront's part of a row's sum: the sum of 2^((x - ref) log2 e + rest), which is that of e^x times 2^-e, where e is
+// ref log2 e to the nearest whole number and rest what that leaves.
 struct BeamPart {
   double sum;
-  float top;
+  float ref;
   int32_t pad;
 };
 
