@@ -655,7 +655,7 @@ SHARQ_API size_t sharq_beam_workspace_bytes(int64_t groups, int64_t beams, int64
  * score or logits hold a NaN or whose logits hold +inf.  Where a group has fewer than `beams`
  * candidates, the places behind have score -inf, token -1 and themselves as parent.
  * Scores are compared in 64 bits, whatever their rounding to scores_out.
- * groups * beams is at most 2^20, beams * vocab below 2^31.  workspace: 8-byte aligned.
+ * groups * beams is at most 2^20, beams * vocab at most 2^30.  workspace: 8-byte aligned.
  */
 SHARQ_API sharq_status sharq_beam_select(const void *logits, sharq_dtype dtype, int64_t ld, int64_t groups,
                                          int64_t beams, int64_t vocab, const float *scores, const uint8_t *done,

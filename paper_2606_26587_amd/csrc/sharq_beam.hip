@@ -20,6 +20,7 @@ namespace sharq {
 
 constexpr float kLog2e = 1.44269504088896341f;
 constexpr float kRefStep = 8.0f;
+constexpr float kRefFast = 1000.0f;   // z below 2^-16: its third power is nothing in 64 bits
 constexpr int kListCap = 256;   // entries of a wavefront's list, while a turn's candidates join it
 
 // An order of whole numbers that is the floats'; -0 counts as 0.
@@ -38,14 +39,21 @@ __device__ __forceinline__ double value64(uint64_t k) {
   return __builtin_bit_cast(double, k >> 63 ? k ^ 0x8000000000000000ull : ~k);
 }
 
+// 16 bytes of logits, at any element's address.
+typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+typedef v4u v4u_any __attribute__((aligned(2)));
+
 template <typename T>
 __device__ __forceinline__ float as_float(T x) { return (float)x; }
 
-// 16 bytes at any element's address.
-template <typename T, int N>
-struct __attribute__((packed, aligned(sizeof(T)))) Vec {
-  T v[N];
-};
+// Logit i of 16 bytes.
+template <typename T>
+__device__ __forceinline__ float logit(v4u w, int i) {
+  if (sizeof(T) == 4) return __uint_as_float(w[i]);
+  const uint32_t x = w[i / 2];
+  if (__is_same(T, __bf16)) return i % 2 ? bf16_hi(x) : bf16_lo(x);
+  return (float)__builtin_bit_cast(_Float16, (uint16_t)(i % 2 ? x >> 16 : x));
+}
 
 // The `most` best of list[0..n) to out, best first; by one wavefront.  All entries differ.
 __device__ __forceinline__ void best_of(const uint64_t* list, int n, int most, uint64_t* out) {
@@ -112,53 +120,78 @@ __device__ __forceinline__ uint64_t wave_max64(uint64_t x) {
   return x;
 }
 
-// A part of a row: workgroup (row, chunk), whose wavefronts work apart, each on its 2048 of a turn's 8192 logits.  An
-// entry of a list: the value's order above, the complement of its column below, so that of equal values the lower
-// column is the better.  A list takes whatever may still be chosen, unsorted; it is cut to the best when it grows.
+// An entry of a sorted list: the value's order above, the complement of its column below, so that of equal values the
+// lower column is the better.
+__device__ __forceinline__ uint64_t entry_of(float x, int col) { return (uint64_t)order32(x) << 32 | (uint32_t)~col; }
+
+// Inclusive sum over a wavefront's lanes.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int add_moved(int x) { return x + __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xF, false); }
+__device__ __forceinline__ int wave_scan(int x) {
+  x = add_moved<0x111, 0xF>(x);
+  x = add_moved<0x112, 0xF>(x);
+  x = add_moved<0x114, 0xF>(x);
+  x = add_moved<0x118, 0xF>(x);
+  x = add_moved<0x142, 0xA>(x);
+  return add_moved<0x143, 0xC>(x);
+}
+
+// A part of a row: workgroup (row, chunk), whose wavefronts work apart, each on its 2048 of a turn's 8192 logits.  A
+// list takes the columns of whatever may still be chosen; it is sorted, and cut to the best, when it grows and at the
+// end.
 template <typename T>
 __global__ __launch_bounds__(256, 4) void k_beam_scan(BeamArgs a) {
   constexpr int kVec = 16 / (int)sizeof(T), kLoads = kBeamPer / kVec;
-  __shared__ uint64_t lds_list[4][kListCap], lds_best[4][kMaxBeams];
+  __shared__ uint64_t lds_entry[4][kListCap], lds_best[4][kMaxBeams];
+  __shared__ int lds_list[4][kListCap];
   const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int row = (int)(blockIdx.x / (unsigned)a.chunks), chunk = (int)(blockIdx.x % (unsigned)a.chunks);
   const T* const x = static_cast<const T*>(a.logits) + (int64_t)row * a.ld;
-  uint64_t *const list = lds_list[wave], *const best = lds_best[wave];
+  uint64_t *const entry = lds_entry[wave], *const best = lds_best[wave];
+  int* const list = lds_list[wave];
   int n = 0;                         // entries of list[], at most half of it between turns
   float least = -__builtin_inff();   // what a value has to pass: `beams` that are listed reach it
   float ref = -__builtin_inff();
   float rest = 0.0f;
   double sum = 0.0, exponent = -__builtin_inf();
-  Vec<T, kVec> w[kLoads] = {};       // a turn's logits, on their way during the turn before
-  auto load = [&](int base) {
-    if (base + 64 * kBeamPer <= a.vocab)
+  v4u w[kLoads];   // a turn's logits, on their way during the turn before
+  const bool some = a.vocab >= kVec;
+  auto load = [&](int base) {   // where the row has ended: others of it
 #pragma unroll
-      for (int k = 0; k < kLoads; ++k) w[k] = *reinterpret_cast<const Vec<T, kVec>*>(x + base + (k * 64 + lane) * kVec);
+    for (int k = 0; k < kLoads; ++k) {
+      const int at = base + (k * 64 + lane) * kVec;
+      w[k] = *reinterpret_cast<const v4u_any*>(x + (at + kVec <= a.vocab ? at : 0));
+    }
   };
   auto cut = [&] {   // to the best, and what the last of them says
     wave_sync();
-    best_of(list, n, a.beams, best);
+    for (int i = lane; i < n; i += 64) entry[i] = entry_of(as_float(x[list[i]]), list[i]);
+    wave_sync();
+    best_of(entry, n, a.beams, best);
     wave_sync();
     n = n < a.beams ? n : a.beams;
-    if (lane < n) list[lane] = best[lane];
+    if (lane < n) list[lane] = (int)~(uint32_t)best[lane];
     if (n == a.beams) least = value32((uint32_t)(best[n - 1] >> 32));
   };
   const int end = (chunk + 1) * a.tiles * kBeamTile < a.vocab ? (chunk + 1) * a.tiles * kBeamTile : a.vocab;
   int base = chunk * a.tiles * kBeamTile + wave * (64 * kBeamPer);
-  if (base < end) load(base);
+  if (base < end && some) load(base);
   if (a.done && a.done[row]) return;   // its one candidate needs no logits
   for (; base < end; base += kBeamTile) {
     float v[kBeamPer];
 #pragma unroll
-    for (int i = 0; i < kBeamPer; ++i) v[i] = as_float(w[i / kVec].v[i % kVec]);
-    if (base + 64 * kBeamPer > a.vocab) {   // the row ends in this turn
-      const int from = base + lane * kVec;
+    for (int i = 0; i < kBeamPer; ++i) v[i] = logit<T>(w[i / kVec], i % kVec);
+    if (base + 64 * kBeamPer > a.vocab) {   // the row ends in this turn, perhaps inside of 16 bytes
+      const int over = a.vocab % kVec, whole = a.vocab - over;
+      const float mine = lane < over ? as_float(x[whole + lane]) : -__builtin_inff();
 #pragma unroll
       for (int i = 0; i < kBeamPer; ++i) {
-        const int at = from + i / kVec * 64 * kVec + i % kVec;
-        v[i] = at < a.vocab ? as_float(x[at]) : -__builtin_inff();
+        const int at = base + (i / kVec * 64 + lane) * kVec;
+        const float o = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(mine), i % kVec));
+        v[i] = at < whole ? v[i] : at == whole ? o : -__builtin_inff();
       }
     }
-    if (base + kBeamTile < end) load(base + kBeamTile);
+    if (base + kBeamTile < end && some) load(base + kBeamTile);
     float top = v[0];
 #pragma unroll
     for (int i = 1; i < kBeamPer; ++i) top = __builtin_fmaxf(top, v[i]);
@@ -171,9 +204,20 @@ __global__ __launch_bounds__(256, 4) void k_beam_scan(BeamArgs a) {
     }
     if (ref != -__builtin_inff()) {
       float s[8] = {};
+      double part = 1.0;
+      if (__builtin_fabsf(ref) < kRefFast) {
+        // x log2 e - exponent in one step.  The constant's error counts for x, not x - ref: ref's part of it, z, is taken
+        // out of the sum.
+        const float e = -(float)exponent;
 #pragma unroll
-      for (int i = 0; i < kBeamPer; ++i) s[i & 7] += __builtin_amdgcn_exp2f(__builtin_fmaf(v[i] - ref, kLog2e, rest));
-      sum += (double)(((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7])));
+        for (int i = 0; i < kBeamPer; ++i) s[i & 7] += __builtin_amdgcn_exp2f(__builtin_fmaf(v[i], kLog2e, e));
+        const double z = (double)ref * ((1.44269504088896341 - (double)kLog2e) * 0.69314718055994531);
+        part = 1.0 + z * (1.0 + 0.5 * z);
+      } else {
+#pragma unroll
+        for (int i = 0; i < kBeamPer; ++i) s[i & 7] += __builtin_amdgcn_exp2f(__builtin_fmaf(v[i] - ref, kLog2e, rest));
+      }
+      sum += part * (double)(((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7])));
     } else {   // nothing yet, unless it is a NaN
 #pragma unroll
       for (int i = 0; i < kBeamPer; ++i)
@@ -195,38 +239,38 @@ __global__ __launch_bounds__(256, 4) void k_beam_scan(BeamArgs a) {
       const float at = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(top), l));
       if (at > least) bound = least = at;
     }
-    const int before = n;
-    int first = base + lane * kVec;   // columns are made from it where they are needed: 32 of them would be kept
-    asm volatile("" : "+v"(first));
+    uint32_t in = 0;   // the lane's logits that reach the bound, the first in the highest bit
 #pragma unroll
-    for (int i = 0; i < kBeamPer; ++i) {
-      const bool in = v[i] >= bound;
-      const unsigned long long who = __ballot(in);
-      if (who) {
-        const int to = n + __popcll(who & ((1ull << lane) - 1));
-        const int col = first + i / kVec * 64 * kVec + i % kVec;
-        if (in && to < kListCap) list[to] = (uint64_t)order32(v[i]) << 32 | (uint32_t)~col;
-        n += __popcll(who);
-      }
+    for (int i = 0; i < kBeamPer; ++i) in = 2 * in + (v[i] >= bound);
+    const int mine = __popc(in), upto = wave_scan(mine), before = n;
+    n += __builtin_amdgcn_readlane(upto, 63);
+    for (int to = before + upto - mine; in; ++to) {
+      const int i = __builtin_clz(in);
+      in &= ~(0x80000000u >> i);
+      if (to < kListCap) list[to] = base + (i / kVec * 64 + lane) * kVec + i % kVec;
     }
     if (n > kListCap) {   // more values at the bound than the list holds (they are equal, or sorted): one after the other
       wave_sync();
-      const uint64_t old0 = lane < before ? list[lane] : 0, old1 = lane + 64 < before ? list[lane + 64] : 0;
-      uint64_t last = ~0ull;
+      uint64_t old[2], last = ~0ull;
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int at = lane + 64 * k;
+        old[k] = at < before ? entry_of(as_float(x[list[at]]), list[at]) : 0;
+      }
       wave_sync();
       for (n = 0; n < a.beams; ++n) {
-        uint64_t mine = old0 < last ? old0 : 0;
-        if (old1 < last && old1 > mine) mine = old1;
+        uint64_t mine = old[0] < last ? old[0] : 0;
+        if (old[1] < last && old[1] > mine) mine = old[1];
 #pragma unroll 1
         for (int i = 0; i < kBeamPer; ++i) {   // read anew: an entry of each, kept, would take 64 registers
           const int col = base + (i / kVec * 64 + lane) * kVec + i % kVec;
           const float y = col < a.vocab ? as_float(x[col]) : -__builtin_inff();
-          const uint64_t e = (uint64_t)order32(y) << 32 | (uint32_t)~col;
+          const uint64_t e = entry_of(y, col);
           if (y > -__builtin_inff() && e < last && e > mine) mine = e;
         }
         mine = wave_max64(mine);
         if (mine == 0) break;
-        if (lane == 0) list[n] = mine;
+        if (lane == 0) list[n] = (int)~(uint32_t)mine;
         last = mine;
       }
       if (n == a.beams) least = value32((uint32_t)(last >> 32));
@@ -247,12 +291,12 @@ __global__ __launch_bounds__(256, 4) void k_beam_scan(BeamArgs a) {
     const int at = i + lane;
     const uint64_t e = at < 4 * a.beams ? lds_best[at / a.beams][at % a.beams] : 0;
     const unsigned long long is = __ballot(e != 0);
-    if (e) list[n + __popcll(is & ((1ull << lane) - 1))] = e;
+    if (e) entry[n + __popcll(is & ((1ull << lane) - 1))] = e;
     n += __popcll(is);
   }
   wave_sync();
   uint64_t* const out = a.lists + part * a.beams;
-  best_of(list, n, a.beams, out);
+  best_of(entry, n, a.beams, out);
   for (int i = n + lane; i < a.beams; i += 64) out[i] = 0;
 }
 

@@ -20,6 +20,7 @@ using namespace sharq;
 
 constexpr int64_t kMaxColumns = (int64_t)1 << 30;   // of all sequences: pages given out are counted in 32 bits
 constexpr int64_t kMaxBeamRows = (int64_t)1 << 20;
+constexpr int64_t kMaxCandidates = (int64_t)1 << 30;   // of a group
 
 bool page_size_ok(int64_t p) { return p >= 1 && (p & (p - 1)) == 0; }
 
@@ -44,7 +45,7 @@ sharq_status check_choice(int64_t groups, int64_t beams, int64_t vocab) {
   const sharq_status s = check_beams(groups, beams);
   if (s != SHARQ_OK) return s;
   if (vocab < 1) return SHARQ_EINVAL;
-  return vocab > INT_MAX / beams ? SHARQ_EUNSUPPORTED : SHARQ_OK;
+  return vocab > kMaxCandidates / beams ? SHARQ_EUNSUPPORTED : SHARQ_OK;
 }
 
 }  // namespace
