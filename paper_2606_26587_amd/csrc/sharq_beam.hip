@@ -21,7 +21,7 @@ namespace sharq {
 constexpr float kLog2e = 1.44269504088896341f;
 constexpr float kRefStep = 8.0f;
 constexpr float kRefFast = 1000.0f;   // z below 2^-16: its third power is nothing in 64 bits
-constexpr int kListCap = 256;   // entries of a wavefront's list, while a turn's candidates join it
+constexpr int kListCap = 256;   // entries of a wavefront's list
 
 // An order of whole numbers that is the floats'; -0 counts as 0.
 __device__ __forceinline__ uint32_t order32(float x) {
@@ -124,33 +124,46 @@ __device__ __forceinline__ uint64_t wave_max64(uint64_t x) {
 // lower column is the better.
 __device__ __forceinline__ uint64_t entry_of(float x, int col) { return (uint64_t)order32(x) << 32 | (uint32_t)~col; }
 
-// Inclusive sum over a wavefront's lanes.
-template <int CTRL, int ROWS>
-__device__ __forceinline__ int add_moved(int x) { return x + __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xF, false); }
-__device__ __forceinline__ int wave_scan(int x) {
-  x = add_moved<0x111, 0xF>(x);
-  x = add_moved<0x112, 0xF>(x);
-  x = add_moved<0x114, 0xF>(x);
-  x = add_moved<0x118, 0xF>(x);
-  x = add_moved<0x142, 0xA>(x);
-  return add_moved<0x143, 0xC>(x);
+// The `most`-th largest of n values in LDS (n is at least that), by one wavefront.
+__device__ __forceinline__ float least_of(const float* value, int n, int most) {
+  float found = -__builtin_inff();
+  for (int i = (int)threadIdx.x & 63; i < n; i += 64) {
+    const float x = value[i];
+    int reach = 0;
+#pragma unroll 8
+    for (int j = 0; j < n; ++j) reach += value[j] >= x;
+    if (reach >= most) found = __builtin_fmaxf(found, x);
+  }
+  return wave_max(found);
 }
 
-// A part of a row: workgroup (row, chunk), whose wavefronts work apart, each on its 2048 of a turn's 8192 logits.  A
-// list takes the columns of whatever may still be chosen; it is sorted, and cut to the best, when it grows and at the
-// end.
+// The same of the wavefront's own values, one a lane.
+__device__ __forceinline__ float least_of_lanes(float x, int most) {
+  int reach = 0;
+#pragma unroll 16
+  for (int j = 0; j < 64; ++j) reach += __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), j)) >= x;
+  return wave_max(reach >= most ? x : -__builtin_inff());
+}
+
+// A part of a row: workgroup (row, chunk), whose wavefronts work apart, each on its 2048 of a turn's 8192 logits.  During
+// the walk only a lane's largest of a turn is looked at: its 32 logits are listed where that may still be chosen.  The
+// `beams`-th largest of such maxima is a bound (so many logits reach it), and at the end the few turns of a lane whose
+// maximum reaches the last bound, about `beams` of them, are read once more.
 template <typename T>
-__global__ __launch_bounds__(256, 4) void k_beam_scan(BeamArgs a) {
+__global__ __launch_bounds__(256) void k_beam_scan(BeamArgs a) {
   constexpr int kVec = 16 / (int)sizeof(T), kLoads = kBeamPer / kVec;
   __shared__ uint64_t lds_entry[4][kListCap], lds_best[4][kMaxBeams];
-  __shared__ int lds_list[4][kListCap];
+  __shared__ float lds_value[4][kListCap];
+  __shared__ int lds_turn[4][kListCap];
   const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int row = (int)(blockIdx.x / (unsigned)a.chunks), chunk = (int)(blockIdx.x % (unsigned)a.chunks);
   const T* const x = static_cast<const T*>(a.logits) + (int64_t)row * a.ld;
   uint64_t *const entry = lds_entry[wave], *const best = lds_best[wave];
-  int* const list = lds_list[wave];
-  int n = 0;                         // entries of list[], at most half of it between turns
-  float least = -__builtin_inff();   // what a value has to pass: `beams` that are listed reach it
+  float* const value = lds_value[wave];    // of a listed turn of a lane: its largest logit, and
+  int* const turn = lds_turn[wave];        // its first column
+  int n = 0;                         // how many there are
+  bool full = false;                 // more than the list holds are equal to the bound
+  float least = -__builtin_inff();   // what has to be passed: `beams` logits before reach it
   float ref = -__builtin_inff();
   float rest = 0.0f;
   double sum = 0.0, exponent = -__builtin_inf();
@@ -163,21 +176,29 @@ __global__ __launch_bounds__(256, 4) void k_beam_scan(BeamArgs a) {
       w[k] = *reinterpret_cast<const v4u_any*>(x + (at + kVec <= a.vocab ? at : 0));
     }
   };
-  auto cut = [&] {   // to the best, and what the last of them says
+  auto cut = [&] {   // the list to what reaches its own bound
     wave_sync();
-    for (int i = lane; i < n; i += 64) entry[i] = entry_of(as_float(x[list[i]]), list[i]);
+    if (n >= a.beams) least = __builtin_fmaxf(least, least_of(value, n, a.beams));
+    int kept = 0;
+    for (int i = 0; i < n; i += 64) {
+      const float y = i + lane < n ? value[i + lane] : -__builtin_inff();
+      const int t = i + lane < n ? turn[i + lane] : 0;
+      const unsigned long long who = __ballot(i + lane < n && y >= least);
+      wave_sync();
+      if ((who >> lane) & 1) {
+        const int to = kept + __popcll(who & ((1ull << lane) - 1));
+        value[to] = y, turn[to] = t;
+      }
+      kept += __popcll(who);
+    }
+    n = kept;
     wave_sync();
-    best_of(entry, n, a.beams, best);
-    wave_sync();
-    n = n < a.beams ? n : a.beams;
-    if (lane < n) list[lane] = (int)~(uint32_t)best[lane];
-    if (n == a.beams) least = value32((uint32_t)(best[n - 1] >> 32));
   };
   const int end = (chunk + 1) * a.tiles * kBeamTile < a.vocab ? (chunk + 1) * a.tiles * kBeamTile : a.vocab;
-  int base = chunk * a.tiles * kBeamTile + wave * (64 * kBeamPer);
-  if (base < end && some) load(base);
+  const int begin = chunk * a.tiles * kBeamTile + wave * (64 * kBeamPer);
+  if (begin < end && some) load(begin);
   if (a.done && a.done[row]) return;   // its one candidate needs no logits
-  for (; base < end; base += kBeamTile) {
+  for (int base = begin; base < end; base += kBeamTile) {
     float v[kBeamPer];
 #pragma unroll
     for (int i = 0; i < kBeamPer; ++i) v[i] = logit<T>(w[i / kVec], i % kVec);
@@ -223,66 +244,63 @@ __global__ __launch_bounds__(256, 4) void k_beam_scan(BeamArgs a) {
       for (int i = 0; i < kBeamPer; ++i)
         if (v[i] != v[i]) sum = __builtin_nan("");
     }
-    const unsigned long long above = __ballot(top > least);
-    if (above == 0) continue;
-    float bound = value32(order32(least) + 1);   // the next number above
-    // Where many lanes have something, the `beams`-th of their best is a bound as well: so many values reach it.
-    if (__popcll(above) > 2 * a.beams || (n == 0 && __popcll(above) > a.beams)) {
-      const uint32_t mine = order32(top);
-      int rank = 0;
-#pragma unroll 8
-      for (int j = 0; j < 64; ++j) {
-        const uint32_t o = (uint32_t)__builtin_amdgcn_readlane((int)mine, j);
-        rank += o > mine || (o == mine && j < lane);
-      }
-      const int l = __builtin_ctzll(__ballot(rank == a.beams - 1));
-      const float at = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(top), l));
-      if (at > least) bound = least = at;
+    unsigned long long who = __ballot(top > least);
+    if (__popcll(who) > (n == 0 ? a.beams : 2 * a.beams)) {
+      const float bound = least_of_lanes(top, a.beams);
+      if (bound > least) least = bound, who = __ballot(top >= least);
     }
-    uint32_t in = 0;   // the lane's logits that reach the bound, the first in the highest bit
-#pragma unroll
-    for (int i = 0; i < kBeamPer; ++i) in = 2 * in + (v[i] >= bound);
-    const int mine = __popc(in), upto = wave_scan(mine), before = n;
-    n += __builtin_amdgcn_readlane(upto, 63);
-    for (int to = before + upto - mine; in; ++to) {
-      const int i = __builtin_clz(in);
-      in &= ~(0x80000000u >> i);
-      if (to < kListCap) list[to] = base + (i / kVec * 64 + lane) * kVec + i % kVec;
-    }
-    if (n > kListCap) {   // more values at the bound than the list holds (they are equal, or sorted): one after the other
-      wave_sync();
-      uint64_t old[2], last = ~0ull;
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const int at = lane + 64 * k;
-        old[k] = at < before ? entry_of(as_float(x[list[at]]), list[at]) : 0;
+    if (who) {
+      if ((who >> lane) & 1) {
+        const int to = n + __popcll(who & ((1ull << lane) - 1));
+        value[to] = top, turn[to] = base + lane * kVec;
       }
-      wave_sync();
-      for (n = 0; n < a.beams; ++n) {
-        uint64_t mine = old[0] < last ? old[0] : 0;
-        if (old[1] < last && old[1] > mine) mine = old[1];
-#pragma unroll 1
-        for (int i = 0; i < kBeamPer; ++i) {   // read anew: an entry of each, kept, would take 64 registers
-          const int col = base + (i / kVec * 64 + lane) * kVec + i % kVec;
-          const float y = col < a.vocab ? as_float(x[col]) : -__builtin_inff();
-          const uint64_t e = entry_of(y, col);
-          if (y > -__builtin_inff() && e < last && e > mine) mine = e;
-        }
-        mine = wave_max64(mine);
-        if (mine == 0) break;
-        if (lane == 0) list[n] = (int)~(uint32_t)mine;
-        last = mine;
-      }
-      if (n == a.beams) least = value32((uint32_t)(last >> 32));
-    } else if (n > kListCap / 2) {
-      cut();
+      n += __popcll(who);
+      if (n > kListCap - 64) cut();
+      if (n > kListCap - 64) full = true, n = 0;
     }
   }
   sum = wave_sum(sum);
   const int64_t part = (int64_t)row * a.chunks + chunk;
   if (lane == 63) a.parts[part * 4 + wave] = BeamPart{sum, ref, 0};
   cut();
-  if (lane >= n && lane < a.beams) best[lane] = 0;
+  int found = 0;
+  if (!full) {
+    for (int i = 0; i < n * kBeamPer; i += 64) {   // two turns of a lane at a time
+      const int at = i + lane, k = at % kBeamPer;
+      const int col = at < n * kBeamPer ? turn[at / kBeamPer] + k / kVec * 64 * kVec + k % kVec : a.vocab;
+      const float y = col < a.vocab ? as_float(x[col]) : -__builtin_inff();
+      const unsigned long long who = __ballot(y >= least && y > -__builtin_inff());
+      const int to = found + __popcll(who & ((1ull << lane) - 1));
+      if (((who >> lane) & 1) && to < kListCap) entry[to] = entry_of(y, col);
+      found += __popcll(who);
+    }
+    wave_sync();
+    if (found <= kListCap) {
+      best_of(entry, found, a.beams, best);
+      found = found < a.beams ? found : a.beams;
+    } else {
+      full = true;
+    }
+  }
+  if (full) {   // rows of equal values: the best of all, one after the other
+    uint64_t last = ~0ull;
+    for (found = 0; found < a.beams; ++found) {
+      uint64_t mine = 0;
+      for (int base = begin; base < end; base += kBeamTile)
+#pragma unroll 8
+        for (int i = 0; i < kBeamPer; ++i) {
+          const int col = base + i * 64 + lane;
+          const float y = col < a.vocab ? as_float(x[col]) : -__builtin_inff();
+          const uint64_t e = entry_of(y, col);
+          if (y > -__builtin_inff() && e < last && e > mine) mine = e;
+        }
+      mine = wave_max64(mine);
+      if (mine == 0) break;
+      if (lane == 0) best[found] = mine;
+      last = mine;
+    }
+  }
+  if (lane >= found && lane < a.beams) best[lane] = 0;
   __syncthreads();
   if (wave != 0) return;
   // the four lists' best; entries of 0 are none
