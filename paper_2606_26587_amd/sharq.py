@@ -758,6 +758,9 @@ def sharq_attention(q: torch.Tensor, cache: KVCache, batch: KVBatch, scale: Opti
     return out
 
 
+_F32, _I32, _U8 = torch.float32, torch.int32, torch.uint8
+
+
 def kv_assign_workspace_bytes(requests: KVRequests) -> int:
     """Bytes of workspace of sharq_kv_assign for these sizes."""
     return lib.sharq_kv_assign_workspace_bytes(requests.ref)
@@ -780,8 +783,8 @@ def sharq_kv_assign(pool: KVPool, requests: KVRequests, workspace: Optional[torc
     dev = requests.device_index
     if dev < 0 or dev != pool.device_index or dev != _device():
         raise SharqError(EINVAL, where)
-    workspace, size = _workspace(workspace, 0 if workspace is not None else kv_assign_workspace_bytes(requests), dev,
-                                 stream, where)
+    size = kv_assign_workspace_bytes(requests) if workspace is None else 0
+    workspace, size = _workspace(workspace, size, dev, stream, where)
     _check(lib.sharq_kv_assign(pool.ref, requests.ref, workspace.data_ptr(), size, _stream(stream)), where)
 
 
@@ -808,31 +811,48 @@ def sharq_beam_select(logits: torch.Tensor, scores: torch.Tensor, done: Optional
     (scores, parents, tokens, done) [groups, beams], the best first; scores_out and done_out may be `scores` and
     `done`.  done is None without it."""
     where = "sharq_beam_select"
-    dev = logits.get_device()
+    device, dev = logits.device, logits.get_device()
     if dev < 0 or dev != _device() or logits.dim() != 2 or scores.dim() != 2:
         raise SharqError(EINVAL, where)
-    (groups, beams), (rows, vocab) = scores.shape, logits.shape
-    if rows != groups * beams or (vocab > 1 and logits.stride(1) != 1):
+    shape = groups, beams = scores.shape
+    rows, vocab = logits.shape
+    ld, inner = logits.stride()
+    if rows != groups * beams or (inner != 1 and vocab > 1):
         raise SharqError(EINVAL, where)
-    ld = logits.stride(0) if rows > 1 else vocab
-    shape = (groups, beams)
-    with _on(stream):
-        if scores_out is None:
-            scores_out = torch.empty(shape, dtype=torch.float32, device=logits.device)
-        if parents is None:
-            parents = torch.empty(shape, dtype=torch.int32, device=logits.device)
-        if tokens is None:
-            tokens = torch.empty(shape, dtype=torch.int32, device=logits.device)
-        if done_out is None and done is not None:
-            done_out = torch.empty(shape, dtype=torch.uint8, device=logits.device)
-    pointers = [_flat(t, dtype, shape, dev, where) for t, dtype in (
-        (scores, torch.float32), (done, torch.uint8), (scores_out, torch.float32), (parents, torch.int32),
-        (tokens, torch.int32), (done_out, torch.uint8))]
-    workspace, size = _workspace(workspace, 0 if workspace is not None else beam_workspace_bytes(groups, beams, vocab),
-                                 dev, stream, where)
-    _check(lib.sharq_beam_select(logits.data_ptr(), _DT.get(logits.dtype, -1), ld, groups, beams, vocab, *pointers[:2],
-                                 eos, *pointers[2:], workspace.data_ptr(), size, _stream(stream)), where)
+    if rows <= 1:
+        ld = vocab          # the stride of a single row means nothing
+    p_scores, p_done = _flat(scores, _F32, shape, dev, where), _flat(done, _U8, shape, dev, where)
+    given = [_flat(t, dtype, shape, dev, where) for t, dtype in (
+        (scores_out, _F32), (parents, _I32), (tokens, _I32), (done_out, _U8)) if t is not None]
+    if stream is None or len(given) == 4:   # what a call allocates lies on its stream
+        scores_out, parents, tokens, done_out = _beam_outputs(scores_out, parents, tokens, done_out, done, shape, device)
+    else:
+        with _on(stream):
+            scores_out, parents, tokens, done_out = _beam_outputs(scores_out, parents, tokens, done_out, done, shape,
+                                                                  device)
+    if workspace is None:
+        workspace, size = _workspace(None, beam_workspace_bytes(groups, beams, vocab), dev, stream, where)
+    else:
+        workspace, size = _workspace(workspace, 0, dev, stream, where)
+    status = lib.sharq_beam_select(logits.data_ptr(), _DT.get(logits.dtype, -1), ld, groups, beams, vocab, p_scores,
+                                   p_done, eos, scores_out.data_ptr(), parents.data_ptr(), tokens.data_ptr(),
+                                   _ptr(done_out), workspace.data_ptr(), size, _stream(stream))
+    if status:
+        raise SharqError(status, where)
     return scores_out, parents, tokens, done_out
+
+
+def _beam_outputs(scores, parents, tokens, done_out, done, shape, device):
+    """The outputs that a call was not given."""
+    if scores is None:
+        scores = torch.empty(shape, dtype=_F32, device=device)
+    if parents is None:
+        parents = torch.empty(shape, dtype=_I32, device=device)
+    if tokens is None:
+        tokens = torch.empty(shape, dtype=_I32, device=device)
+    if done_out is None and done is not None:
+        done_out = torch.empty(shape, dtype=_U8, device=device)
+    return scores, parents, tokens, done_out
 
 
 def sharq_beam_reorder(parents: torch.Tensor, lens: torch.Tensor, page_table: Optional[torch.Tensor], page_size: int,
