@@ -17,24 +17,28 @@ __device__ __forceinline__ uint32_t add_most(uint32_t a, uint32_t b, uint32_t to
   return s < top ? s : top;
 }
 
-// Inclusive prefix of v over the workgroup's threads, saturating at top, and the total; `mem`: a word a wavefront.
+// Sum of v over the workgroup's threads before this one, saturating at top, and the total; `mem`: a word a wavefront,
+// another one than that of the scan before.
 __device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t top, uint32_t* mem, uint32_t& total) {
-  const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, waves = (int)blockDim.x >> 6;
+  const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  uint32_t x = v;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
-    const uint32_t o = (uint32_t)__shfl_up((int)v, d);
-    if (lane >= d) v = add_most(v, o, top);
+    const uint32_t o = (uint32_t)__shfl_up((int)x, d);
+    if (lane >= d) x = add_most(x, o, top);
   }
-  __syncthreads();   // the scan before is read
-  if (lane == 63) mem[wave] = v;
+  if (lane == 63) mem[wave] = x;
   __syncthreads();
-  uint32_t before = 0;
-  total = 0;
-  for (int w = 0; w < waves; ++w) {
-    if (w == wave) before = total;
-    total = add_most(total, mem[w], top);
+  uint32_t w = lane < kAssignThreads / 64 ? mem[lane] : 0;   // of all wavefronts, by each of them
+#pragma unroll
+  for (int d = 1; d < kAssignThreads / 64; d <<= 1) {
+    const uint32_t o = (uint32_t)__shfl_up((int)w, d);
+    if (lane >= d) w = add_most(w, o, top);
   }
-  return add_most(v, before, top);
+  total = (uint32_t)__builtin_amdgcn_readlane((int)w, kAssignThreads / 64 - 1);
+  const uint32_t before = wave ? (uint32_t)__builtin_amdgcn_readlane((int)w, wave ? wave - 1 : 0) : 0;
+  const uint32_t left = (uint32_t)__shfl_up((int)x, 1);
+  return lane ? add_most(left, before, top) : before;
 }
 
 // The page of the k-th column that the call fills: from the top of the stack down, -1 when it is empty.
@@ -79,80 +83,116 @@ __device__ __forceinline__ void assign_row(const AssignArgs& a, int there, int r
   }
 }
 
+// The pages in columns lo..hi-1 of a row of a table, 64 at a time and eight of these on their way together: f(whether
+// there is one, it).
+template <typename Fn>
+__device__ __forceinline__ void each_page(const int32_t* row, int lo, int hi, int pages, Fn f) {
+  const int lane = (int)threadIdx.x & 63;
+  for (int c0 = lo; c0 < hi; c0 += 512) {
+    int page[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) page[i] = c0 + 64 * i + lane < hi ? row[c0 + 64 * i + lane] : -1;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (c0 + 64 * i < hi) f(page[i] >= 0 && page[i] < pages, page[i]);
+  }
+}
+
 // One workgroup: offsets, lengths and columns of all sequences by prefix sums,
 // pages that go back onto the stack, and (WHOLE) the pages that leave it and the
-// rows.  256 sequences, 950 rows: one launch, a chain of three dependent loads
-// and two scans.
+// rows.  A chain of latencies: the count, the lengths, three scans, the pages
+// that go back read for their number and again for their places (columns may hold
+// none), which all wavefronts share.
 template <bool WHOLE>
 __global__ __launch_bounds__(kAssignThreads) void k_kv_assign(AssignArgs a) {
-  __shared__ uint32_t mem[kAssignThreads / 64];
+  constexpr int kItems = 2, kPass = kItems * kAssignThreads;
+  __shared__ uint32_t mem[3][kAssignThreads / 64];
   __shared__ int l_end[WHOLE ? kAssignSeqs : 1], l_given[WHOLE ? kAssignSeqs : 1], l_held[WHOLE ? kAssignSeqs : 1],
       l_len[WHOLE ? kAssignSeqs : 1];
-  const int tid = (int)threadIdx.x, lane = tid & 63;
+  __shared__ int g_seq[kPass], g_lo[kPass], g_hi[kPass], g_n[kPass], g_count;   // sequences that give pages back
+  const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int size = 1 << a.page_shift;
   const int on_stack = kv_clamp(*a.count, 0, a.pages);
   const int32_t* const from = a.own ? a.own : a.table;
+  const uint32_t top = (uint32_t)a.rows;
   uint32_t rows = 0, given = 0, back = 0;   // of the sequences before these
-  for (int s0 = 0; s0 < a.seqs; s0 += (int)blockDim.x) {
-    const int s = s0 + tid;
-    int keep = 0, add = 0, held = 0;
-    if (s < a.seqs) {
-      keep = kv_clamp(a.keep[s], 0, a.max_len);
-      add = kv_clamp(a.add[s], 0, a.max_len - keep);
-      held = kv_clamp(a.held[s], 0, a.cols);
+  for (int s0 = 0; s0 < a.seqs; s0 += kPass) {
+    int keep[kItems] = {}, add[kItems] = {}, held[kItems] = {};
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) {
+      const int s = s0 + tid * kItems + i;
+      if (s < a.seqs) keep[i] = a.keep[s], add[i] = a.add[s], held[i] = a.held[s];
     }
-    uint32_t total;
-    const uint32_t top = (uint32_t)a.rows;
-    const uint32_t in = (uint32_t)(add < a.rows ? add : a.rows);
-    const int end = (int)add_most(rows, block_scan(in, top, mem, total), top);
-    // exclusive: the end of the sequence before
-    int first = __shfl_up(end, 1);
-    {
-      __syncthreads();
-      if (lane == 63) mem[tid >> 6] = (uint32_t)end;
-      __syncthreads();
-      if (lane == 0) first = tid == 0 ? (int)rows : (int)mem[(tid >> 6) - 1];
+    if (tid == 0) g_count = 0;
+    uint32_t in[kItems], mine = 0, total;
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) {
+      keep[i] = kv_clamp(keep[i], 0, a.max_len);
+      add[i] = kv_clamp(add[i], 0, a.max_len - keep[i]);
+      held[i] = kv_clamp(held[i], 0, a.cols);
+      in[i] = (uint32_t)(add[i] < a.rows ? add[i] : a.rows);
+      mine = add_most(mine, in[i], top);
     }
+    uint32_t at = add_most(rows, block_scan(mine, top, mem[0], total), top);
     rows = add_most(rows, total, top);
-    const int len = keep + (end - first), need = (len + size - 1) >> a.page_shift;
-    const int fresh = need > held ? need - held : 0;
-    const uint32_t g = given + block_scan((uint32_t)fresh, 0x7FFFFFFFu, mem, total) - (uint32_t)fresh;
+    int first[kItems], len[kItems], need[kItems], fresh[kItems], place[kItems];
+    mine = 0;
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) {
+      first[i] = (int)at;
+      at = add_most(at, in[i], top);
+      len[i] = keep[i] + ((int)at - first[i]), need[i] = (len[i] + size - 1) >> a.page_shift;
+      fresh[i] = need[i] > held[i] ? need[i] - held[i] : 0;
+      mine += (uint32_t)fresh[i];
+      place[i] = -1;
+      if (held[i] > need[i]) {   // in any order: each has its own number
+        place[i] = atomicAdd(&g_count, 1);
+        g_seq[place[i]] = s0 + tid * kItems + i, g_lo[place[i]] = need[i], g_hi[place[i]] = held[i];
+      }
+    }
+    uint32_t g = given + block_scan(mine, 0x7FFFFFFFu, mem[1], total);   // behind its barrier the list is whole
     given += total;
-    // pages that go back: first how many there are (some columns may hold none), then where
-    unsigned long long some = __ballot(s < a.seqs && held > need);
-    int mine = 0;
-    for (unsigned long long m = some; m; m &= m - 1) {
-      const int l = __builtin_ctzll(m), sl = __builtin_amdgcn_readlane(s, l);
-      const int lo = __builtin_amdgcn_readlane(need, l), hi = __builtin_amdgcn_readlane(held, l);
+    for (int e = wave; e < g_count; e += kAssignThreads / 64) {
       int n = 0;
-      for (int c = lo; c < hi; c += 64) {
-        const int page = c + lane < hi ? from[sl * a.ldt + c + lane] : -1;
-        n += __popcll(__ballot(page >= 0 && page < a.pages));
-      }
-      if (lane == l) mine = n;
+      each_page(from + g_seq[e] * a.ldt, g_lo[e], g_hi[e], a.pages, [&](bool there, int) { n += __popcll(__ballot(there)); });
+      if (lane == 0) g_n[e] = n;
     }
-    const uint32_t b = back + block_scan((uint32_t)mine, 0x7FFFFFFFu, mem, total) - (uint32_t)mine;
+    __syncthreads();
+    uint32_t n_back[kItems];
+    mine = 0;
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) {
+      n_back[i] = place[i] >= 0 ? (uint32_t)g_n[place[i]] : 0;
+      mine += n_back[i];
+    }
+    uint32_t b = back + block_scan(mine, 0x7FFFFFFFu, mem[2], total);
     back += total;
-    for (unsigned long long m = some; m; m &= m - 1) {
-      const int l = __builtin_ctzll(m), sl = __builtin_amdgcn_readlane(s, l);
-      const int lo = __builtin_amdgcn_readlane(need, l), hi = __builtin_amdgcn_readlane(held, l);
-      int64_t at = (int64_t)on_stack + __builtin_amdgcn_readlane((int)b, l);
-      for (int c = lo; c < hi; c += 64) {
-        const int page = c + lane < hi ? from[sl * a.ldt + c + lane] : -1;
-        const bool there = page >= 0 && page < a.pages;
-        const unsigned long long is = __ballot(there);
-        const int64_t to = at + __popcll(is & ((1ull << lane) - 1));
-        if (there && to < a.pages) a.free[to] = page;
-        at += __popcll(is);
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) {
+      const int s = s0 + tid * kItems + i;
+      if (place[i] >= 0) g_n[place[i]] = (int)b;   // now where they go
+      b += n_back[i];
+      if (s < a.seqs) {
+        a.offs[s] = first[i];
+        a.lens[s] = len[i];
+        a.held_out[s] = need[i];
+        const int end = first[i] + (len[i] - keep[i]);
+        if (WHOLE) l_end[s] = end, l_given[s] = (int)g, l_held[s] = held[i], l_len[s] = len[i];
+        else a.ws[s] = (int)g, a.ws[a.seqs + s] = held[i];
       }
+      g += (uint32_t)fresh[i];
     }
-    if (s < a.seqs) {
-      a.offs[s] = first;
-      a.lens[s] = len;
-      a.held_out[s] = need;
-      if (WHOLE) l_end[s] = end, l_given[s] = (int)g, l_held[s] = held, l_len[s] = len;
-      else a.ws[s] = (int)g, a.ws[a.seqs + s] = held;
+    __syncthreads();
+    for (int e = wave; e < g_count; e += kAssignThreads / 64) {
+      int64_t to = (int64_t)on_stack + g_n[e];
+      each_page(from + g_seq[e] * a.ldt, g_lo[e], g_hi[e], a.pages, [&](bool there, int page) {
+        const unsigned long long is = __ballot(there);
+        const int64_t mine_to = to + __popcll(is & ((1ull << lane) - 1));
+        if (there && mine_to < a.pages) a.free[mine_to] = page;
+        to += __popcll(is);
+      });
     }
+    __syncthreads();   // the list is read
   }
   const int64_t all = (int64_t)on_stack + back;
   const int there = all < a.pages ? (int)all : a.pages;
