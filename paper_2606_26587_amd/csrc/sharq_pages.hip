@@ -336,6 +336,8 @@ __global__ __launch_bounds__(256) void k_beam_reorder(ReorderArgs a, int table_u
   to[2] = copy ? part : -1;
 }
 
+typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+
 // The first tokens of pages into other pages, keys and values of a head: a copy, a
 // head and (large pages) a part of it to a workgroup.
 template <int F>
@@ -349,18 +351,18 @@ __global__ __launch_bounds__(256) void k_kv_copy(KvCacheArgs c, const int32_t* c
   const int64_t to = kv_row(dst, 0, c.pages, c.heads, head, c.page_shift);
   const int bytes = copy_row_bytes(D, F), chunks = n * (bytes / 16);   // of K, and of V
   const int begin = part * kCopyChunks, end = 2 * chunks < begin + kCopyChunks ? 2 * chunks : begin + kCopyChunks;
-  uint4 x[kCopyChunks / 256];
+  if (begin >= end) return;
+  v4u x[kCopyChunks / 256];
 #pragma unroll
-  for (int i = 0; i < kCopyChunks / 256; ++i) {
-    const int at = begin + i * 256 + tid;
-    if (at < end)
-      x[i] = *reinterpret_cast<const uint4*>((at < chunks ? c.k : c.v) + from * bytes + 16 * (int64_t)(at < chunks ? at : at - chunks));
+  for (int i = 0; i < kCopyChunks / 256; ++i) {   // without conditions: a place past the end reads the last one again
+    const int at = begin + i * 256 + tid < end ? begin + i * 256 + tid : end - 1;
+    x[i] = *reinterpret_cast<const v4u*>((at < chunks ? c.k : c.v) + from * bytes + 16 * (int64_t)(at < chunks ? at : at - chunks));
   }
 #pragma unroll
   for (int i = 0; i < kCopyChunks / 256; ++i) {
     const int at = begin + i * 256 + tid;
     if (at < end)
-      *reinterpret_cast<uint4*>((at < chunks ? c.k : c.v) + to * bytes + 16 * (int64_t)(at < chunks ? at : at - chunks)) = x[i];
+      *reinterpret_cast<v4u*>((at < chunks ? c.k : c.v) + to * bytes + 16 * (int64_t)(at < chunks ? at : at - chunks)) = x[i];
   }
   if (F == kKvBf16 || part != 0) return;
   // scales: bytes of K and of V
