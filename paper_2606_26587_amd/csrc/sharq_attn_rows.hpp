@@ -260,12 +260,14 @@ __device__ __forceinline__ void attn_rows(const AttnArgs& a, int block, int tile
     }
     if (F8) {
       const Codes& x = ahead[stage];
+      // without selects where all 16 tokens are there, as most are
+      const bool whole = ((live >> (16 * wave)) & 0xFFFF) == 0xFFFF;
 #pragma unroll
       for (int i = 0; i < kW; ++i) {
         const int row = 16 * wave + i * (1024 / D) + lane / (D / 16), c0 = 2 * (lane % (D / 16));
-        const bool dead = !((live >> row) & 1);
-        const uint32_t ks = dead ? 127 : x.ks, vs = dead ? 127 : x.vs;
-        const uint4 k = dead ? make_uint4(0, 0, 0, 0) : x.k[i], v = dead ? make_uint4(0, 0, 0, 0) : x.v[i];
+        uint32_t ks = x.ks, vs = x.vs;
+        uint4 k = x.k[i], v = x.v[i];
+        if (!whole && !((live >> row) & 1)) ks = vs = 127, k = v = make_uint4(0, 0, 0, 0);
         lds[stage][0][kv_chunk<D>(row, c0)] = f8_bf16x8(make_uint2(k.x, k.y), ks);
         lds[stage][0][kv_chunk<D>(row, c0 + 1)] = f8_bf16x8(make_uint2(k.z, k.w), ks);
         lds[stage][1][kv_chunk<D>(row, c0)] = f8_bf16x8(make_uint2(v.x, v.y), vs);
@@ -291,7 +293,7 @@ __device__ __forceinline__ void attn_rows(const AttnArgs& a, int block, int tile
 
   // Tiles and pages of a tile on their way while one is worked on.  Codes: tile ti is in ahead[] and in LDS at the
   // parity of ti - first.
-  constexpr int kAhead = CODES ? 2 : 1;
+  constexpr int kAhead = MX ? 2 : 1;
   unsigned long long live[kAhead + 1] = {};   // of this tile and the next ones, token by token: whether it is there
   int next = 0;
   const bool any = first < end && a.c.pages > 0;
@@ -319,7 +321,7 @@ __device__ __forceinline__ void attn_rows(const AttnArgs& a, int block, int tile
     const int at = row_of(next, ti + kAhead);
     live[kAhead] = __ballot(at >= 0);
     next = page_of(ti + kAhead + 1);
-    load(at, CODES ? stage : stage ^ 1);
+    load(at, kAhead == 2 ? stage : stage ^ 1);
     if (ts <= w_hi && live[0] != 0) {
       const char *sk = reinterpret_cast<const char*>(lds[stage][0]), *sv = reinterpret_cast<const char*>(lds[stage][1]);
       v16f s[2] = {};
