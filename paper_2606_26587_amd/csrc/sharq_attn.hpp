@@ -53,6 +53,11 @@ __device__ __forceinline__ int mx_token(int lane) {
   return D == 128 ? (l & 1) | (l & 6) << 1 | (l & 8) >> 2 : (l & 7) << 1 | l >> 3;
 }
 
+// The token of 16 whose 16 values from 16 (lane & 3) on (and, of heads of 128, from 64 further on) a lane writes to LDS
+// from an E4M3 cache.  8 lanes in a row take two tokens that are 8 apart, which kv_chunk's exchange puts at odd and at
+// even places: the first of the two chunks of all 8, and the second, reach 8 different ones of 128 bytes.
+__device__ __forceinline__ int f8_token(int lane) { return lane >> 3 | (lane & 4) << 1; }
+
 // Transposing LDS read: a group of 16 lanes reads 4 rows of 16 values, lane i
 // giving the address of values 4 (i % 4) .. + 3 of row i / 4, and gets value i
 // of the 4 rows.

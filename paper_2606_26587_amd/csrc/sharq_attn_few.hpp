@@ -130,12 +130,12 @@ __device__ __forceinline__ void attn_few(const AttnArgs& a, int block, int chunk
         }
         ke[i] = ksp[(uint32_t)(col * (D / 32) + g * (D / 32) / 4)];
         ve[i] = vsp[(uint32_t)(v_tok * (D / 32) + g * (D / 32) / 4)];
-      } else if (F8) {   // 16 tokens lie in a row: their values come as they lie
+      } else if (F8) {
         const uint8_t *kp = a.c.k + row * D, *vp = a.c.v + row * D;
 #pragma unroll
         for (int j = 0; j < kKeys; ++j) {
           kb[i][j] = *reinterpret_cast<const uint4*>(kp + (uint32_t)(col * D + 16 * g) + 64 * j);
-          vb[i][j] = *reinterpret_cast<const uint4*>(vp + (uint32_t)(lane * 16) + 1024 * j);
+          vb[i][j] = *reinterpret_cast<const uint4*>(vp + (uint32_t)(f8_token(lane) * D + 16 * (lane & 3)) + 64 * j);
         }
         ke[i] = (uint32_t)__builtin_amdgcn_readlane((int)kse, l0);
         ve[i] = (uint32_t)__builtin_amdgcn_readlane((int)vse, l0);
@@ -183,7 +183,7 @@ __device__ __forceinline__ void attn_few(const AttnArgs& a, int block, int chunk
         } else if (F8) {
 #pragma unroll
           for (int j = 0; j < kVals; ++j) {
-            const int t = j * (1024 / D) + lane / (D / 16), c0 = 2 * (lane % (D / 16));
+            const int t = f8_token(lane), c0 = 8 * j + 2 * (lane & 3);
             const bool dead = !((mine >> t) & 1);
             const uint4 x = vb[i][j];
             const uint32_t e = dead ? 127 : ve[i];

@@ -201,7 +201,8 @@ __device__ __forceinline__ void attn_rows(const AttnArgs& a, int block, int tile
   // they go to LDS over all banks.  A step of few rows is shorter than the way from HBM: with one tile on its way
   // 16 x 9 tokens, 4 query heads a key/value head, over 8000 took 80 us, with two 69; a prompt of 5759, heads of 64,
   // 210 and 191.
-  // E4M3: the same with 16 values a load as they lie; the 16 tokens have one scale.
+  // E4M3: 16 values a load, and the 16 tokens have one scale; one tile on its way, as two take the registers that the
+  // products need (two prompts of 6000, 28 and 4 heads of 128: 512 us with two, 502 with one).
   constexpr int kW = F8 ? D / 64 : 1;
   struct Codes {
     uint4 k[kW], v[kW];
@@ -226,8 +227,9 @@ __device__ __forceinline__ void attn_rows(const AttnArgs& a, int block, int tile
       Codes& x = ahead[to];
 #pragma unroll
       for (int i = 0; i < kW; ++i) {
-        x.k[i] = *reinterpret_cast<const uint4*>(kp + (uint32_t)lane * 16 + 1024 * i);
-        x.v[i] = *reinterpret_cast<const uint4*>(vp + (uint32_t)lane * 16 + 1024 * i);
+        const uint32_t place = (uint32_t)(f8_token(lane) * D + 16 * (lane & 3));
+        x.k[i] = *reinterpret_cast<const uint4*>(kp + place + 64 * i);
+        x.v[i] = *reinterpret_cast<const uint4*>(vp + place + 64 * i);
       }
       x.ks = a.c.ks[row0 / kF8Block], x.vs = a.c.vs[row0 / kF8Block];
     } else if (mine) {
@@ -264,7 +266,7 @@ __device__ __forceinline__ void attn_rows(const AttnArgs& a, int block, int tile
       const bool whole = ((live >> (16 * wave)) & 0xFFFF) == 0xFFFF;
 #pragma unroll
       for (int i = 0; i < kW; ++i) {
-        const int row = 16 * wave + i * (1024 / D) + lane / (D / 16), c0 = 2 * (lane % (D / 16));
+        const int row = 16 * wave + f8_token(lane), c0 = 8 * i + 2 * (lane & 3);
         uint32_t ks = x.ks, vs = x.vs;
         uint4 k = x.k[i], v = x.v[i];
         if (!whole && !((live >> row) & 1)) ks = vs = 127, k = v = make_uint4(0, 0, 0, 0);
