@@ -223,17 +223,25 @@ __device__ __forceinline__ void append8_block(const KvAppendArgs& a, const KvCac
 // the row that begins it finds: the first of a sequence's rows, or one at a multiple of 16.
 template <int D>
 __global__ __launch_bounds__(kAppend8Threads) void k_kv_append8(KvAppendArgs a, KvBatchArgs b, KvCacheArgs c,
-                                                                unsigned queries, int group) {
+                                                                unsigned first_query, int group) {
   const int tid = (int)threadIdx.x;
-  if (blockIdx.x < queries) {   // a thread: 8 values of a head's first half and the 8 that pair with them
+  if (blockIdx.x >= first_query) {
+    // a thread: 8 values of a head's first half and the 8 that pair with them, of two heads: one lookup, one angle
     constexpr int kPer = D / 16;
-    const unsigned item = blockIdx.x * kAppend8Threads + tid, per_row = (unsigned)a.q_heads * kPer;
+    const int pair = kv_append8_pair(a.q_heads);
+    const unsigned block = blockIdx.x - first_query;
+    const unsigned item = block * kAppend8Threads + tid, per_row = (unsigned)pair * kPer;
     const int row = (int)(item / per_row), rest = (int)(item % per_row), h = rest / kPer, j = rest % kPer * 8;
-    const int first = (int)((blockIdx.x * kAppend8Threads + (tid & ~63)) / per_row);   // of the wavefront
+    const int first = (int)((block * kAppend8Threads + (tid & ~63)) / per_row);   // of the wavefront
     if (first >= b.rows) return;
-    float lo[8], hi[8];
-    const bool has = row < b.rows;
-    if (has) load_halves<D, 8>(a.q + row * a.ldq + h * D + j, lo, hi);
+    float lo[2][8], hi[2][8];
+    const bool has = row < b.rows, two = h + pair < a.q_heads;
+    const int next = two ? pair * D : 0;
+    if (has) {
+      const uint16_t* const src = a.q + row * a.ldq + h * D + j;
+      load_halves<D, 8>(src, lo[0], hi[0]);
+      load_halves<D, 8>(src + next, lo[1], hi[1]);
+    }
     int s = find_seq(b, first), past = b.seqs;   // few of a wavefront's threads are at a later row than the first
     if (!has) return;
     if (row == first) past = s;
@@ -246,19 +254,26 @@ __global__ __launch_bounds__(kAppend8Threads) void k_kv_append8(KvAppendArgs a, 
     const SeqRows r = seq_rows(b, s);
     const int i = row - r.first, p = r.len - r.n + i;
     if (i < 0 || i >= r.n || p < 0) return;
+    int angle = 0;
     if (a.cos) {
-      const int angle = a.pos ? a.pos[row] : p;
+      angle = a.pos ? a.pos[row] : p;
       if (angle < 0 || angle >= a.angles) return;
-      rotate_halves<8>(a.cos + (int64_t)angle * (D / 2) + j, a.sin + (int64_t)angle * (D / 2) + j, lo, hi);
     }
+    const float *cp = a.cos + (int64_t)angle * (D / 2) + j, *sp = a.sin + (int64_t)angle * (D / 2) + j;
     uint16_t* const dst = a.qo + row * a.ldqo + h * D + j;
-    *reinterpret_cast<uint4*>(dst) = make_uint4(bf16x2(lo[0], lo[1]), bf16x2(lo[2], lo[3]), bf16x2(lo[4], lo[5]),
-                                                bf16x2(lo[6], lo[7]));
-    *reinterpret_cast<uint4*>(dst + D / 2) = make_uint4(bf16x2(hi[0], hi[1]), bf16x2(hi[2], hi[3]),
-                                                        bf16x2(hi[4], hi[5]), bf16x2(hi[6], hi[7]));
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      if (a.cos) rotate_halves<8>(cp, sp, lo[k], hi[k]);
+      if (k == 1 && !two) continue;
+      uint16_t* const to = dst + k * next;
+      *reinterpret_cast<uint4*>(to) = make_uint4(bf16x2(lo[k][0], lo[k][1]), bf16x2(lo[k][2], lo[k][3]),
+                                                 bf16x2(lo[k][4], lo[k][5]), bf16x2(lo[k][6], lo[k][7]));
+      *reinterpret_cast<uint4*>(to + D / 2) = make_uint4(bf16x2(hi[k][0], hi[k][1]), bf16x2(hi[k][2], hi[k][3]),
+                                                         bf16x2(hi[k][4], hi[k][5]), bf16x2(hi[k][6], hi[k][7]));
+    }
     return;
   }
-  const unsigned block = blockIdx.x - queries, parts = (unsigned)kv_append8_parts(c.heads);
+  const unsigned block = blockIdx.x, parts = (unsigned)kv_append8_parts(c.heads);
   const int item = (int)(block % parts) * 4 + (tid >> 6), unit = (int)(block / parts);
   if (item >= 2 * c.heads) return;
   const bool is_v = item & 1;
@@ -326,8 +341,9 @@ hipError_t launch_kv_append(const uint16_t* q, const uint16_t* k, const uint16_t
   KvAppendArgs a{q, k, v, ldq, ldk, ldv, qo, ldqo, cos, sin, pos, angles, q_heads, 0, rule_bias};
   if (fmt == kKvF8) {
     const int group = kv_append8_group(max_rows);
-    const unsigned first = (unsigned)kv_append8_queries(b.rows, q_heads, D);
-    const dim3 g8((unsigned)kv_append8_blocks(b.rows, max_rows, q_heads, c.heads, D)), t8(kAppend8Threads);
+    const unsigned all = (unsigned)kv_append8_blocks(b.rows, max_rows, q_heads, c.heads, D);
+    const unsigned first = all - (unsigned)kv_append8_queries(b.rows, q_heads, D);
+    const dim3 g8(all), t8(kAppend8Threads);
     if (D == 128) k_kv_append8<128><<<g8, t8, 0, st>>>(a, b, c, first, group);
     else k_kv_append8<64><<<g8, t8, 0, st>>>(a, b, c, first, group);
     return hipGetLastError();

@@ -80,14 +80,16 @@ constexpr int kv_append_parts(int q_heads, int heads, int D) {
 constexpr int kv_read_parts(int heads, int D) { return (2 * heads * (D / 8) + kReadThreads - 1) / kReadThreads; }
 
 // E4M3: the append's workgroups of four wavefronts.  The first of them take the
-// queries, 16 values a thread; the others the blocks of 16 tokens that `group`
-// consecutive rows begin, a wavefront for the keys or the values of a head.  One
+// blocks of 16 tokens that `group` consecutive rows begin, a wavefront for the keys
+// or the values of a head; the others, whose chain of loads is shorter, the
+// queries, 16 values of two heads a thread.  One
 // row a unit where sequences bring few, so that as many wavefronts run as there
 // are blocks; 16 where they bring many, of which about one begins a block.
 constexpr int kAppend8Threads = 256;
 constexpr int kv_append8_group(int64_t max_rows) { return max_rows < 2 * kF8Block ? 1 : kF8Block; }
+constexpr int kv_append8_pair(int q_heads) { return (q_heads + 1) / 2; }   // a thread takes heads h and h + this
 constexpr int64_t kv_append8_queries(int64_t rows, int q_heads, int D) {
-  return (rows * q_heads * (D / 16) + kAppend8Threads - 1) / kAppend8Threads;
+  return (rows * kv_append8_pair(q_heads) * (D / 16) + kAppend8Threads - 1) / kAppend8Threads;
 }
 constexpr int kv_append8_parts(int heads) { return (2 * heads + 3) / 4; }
 constexpr int64_t kv_append8_blocks(int64_t rows, int64_t max_rows, int q_heads, int heads, int D) {

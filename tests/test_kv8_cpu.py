@@ -150,7 +150,7 @@ def test_append_work_split(tmp_path):
         offs = np.concatenate([[0], np.cumsum(n)])
         rows, g = int(offs[-1]) + int(rng.integers(0, 4)), lib.group(most)
         heads, q = int(rng.integers(1, 9)), int(rng.integers(0, 9))
-        assert lib.parts(heads) * 4 >= 2 * heads and lib.queries(rows, q, 64) * 256 >= rows * q * 4
+        assert lib.parts(heads) * 4 >= 2 * heads and lib.queries(rows, q, 64) * 256 >= rows * -(-q // 2) * 4
         units = (lib.blocks(rows, most, q, heads, 64) - lib.queries(rows, q, 64)) // lib.parts(heads)
         found = []
         for u in range(units):                       # the walk of the kernel
