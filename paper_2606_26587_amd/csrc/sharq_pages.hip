@@ -83,18 +83,20 @@ __device__ __forceinline__ void assign_row(const AssignArgs& a, int there, int r
   }
 }
 
-// The pages in columns lo..hi-1 of a row of a table, 64 at a time and eight of these on their way together: f(whether
-// there is one, it).
+// The pages in columns lo..hi-1 of a row of a table, 64 at a time and four of these on their way together (without
+// conditions: what is past the end is the last one again): f(whether there is one, it).
 template <typename Fn>
 __device__ __forceinline__ void each_page(const int32_t* row, int lo, int hi, int pages, Fn f) {
   const int lane = (int)threadIdx.x & 63;
-  for (int c0 = lo; c0 < hi; c0 += 512) {
-    int page[8];
+  for (int c0 = lo; c0 < hi; c0 += 256) {
+    int page[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) page[i] = c0 + 64 * i + lane < hi ? row[c0 + 64 * i + lane] : -1;
+    for (int i = 0; i < 4; ++i) {
+      const int c = c0 + 64 * i + lane;
+      page[i] = row[c < hi ? c : hi - 1];
+    }
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (c0 + 64 * i < hi) f(page[i] >= 0 && page[i] < pages, page[i]);
+    for (int i = 0; i < 4; ++i) f(c0 + 64 * i + lane < hi && page[i] >= 0 && page[i] < pages, page[i]);
   }
 }
 
@@ -105,7 +107,7 @@ __device__ __forceinline__ void each_page(const int32_t* row, int lo, int hi, in
 // none), which all wavefronts share.
 template <bool WHOLE>
 __global__ __launch_bounds__(kAssignThreads) void k_kv_assign(AssignArgs a) {
-  constexpr int kItems = 2, kPass = kItems * kAssignThreads;
+  constexpr int kItems = WHOLE ? 2 : 4, kPass = kItems * kAssignThreads;
   __shared__ uint32_t mem[3][kAssignThreads / 64];
   __shared__ int l_end[WHOLE ? kAssignSeqs : 1], l_given[WHOLE ? kAssignSeqs : 1], l_held[WHOLE ? kAssignSeqs : 1],
       l_len[WHOLE ? kAssignSeqs : 1];
@@ -154,7 +156,8 @@ __global__ __launch_bounds__(kAssignThreads) void k_kv_assign(AssignArgs a) {
     given += total;
     for (int e = wave; e < g_count; e += kAssignThreads / 64) {
       int n = 0;
-      each_page(from + g_seq[e] * a.ldt, g_lo[e], g_hi[e], a.pages, [&](bool there, int) { n += __popcll(__ballot(there)); });
+      each_page(from + g_seq[e] * a.ldt, __builtin_amdgcn_readfirstlane(g_lo[e]),
+                __builtin_amdgcn_readfirstlane(g_hi[e]), a.pages, [&](bool there, int) { n += __popcll(__ballot(there)); });
       if (lane == 0) g_n[e] = n;
     }
     __syncthreads();
@@ -185,7 +188,8 @@ __global__ __launch_bounds__(kAssignThreads) void k_kv_assign(AssignArgs a) {
     __syncthreads();
     for (int e = wave; e < g_count; e += kAssignThreads / 64) {
       int64_t to = (int64_t)on_stack + g_n[e];
-      each_page(from + g_seq[e] * a.ldt, g_lo[e], g_hi[e], a.pages, [&](bool there, int page) {
+      each_page(from + g_seq[e] * a.ldt, __builtin_amdgcn_readfirstlane(g_lo[e]),
+                __builtin_amdgcn_readfirstlane(g_hi[e]), a.pages, [&](bool there, int page) {
         const unsigned long long is = __ballot(there);
         const int64_t mine_to = to + __popcll(is & ((1ull << lane) - 1));
         if (there && mine_to < a.pages) a.free[mine_to] = page;
