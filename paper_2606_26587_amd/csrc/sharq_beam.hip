@@ -326,14 +326,16 @@ __device__ __forceinline__ bool better(const BeamKey& x, const BeamKey& y) {
   return x.order > y.order || (x.order == y.order && x.at < y.at);
 }
 
+constexpr int kPickThreads = 512;   // at least kBeamLists
+
 // Joins a group's lists.  A thread has one list, whose entries come best first.  As `beams` lists reach the `beams`-th of
 // a wavefront's first entries, nothing below can be chosen; what is not below it is ranked.
-__global__ __launch_bounds__(256) void k_beam_pick(BeamArgs a) {
+__global__ __launch_bounds__(kPickThreads) void k_beam_pick(BeamArgs a) {
   extern __shared__ uint64_t lds[];
   __shared__ double base_of[kMaxBeams], lse_of[kMaxBeams];
   __shared__ uint8_t done_of[kMaxBeams];
   __shared__ BeamPart part_of[kBeamLists];
-  __shared__ uint32_t bound_of[4];
+  __shared__ uint32_t bound_of[kPickThreads / 64];
   __shared__ int count;
   const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), beams = a.beams;
   const int lists = beams * a.chunks, entries = lists * beams;
@@ -354,7 +356,7 @@ __global__ __launch_bounds__(256) void k_beam_pick(BeamArgs a) {
     if (a.done) done = a.done[row0 + tid];
     score = a.scores[row0 + tid];
   }
-  for (int i = tid; i < entries; i += 256) entry[i] = from[i];
+  for (int i = tid; i < entries; i += kPickThreads) entry[i] = from[i];
   if (tid == 0) count = 0;
   if (tid < beams) done_of[tid] = done != 0, base_of[tid] = (double)score;
   // a thread's four parts of a sum, then a wavefront a beam
@@ -369,7 +371,7 @@ __global__ __launch_bounds__(256) void k_beam_pick(BeamArgs a) {
     if (tid < lists) part_of[tid] = BeamPart{sum, top, 0};
   }
   __syncthreads();
-  for (int i = wave; i < beams; i += 4) {
+  for (int i = wave; i < beams; i += kPickThreads / 64) {
     BeamPart p{0.0, -__builtin_inff(), 0};
     for (int c = lane; c < a.chunks; c += 64) {   // more than 64 where the beams are few
       const BeamPart o = part_of[i * a.chunks + c];
@@ -418,7 +420,7 @@ __global__ __launch_bounds__(256) void k_beam_pick(BeamArgs a) {
   if (lane == 0) bound_of[wave] = bound;
   __syncthreads();
 #pragma unroll
-  for (int w = 0; w < 4; ++w) bound = bound_of[w] > bound ? bound_of[w] : bound;
+  for (int w = 0; w < kPickThreads / 64; ++w) bound = bound_of[w] > bound ? bound_of[w] : bound;
   if (mine) {
     BeamKey k = head;
     for (int i = 0; k.order != 0 && (uint32_t)(k.order >> 32) >= bound;) {
@@ -429,7 +431,7 @@ __global__ __launch_bounds__(256) void k_beam_pick(BeamArgs a) {
   }
   __syncthreads();
   const int n = count;
-  for (int i = tid; i < n; i += 256) {
+  for (int i = tid; i < n; i += kPickThreads) {
     const BeamKey k = found[i];
     int r = 0;
 #pragma unroll 4
@@ -441,7 +443,7 @@ __global__ __launch_bounds__(256) void k_beam_pick(BeamArgs a) {
     a.tokens[row0 + r] = token;
     if (a.done_out) a.done_out[row0 + r] = done_of[parent] || token == a.eos;
   }
-  for (int r = n + tid; r < beams; r += 256) {   // no candidate left
+  for (int r = n + tid; r < beams; r += kPickThreads) {   // no candidate left
     a.scores_out[row0 + r] = -__builtin_inff();
     a.parents[row0 + r] = r;
     a.tokens[row0 + r] = -1;
@@ -457,7 +459,7 @@ hipError_t launch_beam_select(const BeamArgs& a, int64_t groups, int dtype, hipS
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const size_t lds = (size_t)beam_lds(a.beams, a.chunks);
-  k_beam_pick<<<(unsigned)groups, 256, lds, st>>>(a);
+  k_beam_pick<<<(unsigned)groups, kPickThreads, lds, st>>>(a);
   return hipGetLastError();
 }
 
