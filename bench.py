@@ -39,7 +39,7 @@ Other workloads (--workload), one JSON line each:
                 fusions, the o projection, and between qkv and o the rotation
                 and append to the paged key/value cache and the attention that
                 reads it; a prompt of 2048 tokens, and 64 single tokens over
-                4096 cached ones each, with the cache in bf16 and in MXFP4 (one
+                4096 cached ones each, with the cache in bf16, E4M3 and MXFP4 (one
                 line each, in tokens per second of one layer)
   ablation      the path combinations (Sparse, plain FP4 RTN, Dense+Dense,
                 Sparse+Sparse, SharQ) on the Llama prefill linears, MXFP4 2:4
@@ -803,7 +803,7 @@ def attention_work(seqs, new, length, kv_fmt):
     and visible pair; queries and outputs, and every cached key and value once."""
     hq, hkv, D = LAYER_HEADS
     pairs = seqs * (new * (length - new) + new * (new + 1) // 2)
-    held = 2.0 if kv_fmt == "bf16" else 0.5 + 1.0 / 32
+    held = {"bf16": 2.0, "fp8": 1.0 + 1.0 / (16 * D), "mx": 0.5 + 1.0 / 32}[kv_fmt]
     return 4.0 * D * hq * pairs, seqs * (new * hq * D * 4.0 + 2.0 * length * hkv * D * held)
 
 
@@ -832,7 +832,7 @@ def llama_layer(args, torch, S, synth, dev, stream):
         batch = S.KVBatch(torch.arange(seqs + 1, dtype=torch.int32, device=dev) * new,
                           torch.full((seqs,), length, dtype=torch.int32, device=dev),
                           table.view(seqs, per).to(dev), T, new, length)
-        for fmt in ("bf16", "mx"):
+        for fmt in ("bf16", "fp8", "mx"):
             # cached tokens: rows of a normal distribution, appended by the library itself
             cache = S.alloc_kv_cache(seqs * per, LAYER_PAGE, hkv, D, fmt, dev)
             whole = S.KVBatch(torch.arange(seqs + 1, dtype=torch.int32, device=dev) * length, batch.lens,

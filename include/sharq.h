@@ -627,6 +627,7 @@ SHARQ_API size_t sharq_kv_assign_workspace_bytes(const sharq_kv_requests *r);
  * the stack, in the same order; where it is empty they get -1, an absent page, and
  * `missing` counts them.  held_out_s = need_s.  row_offsets, lens and page_table are
  * those of a sharq_kv_batch.  Rows behind the last sequence are left as they were.
+ * Calls on the same pool, and calls that share a workspace, run one after the other.
  * Values of the device arrays outside their range (negative, above max_len or the
  * table's columns) count as the nearest inside.  The result does not depend on the
  * order in which the device runs.  workspace: 4-byte aligned.
@@ -643,7 +644,8 @@ SHARQ_API size_t sharq_beam_workspace_bytes(int64_t groups, int64_t beams, int64
  * BF16, F16 or F32, row stride ld elements, element-aligned).  Candidate (b, v) has
  *   score_b + x_bv - lse_b,  lse_b = ln sum_v e^(x_bv);
  * a beam that is done has one, (b, eos), with score_b.  Of each group the `beams` best,
- * best first, equal ones by the lower b * vocab + v:
+ * best first, equal ones by the lower b, and those of one beam by their logits, equal
+ * ones by the lower v:
  *   scores_out  fp32 [groups][beams] (it may be `scores`)
  *   parents     int32 [groups][beams]: b
  *   tokens      int32 [groups][beams]: v
@@ -651,11 +653,12 @@ SHARQ_API size_t sharq_beam_workspace_bytes(int64_t groups, int64_t beams, int64
  *   done_out    uint8 [groups * beams] (it may be `done`), NULL exactly if done is:
  *               done[b], or v == eos.
  *   eos         -1 where there is none (then done is NULL).
- * A logit of -inf is no candidate, nor is any of a beam whose score is -inf or whose
- * score or logits hold a NaN or whose logits hold +inf.  Where a group has fewer than `beams`
+ * A logit of -inf is no candidate, nor is any of a beam whose score is not finite or
+ * whose logits hold a NaN or +inf.  Where a group has fewer than `beams`
  * candidates, the places behind have score -inf, token -1 and themselves as parent.
  * Scores are compared in 64 bits, whatever their rounding to scores_out.
- * groups * beams is at most 2^20, beams * vocab at most 2^30.  workspace: 8-byte aligned.
+ * groups * beams is at most 2^20, beams * vocab at most 2^30.  workspace: 8-byte aligned;
+ * calls that may run at the same time need workspaces of their own.
  */
 SHARQ_API sharq_status sharq_beam_select(const void *logits, sharq_dtype dtype, int64_t ld, int64_t groups,
                                          int64_t beams, int64_t vocab, const float *scores, const uint8_t *done,
@@ -681,7 +684,8 @@ SHARQ_API sharq_status sharq_beam_select(const void *logits, sharq_dtype dtype, 
  *                       [groups * beams][id_cols], row strides ldi, ldio (ids_out may
  *                       be `ids`): ids_out[i][t] = ids[parents[i]][t] for t < len,
  *                       ids_out[i][len] = tokens[i]; columns behind are left as they were.
- * Parents outside [0, beams) count as the nearest inside.  groups * beams is at most 2^20.
+ * Parents outside [0, beams) count as the nearest inside.  Outputs overlap inputs only where
+ * they are the same array.  groups * beams is at most 2^20.
  */
 SHARQ_API sharq_status sharq_beam_reorder(int64_t groups, int64_t beams, const int32_t *parents, const int32_t *lens,
                                           int32_t page_size, const int32_t *table, int64_t ldt, int32_t *table_out,

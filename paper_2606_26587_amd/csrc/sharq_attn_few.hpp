@@ -17,15 +17,17 @@
 // registers (no byte is used by two lanes); values through a wavefront's
 // own LDS for the transposing read.  An MXFP4 key's operand takes the k slots in
 // the order that gives each lane D/4 consecutive values of its token: one load,
-// one block scale.
+// one block scale.  An E4M3 key's takes 16 bytes of every 64; the 16 tokens of a
+// group have one scale, which a lane reads beside the page of its token.
 //
 // A turn's loads are made without conditions on page bases in scalar registers,
 // and the page table is read a turn ahead: with a wait for the table among the
 // loads, 24 x 32768 tokens in MXFP4 took 180 us, now 128.  Measured with 8
 // key/value heads of 128: 64 x up to 6000 tokens, window 4096, bf16: 178 us, 5.4
 // TB/s (a 1 GiB copy: 5.16); 24 x up to 32768, MXFP4: 128 us, 4.6 TB/s, the
-// dequantization and the products beside the stream; one token over 8191: 9.6 us
-// and 3.6 for the join, latencies of launch, table, keys and join.
+// dequantization and the products beside the stream; 32 x up to 16384, E4M3: 144
+// us, 5.2 TB/s; one token over 8191: 9.6 us and 3.6 for the join (E4M3: 8 and 3),
+// latencies of launch, table, keys and join.
 
 #pragma once
 

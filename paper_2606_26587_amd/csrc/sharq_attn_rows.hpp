@@ -25,8 +25,8 @@
 // two wavefronts a SIMD, of two workgroups that run apart, so one's exponentials
 // can run beside the other's products), and walks tiles of 64 tokens in two LDS
 // stages: while one is worked on, the next is on its way, bf16 straight from
-// global memory to LDS; of MXFP4 the next two, through registers, from where it
-// becomes bf16 once for all rows.  Rows of consecutive tokens share the tiles:
+// global memory to LDS; E4M3, and of MXFP4 the next two, through registers, from
+// where it becomes bf16 once for all rows.  Rows of consecutive tokens share the tiles:
 // with 4 query heads a key/value head a tile is 32 tokens, so little of a causal
 // or windowed tile is masked, and masks are formed only in tiles that need one.
 //
@@ -38,7 +38,8 @@
 // second half's products (544, and with the maximum left out 546 against 540),
 // halves of masked tiles skipped (571) and raised priority around the products
 // (550) were measured and not kept.  Heads of 64: 830 TFLOP/s, the exponentials
-// weigh twice as much.  An MXFP4 cache costs 2.5% here (538 and 552).
+// weigh twice as much.  An MXFP4 cache costs 2.5% here (538 and 552), one in E4M3 6.5%
+// (494 and 527): twice the registers and loads of MXFP4 on the way, the same conversions.
 
 #pragma once
 

@@ -7,6 +7,15 @@
 // reference, which moves only when a logit passes it by 8.  What is left, a few
 // candidates a part of a row, is joined by one workgroup a group (k_beam_pick).
 //
+// Measured, bf16: 32 groups of 8 beams over 152064 tokens (78 MB, some beams done)
+// 22.6 us and 6.9 for the join, 3.4 TB/s; one group of 4 over 128256 6.7 and 5.5.
+// What bounds the first is the VALU (32 exponentials at a quarter of its rate and
+// 180 other operations for 32 logits of a lane, 16 of the 22 us) beside what every
+// launch takes to begin and end; the second and the join are chains of latencies.
+// Listing single logits during the walk, not a lane's 32 by their largest, took
+// 27.6 us; loading a row's last logits one by one, and loads that wait before the
+// turn they are for, 36; joining lists with 64-bit exponentials 9 for 5.5.
+//
 // Candidates of different beams lie close: sums of more than a turn, the
 // logarithm and the candidates' keys are held in 64 bits.  All orders are total
 // (value, then the lower index), and elements are dealt to threads by their
@@ -101,7 +110,9 @@ __device__ __forceinline__ double wave_sum(double x) {
 }
 
 // x times 2^e, e a whole number of any size (not above 0).
-__device__ __forceinline__ double times_exp2(double x, double e) { return __builtin_amdgcn_ldexp(x, e > -4000.0 ? (int)e : -4000); }
+__device__ __forceinline__ double times_exp2(double x, double e) {
+  return __builtin_amdgcn_ldexp(x, e > -4000.0 ? (int)e : -4000);
+}
 
 // The whole exponent of a reference, and what is left of it (a reference past 2^53 has nothing left).
 __device__ __forceinline__ double exponent_of(float ref, float& rest) {
@@ -319,14 +330,19 @@ __global__ __launch_bounds__(256) void k_beam_scan(BeamArgs a) {
 }
 
 struct __attribute__((aligned(16))) BeamKey {
-  uint64_t order;   // of the score, 0: none
-  uint32_t at, pad;   // beam * vocab + token
+  uint64_t order;     // of the score, 0: none
+  uint32_t at, own;   // beam * vocab + token; the logit's order
 };
-__device__ __forceinline__ bool better(const BeamKey& x, const BeamKey& y) {
-  return x.order > y.order || (x.order == y.order && x.at < y.at);
+// Equal scores: the lower beam.  Within a beam the logits decide: under a score of large magnitude different ones may
+// give the same sum.
+__device__ __forceinline__ bool better(const BeamKey& x, const BeamKey& y, uint32_t vocab) {
+  if (x.order != y.order) return x.order > y.order;
+  if (x.own == y.own || x.at / vocab != y.at / vocab) return x.at < y.at;
+  return x.own > y.own;
 }
 
-constexpr int kPickThreads = 512;   // at least kBeamLists
+// At least kBeamLists; a wavefront a beam forms the sums (32 groups of 8: 7.5 us with 256 threads, 6.9 with 512).
+constexpr int kPickThreads = 512;
 
 // Joins a group's lists.  A thread has one list, whose entries come best first.  As `beams` lists reach the `beams`-th of
 // a wavefront's first entries, nothing below can be chosen; what is not below it is ranked.
@@ -398,9 +414,9 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(BeamArgs a) {
     } else {
       if (e == 0) return k;
       total = base_of[b] + ((double)value32((uint32_t)(e >> 32)) - lse_of[b]);
-      k.at = (uint32_t)(b * a.vocab) + (uint32_t)~(uint32_t)e;
+      k.at = (uint32_t)(b * a.vocab) + (uint32_t)~(uint32_t)e, k.own = (uint32_t)(e >> 32);
     }
-    if (total > -__builtin_inf()) k.order = order64(total);
+    if (total > -__builtin_inf() && total < __builtin_inf()) k.order = order64(total);
     return k;
   };
   const bool mine = tid < lists && (!done_of[b] || tid % a.chunks == 0);
@@ -435,7 +451,7 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(BeamArgs a) {
     const BeamKey k = found[i];
     int r = 0;
 #pragma unroll 4
-    for (int j = 0; j < n; ++j) r += better(found[j], k);
+    for (int j = 0; j < n; ++j) r += better(found[j], k, (uint32_t)a.vocab);
     if (r >= beams) continue;
     const int parent = (int)(k.at / (uint32_t)a.vocab), token = (int)(k.at % (uint32_t)a.vocab);
     a.scores_out[row0 + r] = (float)value64(k.order);

@@ -875,7 +875,8 @@ def sharq_beam_reorder(parents: torch.Tensor, lens: torch.Tensor, page_table: Op
     ldt = ldto = cols = ldi = ldio = id_cols = 0
     if page_table is not None:
         table_out = page_table if table_out is None else table_out
-        ldt, ldto, cols = _int_rows(page_table, rows, device, where), _int_rows(table_out, rows, device, where), page_table.shape[1]
+        ldt, ldto = (_int_rows(t, rows, device, where) for t in (page_table, table_out))
+        cols = page_table.shape[1]
         if copies is None:
             with _on(stream):
                 copies = torch.empty((rows, 3), dtype=torch.int32, device=device)

@@ -54,9 +54,10 @@ def candidates(x, scores, done, eos):
     """x [beams, vocab], scores [beams] -> [(score, beam, token)], the best first, ties by the lower beam, then token."""
     out = []
     for b in range(len(scores)):
+        if not np.isfinite(scores[b]):
+            continue
         if done is not None and done[b]:
-            if scores[b] > -np.inf:
-                out.append((float(scores[b]), b, eos))
+            out.append((float(scores[b]), b, eos))
             continue
         with np.errstate(all="ignore"):
             t = np.float64(scores[b]) + log_probabilities(x[b])

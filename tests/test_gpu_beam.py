@@ -157,6 +157,13 @@ def test_the_first_step_and_beams_without_a_score():
     check(x, scores)
     scores[1, 0], scores[2, 0], scores[2, 3] = -np.inf, np.nan, -4
     check(x, scores)
+    scores[0, 2], scores[1, 1], scores[2, 1] = np.inf, -1, np.inf
+    check(x, scores)
+    check(x, scores, np.array([[0, 0, 1, 0, 0], [1, 1, 0, 0, 0], [1, 1, 0, 1, 0]], np.uint8), eos=3)
+    # sums that lose the logits: within a beam these decide
+    for huge in (-1e9, -1e30, 3e38):
+        check(x.float(), np.full((3, 5), huge))
+        check(x.float() * 1e-3, np.array([[huge, -np.inf, -np.inf, -np.inf, -np.inf]] * 3))
 
 
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("nan")])
