@@ -333,10 +333,9 @@ struct __attribute__((aligned(16))) BeamKey {
   uint64_t order;     // of the score, 0: none
   uint32_t at, own;   // beam * vocab + token; the logit's order
 };
-// Equal scores: the lower beam.  Within a beam the logits decide: under a score of large magnitude different ones may
-// give the same sum.
-__device__ __forceinline__ bool better(const BeamKey& x, const BeamKey& y, uint32_t vocab) {
-  if (x.order != y.order) return x.order > y.order;
+// Of equal scores the lower beam's is the better.  Within a beam the logits decide: under a score of large magnitude
+// different ones may give the same sum.
+__device__ __forceinline__ bool better_equal(const BeamKey& x, const BeamKey& y, uint32_t vocab) {
   if (x.own == y.own || x.at / vocab != y.at / vocab) return x.at < y.at;
   return x.own > y.own;
 }
@@ -449,9 +448,12 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(BeamArgs a) {
   const int n = count;
   for (int i = tid; i < n; i += kPickThreads) {
     const BeamKey k = found[i];
-    int r = 0;
+    int r = 0, same = 0;
 #pragma unroll 4
-    for (int j = 0; j < n; ++j) r += better(found[j], k, (uint32_t)a.vocab);
+    for (int j = 0; j < n; ++j) r += found[j].order > k.order, same += found[j].order == k.order;
+    if (same > 1)
+      for (int j = 0; j < n; ++j)
+        if (found[j].order == k.order) r += better_equal(found[j], k, (uint32_t)a.vocab);
     if (r >= beams) continue;
     const int parent = (int)(k.at / (uint32_t)a.vocab), token = (int)(k.at % (uint32_t)a.vocab);
     a.scores_out[row0 + r] = (float)value64(k.order);
