@@ -8,7 +8,7 @@
 // candidates a part of a row, is joined by one workgroup a group (k_beam_pick).
 //
 // Measured, bf16: 32 groups of 8 beams over 152064 tokens (78 MB, some beams done)
-// 22.6 us and 6.9 for the join, 3.4 TB/s; one group of 4 over 128256 6.7 and 5.5.
+// 23 us and 7.8 for the join, 3.4 TB/s; one group of 4 over 128256 6.8 and 5.5.
 // What bounds the first is the VALU (32 exponentials at a quarter of its rate and
 // 180 other operations for 32 logits of a lane, 16 of the 22 us) beside what every
 // launch takes to begin and end; the second and the join are chains of latencies.
@@ -340,7 +340,7 @@ __device__ __forceinline__ bool better_equal(const BeamKey& x, const BeamKey& y,
   return x.own > y.own;
 }
 
-// At least kBeamLists; a wavefront a beam forms the sums (32 groups of 8: 7.5 us with 256 threads, 6.9 with 512).
+// At least kBeamLists; a wavefront a beam forms the sums (32 groups of 8: half a microsecond less than with 256 threads).
 constexpr int kPickThreads = 512;
 
 // Joins a group's lists.  A thread has one list, whose entries come best first.  As `beams` lists reach the `beams`-th of
