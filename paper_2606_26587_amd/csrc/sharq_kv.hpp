@@ -170,8 +170,8 @@ constexpr AttnPlan attn_plan(int64_t seqs, int64_t rows, int64_t max_rows, int64
     // 45.6 and 39.9; 33 x 8 tokens over 5000 in MXFP4 68.1 and 55.1.  (With 480 of 512 places taken the same loses 10%.)
     const bool idle = units > 256 && units <= 341 && turns >= (lean ? 3000 : 4000);
     int64_t want = p.shared ? 512 : lean && turns >= 6144 ? 2048 : idle ? 1024 : mx && p.few == 1 ? 768 : 512;
-    // E4M3: one round of what the chip holds, 2 workgroups a CU or (heads of 64) 3, where whole parts of the sequences
-    // fill it or the work is short.  With 512, 768 and 2048 workgroups, single tokens, 8 heads of 128: 8 x 8191 22.0, 25.3
+    // E4M3: one round of 2 workgroups a CU or (heads of 64) 3, where whole parts of the sequences fill it or the work is
+    // short.  With 512, 768 and 2048 workgroups, single tokens, 8 heads of 128: 8 x 8191 22.0, 25.3
     // and 25.1 us, 16 x 8191 34.5, 39.1 and 37.8, 32 x 16384 143.8, 153.8 and 148.0, 64 x 4000 60.4, 60.4 and 59.6, but
     // 33 x 8000 100, 86 and 74; 96 x 700, 4 heads, 14.4, 16.8 and 18.3; 4 heads of 64: 24 x 32000 59.4, 49.4 and 51.4,
     // 64 x 16000 83.7, 73.3 and 77.3, 24 x 8 over 16000 41.6, 35.9 and 42.1, 16 x 8 over 8000 20.4, 21.2 and 28.0.

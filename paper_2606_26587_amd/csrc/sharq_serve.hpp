@@ -42,7 +42,7 @@ constexpr int kMaxBeams = 32;
 constexpr int kBeamPer = 32;                        // logits of a thread in one turn
 constexpr int kBeamTile = 256 * kBeamPer;           // of a workgroup
 constexpr int kBeamLists = 256;                     // candidate lists of a group: a thread each in the second kernel
-constexpr int64_t kBeamLds = 60 << 10;              // what that kernel keeps in LDS at most
+constexpr int64_t kBeamLds = 56 << 10;              // what that kernel keeps in LDS at most, beside 5 KB of its own
 
 // Bytes of LDS that joins the lists of `chunks` parts of a row: their entries, and as many candidates.
 constexpr int64_t beam_lds(int64_t beams, int64_t chunks) { return beams * beams * chunks * (8 + 16); }

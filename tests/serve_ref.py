@@ -50,8 +50,9 @@ def log_probabilities(x):
         return x - (top + np.log(np.exp(x - top).sum()))
 
 
-def candidates(x, scores, done, eos):
-    """x [beams, vocab], scores [beams] -> [(score, beam, token)], the best first, ties by the lower beam, then token."""
+def candidates(x, scores, done, eos, most=None):
+    """x [beams, vocab], scores [beams] -> [(score, beam, token)], the best first, ties by the lower beam, within a beam by
+    the logits and the lower token; of each beam the first `most`."""
     out = []
     for b in range(len(scores)):
         if not np.isfinite(scores[b]):
@@ -61,8 +62,12 @@ def candidates(x, scores, done, eos):
             continue
         with np.errstate(all="ignore"):
             t = np.float64(scores[b]) + log_probabilities(x[b])
-        out += [(float(t[v]), b, v) for v in np.nonzero(t > -np.inf)[0]]
-    return sorted(out, key=lambda c: (-c[0], c[1], c[2]))
+        at = np.nonzero(t > -np.inf)[0]
+        if most is not None and len(at) > 4 * most:      # those that reach the `most`-th largest
+            at = at[x[b][at] >= np.partition(x[b][at], len(at) - most)[len(at) - most]]
+        at = at[np.lexsort((at, -x[b][at]))][:most]
+        out += [(float(t[v]), b, int(v)) for v in at]
+    return sorted(out, key=lambda c: (-c[0], c[1]))
 
 
 def reorder(parents, length, page, table, ids=None, tokens=None):
