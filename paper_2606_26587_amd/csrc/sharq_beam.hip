@@ -166,6 +166,7 @@ __global__ __launch_bounds__(256) void k_beam_scan(BeamArgs a) {
   __shared__ uint64_t lds_entry[4][kListCap], lds_best[4][kMaxBeams];
   __shared__ float lds_value[4][kListCap];
   __shared__ int lds_turn[4][kListCap];
+  __shared__ float lds_least[4];
   const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int row = (int)(blockIdx.x / (unsigned)a.chunks), chunk = (int)(blockIdx.x % (unsigned)a.chunks);
   const T* const x = static_cast<const T*>(a.logits) + (int64_t)row * a.ld;
@@ -187,9 +188,7 @@ __global__ __launch_bounds__(256) void k_beam_scan(BeamArgs a) {
       w[k] = *reinterpret_cast<const v4u_any*>(x + (at + kVec <= a.vocab ? at : 0));
     }
   };
-  auto cut = [&] {   // the list to what reaches its own bound
-    wave_sync();
-    if (n >= a.beams) least = __builtin_fmaxf(least, least_of(value, n, a.beams));
+  auto keep = [&] {   // of the list what reaches `least`
     int kept = 0;
     for (int i = 0; i < n; i += 64) {
       const float y = i + lane < n ? value[i + lane] : -__builtin_inff();
@@ -266,19 +265,31 @@ __global__ __launch_bounds__(256) void k_beam_scan(BeamArgs a) {
         value[to] = top, turn[to] = base + lane * kVec;
       }
       n += __popcll(who);
-      if (n > kListCap - 64) cut();
+      if (n > kListCap - 64) {
+        wave_sync();
+        least = __builtin_fmaxf(least, least_of(value, n, a.beams));
+        keep();
+      }
       if (n > kListCap - 64) full = true, n = 0;
     }
   }
   sum = wave_sum(sum);
   const int64_t part = (int64_t)row * a.chunks + chunk;
   if (lane == 63) a.parts[part * 4 + wave] = BeamPart{sum, ref, 0};
-  cut();
+  // What one wavefront's logits say holds for all four.
+  wave_sync();
+  if (n >= a.beams) least = __builtin_fmaxf(least, least_of(value, n, a.beams));
+  if (lane == 0) lds_least[wave] = least;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 4; ++i) least = __builtin_fmaxf(least, lds_least[i]);
+  keep();
   int found = 0;
   if (!full) {
-    for (int i = 0; i < n * kBeamPer; i += 64) {   // two turns of a lane at a time
-      const int at = i + lane, k = at % kBeamPer;
-      const int col = at < n * kBeamPer ? turn[at / kBeamPer] + k / kVec * 64 * kVec + k % kVec : a.vocab;
+    // two turns of a lane at a time
+    const int k = lane % kBeamPer, off = k / kVec * 64 * kVec + k % kVec;
+    for (int i = lane / kBeamPer; i - lane / kBeamPer < n; i += 2) {
+      const int col = i < n ? turn[i] + off : a.vocab;
       const float y = col < a.vocab ? as_float(x[col]) : -__builtin_inff();
       const unsigned long long who = __ballot(y >= least && y > -__builtin_inff());
       const int to = found + __popcll(who & ((1ull << lane) - 1));
