@@ -33,7 +33,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_shared(AttnArgs a, AttnSplit pr
   else attn_few<D, F, NQ, NT>(a, block - prefix_blocks, chunk_tiles, 0, lds.few);
 }
 
-// Prompts and single tokens over a cache of codes in one call, none of them split: the tiles of 128 rows first, then a
+// Prompts and single tokens over a cache of codes (MXFP4, E4M3) in one call, none of them split: the tiles of 128 rows first, then a
 // workgroup for each sequence of few rows.
 template <int D, int F>
 __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void k_attn_mixed(AttnArgs a, int rows_blocks, int tiles) {

@@ -150,7 +150,8 @@ constexpr AttnPlan attn_plan(int64_t seqs, int64_t rows, int64_t max_rows, int64
   // The kernel for few rows up to 16, and up to 32 or 64 where it is the faster one.  In it and in the kernel for many:
   // bf16, heads of 128, 16 x 8 tokens of 4 query heads over 8000 87 and 81 us, 64 x 5 over 600 29 and 25, 1 x 8 over
   // 4000 13.6 and 14.4; heads of 64, 2 x 8 over 16000 19 and 23, 16 x 12 over 8000 62 and 58; MXFP4, heads of 64,
-  // 16 x 12 39 and 53.  (64 rows' states over heads of 128 fill the registers.)
+  // 16 x 12 39 and 53; E4M3, 16 x 8 over 8000 28 and 34, 64 x 4 of 8 over 4000 43 and 56, heads of 64 with 48 rows 26
+  // and 33.  (64 rows' states over heads of 128 fill the registers.)
   p.few = r <= 16 ? 1 : r <= 32 && (D == 64 || mx) ? 2 : r <= 64 && D == 64 && mx ? 4 : 0;
   // tokens that a tile of rows sees at most: its window and its own positions, and the sinks
   const int64_t span = p.few ? max_rows : kAttnRows / group + 2;
@@ -208,7 +209,8 @@ constexpr AttnPlan attn_plan(int64_t seqs, int64_t rows, int64_t max_rows, int64
     // and 99 us, 6 prompts of 1000 and 4 single tokens over 8000 (mean 0.6) 171 and 119, 16 of 1000 and 16 over 4000 216
     // and 209, but 2 of 2000 and 6 over 4000 95 and 104; prompts alone, whose lengths differ, 20 of 125 to 2000 302 and
     // 300, 1000, 400 and 300 29.2 and 28.9, heads of 64 185 and 186.  (bf16: 240 and 226, but a chunk of 512 and 31
-    // single tokens over 8000 238 and 251.)
+    // single tokens over 8000 238 and 251.)  E4M3, in the same order: 159 and 137, 175 and 129, 227 and 226, 98 and 113,
+    // 1000, 400 and 300 29.0 and 29.7; heads of 64, a prompt of 2000 and 63 single tokens 74 and 51.
     p.mixed = mx && !p.shared && p.own.chunks == 1 && 3 * rows < 2 * seqs * max_rows;
   }
   p.slots = p.own.chunks > 1 ? p.own.chunks : 0;
