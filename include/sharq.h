@@ -497,7 +497,11 @@ SHARQ_API size_t sharq_kv_buffer_bytes(const sharq_kv_cache *c, int32_t which);
  * where the new ones need a larger one, their codes are rounded again to it (which
  * changes only values that become subnormal codes).  Bytes of the block's other
  * slots stay.  A value that is not finite is stored as NaN and does not count for
- * the scale.
+ * the scale.  Where all of a block's tokens have been left out so far (or their page
+ * was absent) nothing has written its scale either, and the byte is what the page held
+ * before.  One outside [10, 247] is no scale: the first tokens that are stored then get
+ * one of their own.  A caller that leaves out a block's first rows clears the
+ * scales (to 0) of pages that are used again; otherwise the byte found there counts.
  */
 SHARQ_API sharq_status sharq_kv_append(const void *Q, const void *K, const void *V, sharq_dtype xdt, int64_t q_heads,
                                        int64_t ldq, int64_t ldk, int64_t ldv, const float *cos, const float *sin,

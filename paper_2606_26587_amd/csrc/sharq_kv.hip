@@ -169,16 +169,19 @@ __device__ __forceinline__ void append8_block(const KvAppendArgs& a, const KvCac
   float lo[N], hi[N];
   load_halves<D, N>((is_v ? a.v + r * a.ldv : a.k + r * a.ldk) + h * D + j, lo, hi);
   uint32_t old[2][N / 4] = {};
-  const bool was = olds && t < from;
+  bool was = olds && t < from;
   int before = kF8Least;
   if (olds) {   // on its way with the row's values, whether the scale grows or not
-    before = (int)*scale - 127;
+    const int held = (int)*scale - 127;
     if (was)
 #pragma unroll
       for (int i = 0; i < N / 4; ++i) {
         old[0][i] = reinterpret_cast<const uint32_t*>(codes)[i];
         old[1][i] = reinterpret_cast<const uint32_t*>(codes + D / 2)[i];
       }
+    // no scale that an append leaves: the tokens before these were left out, and nothing of theirs is here
+    if (held < kF8Least || held > kF8Most) was = false;
+    else before = held;
   }
   if (a.cos) {
     const int angle = a.pos ? a.pos[r] : pos + (r - row);

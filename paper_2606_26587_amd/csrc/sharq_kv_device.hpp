@@ -52,7 +52,8 @@ __device__ __forceinline__ uint32_t bf16x2(float a, float b) {
 // `peak`: floor(log2 peak) - 8, or ceil(log2(peak / 448)), which is one more
 // where the mantissa is above 1.75 (448 = 1.75 * 2^8), i.e. where adding
 // 0x1FFFFF carries.  At least -117: the least code, 2^-9, is then a normal bf16.
-constexpr int kF8Least = -117;
+// At most 120, of the largest fp32.
+constexpr int kF8Least = -117, kF8Most = 120;
 constexpr uint32_t kF8Floor = 0u, kF8Ceil = 0x1FFFFFu;
 __device__ __forceinline__ int f8_exponent(uint32_t peak, uint32_t rule_bias) {
   const int e = (int)((peak + rule_bias) >> 23) - 135;

@@ -427,13 +427,16 @@ class KVRequests:
 
 def alloc_kv_cache(pages: int, page_size: int, kv_heads: int, head_dim: int, fmt: str = "bf16", device="cuda",
                    scale_rule: str = "floor") -> KVCache:
-    """An empty paged cache; its pages are read only where something was appended."""
+    """An empty paged cache; its pages are read only where something was appended.  The scales of "fp8" are cleared on
+    the current stream: a block without a token has none, whatever rows the first append leaves out."""
     shape = (pages, kv_heads, page_size)
     if KV_FORMATS[fmt] != 1:
         dtype = _KV_DTYPES[KV_FORMATS[fmt]]
         codes = [torch.empty(shape + (head_dim,), dtype=dtype, device=device) for _ in "kv"]
-        scales = [torch.empty(shape[:2] + (page_size // KV_BLOCK,), dtype=torch.uint8, device=device) for _ in "kv"]
-        return KVCache(fmt, *codes, *(scales if KV_FORMATS[fmt] == 2 else ()), scale_rule=scale_rule)
+        scales = ()
+        if KV_FORMATS[fmt] == 2:
+            scales = [torch.zeros(shape[:2] + (page_size // KV_BLOCK,), dtype=torch.uint8, device=device) for _ in "kv"]
+        return KVCache(fmt, *codes, *scales, scale_rule=scale_rule)
     return KVCache(fmt, *(torch.empty(shape + (head_dim // n,), dtype=torch.uint8, device=device)
                           for n in (2, 2, 32, 32)), scale_rule=scale_rule)
 
