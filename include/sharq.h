@@ -601,9 +601,11 @@ typedef struct {
  *   lens         device int32 [seqs], written (it may be `keep`).
  *   page_table   device int32 [seqs][ld_table]: new columns are written.
  *   own_table    device int32 [seqs][ld_table] or NULL: new columns are written
- *                there as well, and pages that go back are taken from it.  For
+ *                there as well, and pages that go back are taken from it.  Needed for
  *                sequences whose page_table names pages of others (beams that share
- *                a prompt: -1 in own_table where the page is another's).
+ *                a prompt, any tables that sharq_beam_reorder has written): -1 in
+ *                own_table where the page is another's.  With NULL, a page that several
+ *                rows name would go back once for each of them.
  *   row_seq, positions, slots
  *                device int32 [rows] or NULL: of every row its sequence, its
  *                position and its slot in the pool, page * page_size + position %
@@ -679,6 +681,9 @@ SHARQ_API sharq_status sharq_beam_select(const void *logits, sharq_dtype dtype, 
  *                       page that is partly filled goes to a parent's first child; each
  *                       further child takes over the page of a parent without children
  *                       (in order; there are as many).  Columns behind stay a beam's own.
+ *                       Rows then share pages: sharq_kv_assign takes what goes back from
+ *                       an own_table, which is not reordered, and a group's beams end
+ *                       together.
  *   copies              device int32 [groups * beams][3], with table: (source page, destination
  *                       page, tokens) of what has to be copied into the pages taken over,
  *                       for sharq_kv_copy on the caches of all layers; -1s for

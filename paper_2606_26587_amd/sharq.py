@@ -385,7 +385,9 @@ class KVRequests:
     stay, tokens that come, columns of the page table that are filled); row_offsets [seqs + 1], lens [seqs] (it may be
     `keep`) and page_table [seqs, n], written by sharq_kv_assign and then those of a KVBatch; rows: entries of the row
     arrays; max_len: no sequence gets longer.  Optional: held_out [seqs] (None: `held` itself), own_table like
-    page_table, row_seq, positions, slots [rows], missing [1]."""
+    page_table, row_seq, positions, slots [rows], missing [1].  Where sequences share pages, as beams do behind
+    sharq_beam_reorder, own_table is needed: pages that go back are then taken from it (-1: another's page), not from
+    page_table, whose rows name the same page more than once."""
     keep: torch.Tensor
     add: torch.Tensor
     held: torch.Tensor
@@ -865,7 +867,8 @@ def sharq_beam_reorder(parents: torch.Tensor, lens: torch.Tensor, page_table: Op
     """The beams' page tables and token ids behind a choice: parents int32 [groups, beams], lens int32 [groups * beams]
     (a group's beams have the same), page_table int32 [groups * beams, n] or None, ids int32 [groups * beams, n] with the
     chosen tokens, or None.  table_out, ids_out: None, in place.  Returns copies int32 [groups * beams, 3], what
-    sharq_kv_copy has to do in every layer's cache (None without a table)."""
+    sharq_kv_copy has to do in every layer's cache (None without a table).  Rows of the new tables share pages: from then
+    on their KVRequests need an own_table, which is not reordered."""
     where = "sharq_beam_reorder"
     dev = parents.get_device()
     if dev < 0 or dev != _device() or parents.dim() != 2:
