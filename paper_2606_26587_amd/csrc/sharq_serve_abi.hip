@@ -129,6 +129,7 @@ sharq_status sharq_beam_reorder(int64_t groups, int64_t beams, const int32_t* pa
   if (groups == 0 || (!table && !ids)) return SHARQ_OK;
   if (!parents || !lens) return SHARQ_EINVAL;
   const int64_t units = (table ? reorder_units(cols > 0 ? cols : 1) : 0) + (ids ? reorder_units(id_cols) : 0);
+  if (units == 0) return SHARQ_OK;   // token ids without columns
   if (!kv_launches(groups * ((units + 3) / 4), 256)) return SHARQ_EUNSUPPORTED;
   const ReorderArgs a{parents, lens, tokens, table, table_out, ldt, ldto, ids, ids_out, ldi, ldio, copies, (int)beams,
                       (int)cols, (int)id_cols, __builtin_ctz((unsigned)page_size)};
