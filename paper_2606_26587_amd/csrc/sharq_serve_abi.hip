@@ -122,7 +122,7 @@ sharq_status sharq_beam_reorder(int64_t groups, int64_t beams, const int32_t* pa
     return SHARQ_EINVAL;
   if ((table && (ldt < cols || ldto < cols || !copies)) || (ids && (ldi < id_cols || ldio < id_cols)))
     return SHARQ_EINVAL;
-  if ((table == table_out && ldt != ldto) || (ids == ids_out && ldi != ldio)) return SHARQ_EINVAL;
+  if ((table && table == table_out && ldt != ldto) || (ids && ids == ids_out && ldi != ldio)) return SHARQ_EINVAL;
   for (const void* p : {(const void*)parents, (const void*)lens, (const void*)table, (const void*)table_out,
                         (const void*)copies, (const void*)tokens, (const void*)ids, (const void*)ids_out})
     if (!aligned(p, 4)) return SHARQ_EALIGN;
