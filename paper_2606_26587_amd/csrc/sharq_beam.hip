@@ -357,7 +357,7 @@ constexpr int kPickThreads = 512;
 // Joins a group's lists.  A thread has one list, whose entries come best first.  As `beams` lists reach the `beams`-th of
 // a wavefront's first entries, nothing below can be chosen; what is not below it is ranked.
 __global__ __launch_bounds__(kPickThreads) void k_beam_pick(BeamArgs a) {
-  extern __shared__ uint64_t lds[];
+  extern __shared__ BeamKey found[];   // up to as many as there are entries
   __shared__ double base_of[kMaxBeams], lse_of[kMaxBeams];
   __shared__ uint8_t done_of[kMaxBeams];
   __shared__ BeamPart part_of[kBeamLists];
@@ -365,8 +365,7 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(BeamArgs a) {
   __shared__ int count;
   const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), beams = a.beams;
   const int lists = beams * a.chunks, entries = lists * beams;
-  BeamKey* const found = reinterpret_cast<BeamKey*>(lds);         // up to as many as there are entries
-  uint64_t* const entry = lds + 2 * entries;                      // [lists][beams]
+  uint64_t* const entry = reinterpret_cast<uint64_t*>(found + entries);   // [lists][beams]
   const int64_t row0 = (int64_t)blockIdx.x * beams;
   const uint64_t* const from = a.lists + row0 * a.chunks * beams;
   const int b = tid < lists ? tid / a.chunks : 0;
