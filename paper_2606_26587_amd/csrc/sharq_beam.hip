@@ -31,6 +31,7 @@ constexpr float kLog2e = 1.44269504088896341f;
 constexpr float kRefStep = 8.0f;
 constexpr float kRefFast = 1000.0f;   // z below 2^-16: its third power is nothing in 64 bits
 constexpr int kListCap = 256;   // entries of a wavefront's list
+constexpr int kListCut = 64;    // logits beyond which only the best of them stay (at 192: masked 32 x 8 x 152064 63 us, not 46)
 
 // An order of whole numbers that is the floats'; -0 counts as 0.
 __device__ __forceinline__ uint32_t order32(float x) {
@@ -121,16 +122,6 @@ __device__ __forceinline__ double exponent_of(float ref, float& rest) {
   return e;
 }
 
-__device__ __forceinline__ uint64_t wave_max64(uint64_t x) {
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const uint64_t o = (uint64_t)(uint32_t)__shfl_xor((int)(uint32_t)x, d) |
-                       (uint64_t)(uint32_t)__shfl_xor((int)(uint32_t)(x >> 32), d) << 32;
-    x = o > x ? o : x;
-  }
-  return x;
-}
-
 // An entry of a sorted list: the value's order above, the complement of its column below, so that of equal values the
 // lower column is the better.
 __device__ __forceinline__ uint64_t entry_of(float x, int col) { return (uint64_t)order32(x) << 32 | (uint32_t)~col; }
@@ -174,7 +165,6 @@ __global__ __launch_bounds__(256) void k_beam_scan(BeamArgs a) {
   float* const value = lds_value[wave];    // of a listed turn of a lane: its largest logit, and
   int* const turn = lds_turn[wave];        // its first column
   int n = 0;                         // how many there are
-  bool full = false;                 // more than the list holds are equal to the bound
   float least = -__builtin_inff();   // what has to be passed: `beams` logits before reach it
   float ref = -__builtin_inff();
   float rest = 0.0f;
@@ -188,12 +178,12 @@ __global__ __launch_bounds__(256) void k_beam_scan(BeamArgs a) {
       w[k] = *reinterpret_cast<const v4u_any*>(x + (at + kVec <= a.vocab ? at : 0));
     }
   };
-  auto keep = [&] {   // of the list what reaches `least`
+  auto keep = [&](int limit) {   // of the list what reaches `least`; what equals it before column `limit` only
     int kept = 0;
     for (int i = 0; i < n; i += 64) {
       const float y = i + lane < n ? value[i + lane] : -__builtin_inff();
       const int t = i + lane < n ? turn[i + lane] : 0;
-      const unsigned long long who = __ballot(i + lane < n && y >= least);
+      const unsigned long long who = __ballot(i + lane < n && y >= least && (y > least || t < limit));
       wave_sync();
       if ((who >> lane) & 1) {
         const int to = kept + __popcll(who & ((1ull << lane) - 1));
@@ -268,9 +258,14 @@ __global__ __launch_bounds__(256) void k_beam_scan(BeamArgs a) {
       if (n > kListCap - 64) {
         wave_sync();
         least = __builtin_fmaxf(least, least_of(value, n, a.beams));
-        keep();
+        keep(a.vocab);
+        // Many equal ones are left.  The list is in the order of turns: what equals the bound behind the turn that has
+        // the `beams`-th is not chosen, so there are at most 63 more of this turn, and fewer than `beams` above.
+        if (n > kListCap - 64) {
+          const int reached = __builtin_amdgcn_readfirstlane(turn[a.beams - 1]) - begin;
+          keep(begin + (reached / kBeamTile + 1) * kBeamTile);
+        }
       }
-      if (n > kListCap - 64) full = true, n = 0;
     }
   }
   sum = wave_sum(sum);
@@ -283,44 +278,44 @@ __global__ __launch_bounds__(256) void k_beam_scan(BeamArgs a) {
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < 4; ++i) least = __builtin_fmaxf(least, lds_least[i]);
-  keep();
+  keep(a.vocab);
   int found = 0;
-  if (!full) {
-    // two turns of a lane at a time
+  {
+    // Two turns of a lane at a time, four such loads on their way.  Where many logits reach the bound (a mask's, wide
+    // beams) the best so far take their places, and what is not better than the last of these stays out.  A part of a row
+    // with fewer than `beams` tokens left by a mask of the type's lowest value: 2048 equal logits.  10 tokens left of
+    // 152064, 32 x 8 beams 46 us (unmasked 31), 1 x 32 43 us (53); walking the part once for each beam took 486 and 1513.
     const int k = lane % kBeamPer, off = k / kVec * 64 * kVec + k % kVec;
-    for (int i = lane / kBeamPer; i - lane / kBeamPer < n; i += 2) {
-      const int col = i < n ? turn[i] + off : a.vocab;
-      const float y = col < a.vocab ? as_float(x[col]) : -__builtin_inff();
-      const unsigned long long who = __ballot(y >= least && y > -__builtin_inff());
-      const int to = found + __popcll(who & ((1ull << lane) - 1));
-      if (((who >> lane) & 1) && to < kListCap) entry[to] = entry_of(y, col);
-      found += __popcll(who);
+    uint64_t floor = 0;
+    for (int first = 0; first < n; first += 8) {
+      float y[4];
+      int col[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int i = first + 2 * j + lane / kBeamPer;
+        col[j] = i < n ? turn[i] + off : a.vocab;
+        y[j] = col[j] < a.vocab ? as_float(x[col[j]]) : -__builtin_inff();
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint64_t e = entry_of(y[j], col[j]);
+        const unsigned long long who = __ballot(y[j] >= least && y[j] > -__builtin_inff() && e > floor);
+        if ((who >> lane) & 1) entry[found + __popcll(who & ((1ull << lane) - 1))] = e;
+        found += __popcll(who);
+        if (found > kListCut) {
+          wave_sync();
+          best_of(entry, found, a.beams, best);
+          wave_sync();
+          found = a.beams;
+          if (lane < found) entry[lane] = best[lane];
+          floor = best[found - 1];
+          wave_sync();
+        }
+      }
     }
     wave_sync();
-    if (found <= kListCap) {
-      best_of(entry, found, a.beams, best);
-      found = found < a.beams ? found : a.beams;
-    } else {
-      full = true;
-    }
-  }
-  if (full) {   // rows of equal values: the best of all, one after the other
-    uint64_t last = ~0ull;
-    for (found = 0; found < a.beams; ++found) {
-      uint64_t mine = 0;
-      for (int base = begin; base < end; base += kBeamTile)
-#pragma unroll 8
-        for (int i = 0; i < kBeamPer; ++i) {
-          const int col = base + i * 64 + lane;
-          const float y = col < a.vocab ? as_float(x[col]) : -__builtin_inff();
-          const uint64_t e = entry_of(y, col);
-          if (y > -__builtin_inff() && e < last && e > mine) mine = e;
-        }
-      mine = wave_max64(mine);
-      if (mine == 0) break;
-      if (lane == 0) best[found] = mine;
-      last = mine;
-    }
+    best_of(entry, found, a.beams, best);
+    found = found < a.beams ? found : a.beams;
   }
   if (lane >= found && lane < a.beams) best[lane] = 0;
   __syncthreads();
