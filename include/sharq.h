@@ -662,7 +662,9 @@ SHARQ_API size_t sharq_beam_workspace_bytes(int64_t groups, int64_t beams, int64
  * A logit of -inf is no candidate, nor is any of a beam whose score is not finite or
  * whose logits hold a NaN or +inf.  Where a group has fewer than `beams`
  * candidates, the places behind have score -inf, token -1 and themselves as parent.
- * Scores are compared in 64 bits, whatever their rounding to scores_out.
+ * Scores are compared in 64 bits, whatever their rounding to scores_out.  Exponentials and
+ * the sums of 32 of them are fp32: lse_b is within 2^-19 (about 1e-8 measured), and only
+ * candidates of different beams that lie closer than that may change places.
  * groups * beams is at most 2^20, beams * vocab at most 2^30.  workspace: 8-byte aligned;
  * calls that may run at the same time need workspaces of their own.
  */
@@ -689,9 +691,10 @@ SHARQ_API sharq_status sharq_beam_select(const void *logits, sharq_dtype dtype, 
  *                       for sharq_kv_copy on the caches of all layers; -1s for
  *                       the others.
  *   tokens, ids, ids_out
- *                       or all NULL: chosen tokens int32 [groups][beams], and the sequences' tokens, device int32
- *                       [groups * beams][id_cols], row strides ldi, ldio (ids_out may
- *                       be `ids`): ids_out[i][t] = ids[parents[i]][t] for t < len,
+ *                       chosen tokens, device int32 [groups][beams], and the sequences'
+ *                       tokens, device int32 [groups * beams][id_cols], row strides ldi,
+ *                       ldio (ids_out may be `ids`), or all NULL:
+ *                       ids_out[i][t] = ids[parents[i]][t] for t < len,
  *                       ids_out[i][len] = tokens[i]; columns behind are left as they were.
  * Parents outside [0, beams) count as the nearest inside.  Outputs overlap inputs only where
  * they are the same array.  groups * beams is at most 2^20.

@@ -9,9 +9,14 @@
 //
 // Measured, bf16: 32 groups of 8 beams over 152064 tokens (78 MB, some beams done)
 // 23 us and 7.8 for the join, 3.4 TB/s; one group of 4 over 128256 6.8 and 5.5.
-// What bounds the first is the VALU (32 exponentials at a quarter of its rate and
-// 180 other operations for 32 logits of a lane, 16 of the 22 us) beside what every
-// launch takes to begin and end; the second and the join are chains of latencies.
+// No one unit bounds the first: vector units are active for 27700 cycles of each
+// SIMD (11.5 us at 2.4 GHz; 370 instructions a wavefront and turn, its beginning and
+// end among them), a wavefront waits for memory or the others in 43% of its 30000
+// cycles and for its turn to issue in 25%, and launch, first loads, five turns and
+// the end of 1024 workgroups, all there at once, follow one another.  The second and
+// the join are chains of latencies.  One group of 16, 24 and 32 beams over 152064,
+// whole calls: 22, 43 and 61 us (3, 5 and 10 turns on 112, 96 and 64 workgroups,
+// as the join's LDS allows).  fp32: 16 x 8 x 152064, the same bytes, 27 us for 31.
 // Listing single logits during the walk, not a lane's 32 by their largest, took
 // 27.6 us; loading a row's last logits one by one, and loads that wait before the
 // turn they are for, 36; joining lists with 64-bit exponentials 9 for 5.5.

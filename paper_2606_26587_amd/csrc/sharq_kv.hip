@@ -4,11 +4,11 @@
 // into an MXFP4 cache 86 us (5.1 TB/s).  Read back: 22000 rows of 8 heads of 128 from
 // a bf16 cache 38.5 us (4.7 TB/s); 20144 from an MXFP4 one 28.5 us, where a row's
 // workgroup takes part of the cache lines that its neighbours take too, over
-// several XCDs: 47 MB are fetched of 22 held.  An E4M3 cache: 8600 rows of 6 chunks
+// several XCDs: 47 MB are fetched of 22 held.  An E4M3 cache: 8900 rows of 6 chunks
 // of up to 2048, 32 + 8 + 8 heads of 128 (205 MB), 43 us, 4.8 TB/s; with the
-// queries first, or a head a thread, 48.7.  One row takes
-// 2.7 us, the chain of offsets, length, page table and store; the row's values are
-// loaded beside it.
+// queries first, or a head a thread, 48.7; read back, 22000 rows as above, 38.7 us
+// (3.5 TB/s).  One row takes 2.7 us, the chain of offsets, length, page table and
+// store; the row's values are loaded beside it.
 //
 // Rotation of a head's pair (x_j, x_{j + D/2}) by the angle of its position:
 //   y_j = x_j c_j - x_{j+D/2} s_j,  y_{j+D/2} = x_{j+D/2} c_j + x_j s_j,

@@ -222,7 +222,10 @@ constexpr AttnPlan attn_plan(int64_t seqs, int64_t rows, int64_t max_rows, int64
     p.prefix = attn_split(tiles, units, kv, 256, 2);
     // Where that leaves long walks (then the partial results weigh less), twice as many: 32 x up to 32 tokens behind 4096,
     // 32 and 8 heads of 128, 94.7 and 82.8 us, behind 16384 339 and 258; 4 single tokens behind 61440 in MXFP4 48.4 and
-    // 35.2; 256 behind 16384 118 and 122, in MXFP4 106 and 103.  (8 x 100 behind 2048, 32 tiles: 39.5 and 45.2.)
+    // 35.2; 256 behind 16384 118 and 122, in MXFP4 106 and 103.  (8 x 100 behind 2048, 32 tiles: 39.5 and 45.2.)  The
+    // same for E4M3, of which other splits were not measured: 64 single tokens behind 8192, 400 of their own each, in
+    // bf16, E4M3 and MXFP4 48.8, 35.4 and 30.5 us; 16 behind 32768 43.8, 36.9 and 36.0; 32 x 8 behind 4096 40.2, 39.7 and
+    // 41.5.
     if (kv >= 48 && p.prefix.chunk_tiles >= 28) p.prefix = attn_split(tiles, units, kv, 512, 2);
     p.slots = p.own.chunks + p.prefix.chunks;
   }
